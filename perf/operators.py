@@ -266,7 +266,7 @@ def prepare(case, seed):
         st.g = paged.Paged(c["batch"], c["hq"], c["hkv"], c["d"], c["page"], x["n_pages"], x["max_pages"],
                            window=_window(c), n_sinks=c["sinks"], dtype=DTYPE[c["dtype"]])
         st.cache = st.g.cache(x["k_pool"], x["v_pool"], x["table"], x["lens"], x["w_pool"])
-        st.ws = st.g.new_workspace(st.cu[-1] if c["op"] == "prefill" else 0)
+        st.ws = st.g.new_workspace(st.cu[-1] if c["op"] == "prefill" else 0, weights=x["w_pool"] is not None)
     return st
 
 
