@@ -279,6 +279,120 @@ glide_status glide_state_flush(const glide_config* cfg, void* state, size_t stat
 glide_status glide_feature_map(const glide_config* cfg, const void* phi_w, const void* x,
                                int64_t rows, void* out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged softmax cache: layers that stay softmax attention over the whole
+ * context, or over a sliding window and a few first tokens ("sinks"), on a
+ * key-value cache held in pages; the attention weight that each cached token
+ * has received; and the eviction of the tokens that received least.
+ *
+ * The query at position t of a sequence of len cached tokens (its own among
+ * them) sees
+ *   visible(t) = { j <= t : j > t - W or j < n_sinks, j's page allocated }
+ *   O_t   = sum_{visible} e^{tau q_t.k_j} v_j / sum_{visible} e^{tau q_t.k_j}
+ *   lse_t = log sum_{visible} e^{tau q_t.k_j}
+ * O_t = 0 and lse_t = -inf where nothing is visible.  W at or beyond the
+ * context gives causal softmax attention, as for a GLIDE layer; W = 0 leaves
+ * the sinks alone.  What a query does not see, page slots behind a sequence's
+ * last token and pages that are not allocated have no part in its row,
+ * whatever bits they hold; but a NaN or infinity in a value row that some
+ * query of a call sees may reach the rows of other queries of that call (not
+ * of other sequences or KV heads).
+ *
+ * A sequence is its cached tokens in order: after an eviction, positions (and
+ * with them W, n_sinks) count the tokens that were kept. */
+typedef struct {
+  int32_t batch;       /* sequences B (>= 1) */
+  int32_t n_q_heads;   /* Hq */
+  int32_t n_kv_heads;  /* Hkv; Hq % Hkv == 0, G = Hq / Hkv in [1, 16] */
+  int32_t head_dim;    /* d: 64 or 128 */
+  int32_t dtype;       /* GLIDE_F32 or GLIDE_BF16 */
+  int32_t page_size;   /* tokens per page: a power of two in [1, 1024] */
+  int32_t n_pages;     /* pages of the pools (>= 1) */
+  int32_t max_pages;   /* entries of a block-table row (>= 1); max_pages * page_size <= 2^30 */
+  int32_t window;      /* W in [0, 2^30]; 0 only with sinks */
+  int32_t n_sinks;     /* first tokens that stay visible, in [0, 2^20] */
+  float sm_scale;      /* tau */
+} glide_paged_config;
+
+/* The cache of one layer, as device pointers (host struct, read during the
+ * call).  A token's rows are d consecutive elements; row `slot` of KV head g
+ * in page p is at p * strides[0] + g * strides[1] + slot * strides[2]
+ * elements (each stride a multiple of 16 bytes).  weights, where kept, is
+ * contiguous.  block_table [B][max_pages]: token j of sequence b is in slot
+ * j % page_size of page block_table[b][j / page_size]; an entry outside
+ * [0, n_pages) is not allocated: its tokens are not visible and what is
+ * written to them is dropped.  lens [B]: tokens cached, after the call's own
+ * appends (taken as 0 below 0, as max_pages * page_size above it).  A page
+ * that a call writes to belongs to one sequence. */
+typedef struct {
+  void* k;                    /* K pool, cfg->dtype */
+  void* v;                    /* V pool */
+  float* weights;             /* [n_pages][Hkv][page_size], or NULL */
+  const int32_t* block_table;
+  const int32_t* lens;
+  int64_t k_strides[3], v_strides[3];
+} glide_paged_cache;
+
+/* Workspace bytes that serve every glide_paged_* call of this config, prefills
+ * up to max_total_tokens packed tokens; weights != 0: with cache->weights.  At
+ * least 256; 0 if cfg is invalid.  Nothing in it need be cleared, and nothing
+ * is kept in it from one call to the next; calls that overlap in time need
+ * workspaces of their own. */
+size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_total_tokens, int32_t weights);
+
+/* Appends T_b = cu[b+1] - cu[b] >= 0 tokens to every sequence b and reads out
+ * one row per appended token and query head: token i of sequence b is at
+ * position lens[b] - T_b + i.  With cache->weights, the weights of the
+ * appended tokens start from 0, and the last min(T_b, n_observe) queries of
+ * every sequence add theirs,
+ *   weights_j += sum over those queries t and the G heads of e^{tau q_t.k_j - lse_t}.
+ *   q        device [T][Hq][d]      T = total_tokens, packed by sequence
+ *   k, v     device [T][Hkv][d]; both NULL: the tokens are in the cache
+ *   cu_seqlens_host  HOST [B+1], cu[0] = 0, non-decreasing, cu[B] = T; one
+ *            sequence's T_b * Hq * d * element bytes < 2^31, else
+ *            GLIDE_ERR_UNSUPPORTED
+ *   n_observe  >= 0; > 0 needs cache->weights
+ *   max_len  the caller's upper bound of lens (0: the table's capacity): the
+ *            work is split by it; a wrong one costs time only
+ *   out      device [T][Hq][d];  lse  device fp32 [T][Hq], or NULL
+ * Device pointers 16-byte aligned (lse, weights, block_table, lens: 4;
+ * workspace: 256). */
+glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_paged_cache* cache,
+                                 const void* q, const void* k, const void* v,
+                                 const int32_t* cu_seqlens_host, int64_t total_tokens, int32_t n_observe,
+                                 int64_t max_len, void* out, float* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* One token per sequence: appends it (k, v given), at position lens[b] - 1,
+ * and reads out its row.  A sequence of lens[b] = 0 has no token: nothing is
+ * appended, its row is 0.  With cache->weights every sequence's query adds its
+ * weights (the appended token's from 0).
+ *   q device [B][Hq][d];  k, v device [B][Hkv][d], or both NULL
+ *   out device [B][Hq][d];  lse device fp32 [B][Hq], or NULL
+ * max_len, alignment and errors as for glide_paged_prefill. */
+glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged_cache* cache,
+                                const void* q, const void* k, const void* v, int64_t max_len,
+                                void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* Keeps min(lens[b], budget) tokens of every sequence and KV head, in their
+ * order: the first n_sinks, the last n_recent, and of the others those of the
+ * largest weights (of equal weights the first; a NaN, and a token on a page
+ * that is not allocated, counts as the smallest).  Their rows and weights
+ * become tokens 0, 1, ... of the sequence in dst_table's pages.
+ *   budget >= 1, budget >= n_sinks + n_recent;  n_recent >= 0
+ *   dst_table  device [B][max_pages]; NULL: in place (block_table itself).
+ *              Otherwise its pages of tokens 0 .. min(lens[b], budget) - 1
+ *              are no pages of any sequence in block_table, which is left as
+ *              it is (pages shared between sequences stay whole).
+ *   kept       device int32 [B][Hkv][budget]: the old positions, -1 behind the last
+ *   new_lens   device int32 [B]: min(lens[b], budget); may be cache->lens
+ * Needs cache->weights. */
+glide_status glide_paged_evict(const glide_paged_config* cfg, const glide_paged_cache* cache,
+                               int32_t budget, int32_t n_recent, const int32_t* dst_table,
+                               int32_t* kept, int32_t* new_lens, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* glide_status_string(glide_status s);
 

@@ -1,0 +1,107 @@
+// Launch descriptors of the paged softmax cache (kernels in paged.hip and
+// evict.hip, host side in paged_api.hip).
+#pragma once
+
+#include "glide_internal.h"
+
+namespace glide {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// A running maximum before any score: finite, so that (score - maximum) is
+// never inf - inf; every real score lies far above it.
+constexpr float kNoMax = -1e30f;
+
+// Rows of one workgroup of attend_rows: one MFMA tile of (token, head) pairs.
+constexpr int kPagedRows = 16;
+// Keys of one tile of a wave, and the granularity of a piece (four waves).
+constexpr int kPagedTile = 32;
+constexpr int kPagedPieceMin = 512;
+constexpr int kPagedMaxPieces = 64;
+// Workgroups that a launch is split up to.
+constexpr int kPagedWgs = 1024;
+
+struct PagedArgs {
+  const char *q, *kn, *vn;  // queries; new rows of a decode call (NULL: in the cache)
+  char* out;
+  float* lse;               // natural log; NULL: not asked for
+  char *kp, *vp;
+  float* wp;                // NULL: no weights
+  const int32_t *table, *lens;
+  int64_t ks[3], vs[3];     // page, head, row strides in bytes
+  int32_t B, Hq, Hkv, G;
+  int32_t n_pages, max_pages, shift, cap;  // page_size = 1 << shift; cap = max_pages << shift
+  int32_t W, ns;
+  float scale;              // tau log2(e): scores in the log2 domain
+  int32_t npiece, piece;    // workgroups per row tile, keys of each at least
+  float *acc, *ml;          // partial records: acc [row][npiece][d], ml [row][npiece][2]
+  float* scores;            // decode with weights: [B][Hq][nv] raw scores (log2 domain)
+  float* lse2;              // log2-domain lse by row, where weights need it
+  int64_t nv;               // row length of scores
+};
+
+// The sequences of one prefill launch (at most kMaxSeqPerLaunch), in the
+// kernel arguments.
+struct PagedSeqs {
+  int32_t nseq, seq0;
+  int32_t start[kMaxSeqPerLaunch];     // packed row of the first new token
+  int32_t len[kMaxSeqPerLaunch];       // new tokens
+  int32_t tile0[kMaxSeqPerLaunch + 1]; // first row tile
+};
+
+struct EvictArgs {
+  char *kp, *vp;
+  float* wp;
+  const int32_t *table, *lens, *dst;
+  int64_t ks[3], vs[3];
+  int32_t B, Hkv, d, esize;
+  int32_t n_pages, max_pages, shift, cap;
+  int32_t ns, budget, recent;
+  int32_t in_place;
+  int32_t *kept, *new_lens;
+};
+
+hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const void* k, const void* v, int d, int dtype,
+                               hipStream_t stream);
+hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, hipStream_t stream);
+hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs* s, int n_observe, int64_t keys, int d, int dtype,
+                                hipStream_t stream);
+hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream);
+
+// A row of zeros (device memory): what is read in place of a row that has no
+// part in the sums, so that no bits of it reach a product.
+static __device__ const uint4 zero_row[32] = {};
+
+// Page and slot of position j of the sequence whose table row is `row`;
+// false where its page is not allocated.
+struct Slot {
+  int32_t page, slot;
+  bool ok;
+};
+__device__ __forceinline__ Slot paged_slot(const int32_t* row, int32_t j, int32_t shift, int32_t n_pages) {
+  Slot s;
+  s.page = row[j >> shift];
+  s.slot = j & ((1 << shift) - 1);
+  s.ok = uint32_t(s.page) < uint32_t(n_pages);
+  return s;
+}
+__device__ __forceinline__ int64_t slot_offset(const int64_t* st, const Slot& s, int g) {
+  return int64_t(s.page) * st[0] + int64_t(g) * st[1] + int64_t(s.slot) * st[2];
+}
+
+// The tokens that any query at positions t0 .. t1 sees, counted through: the
+// sinks before the window, then the window.
+struct Seen {
+  int32_t sinks, start, n;  // j(v) = v < sinks ? v : v - sinks + start, v in [0, n)
+  __device__ __forceinline__ int32_t pos(int32_t v) const { return v < sinks ? v : v - sinks + start; }
+};
+__device__ __forceinline__ Seen seen_by(int32_t t0, int32_t t1, int32_t W, int32_t ns) {
+  Seen s;
+  s.start = t0 - W + 1 > 0 ? t0 - W + 1 : 0;
+  if (s.start > t1 + 1) s.start = t1 + 1;  // W = 0
+  s.sinks = ns < s.start ? ns : s.start;
+  s.n = s.sinks + (t1 + 1 - s.start);
+  return s;
+}
+
+}  // namespace glide

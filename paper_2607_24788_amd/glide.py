@@ -30,7 +30,8 @@ DECODE_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = ["glide_state_bytes", "glide_state_layout", "glide_workspace_bytes", "glide_state_init",
            "glide_prefill", "glide_decode_step", "glide_decode_step_noalloc", "glide_state_flush", "glide_feature_map",
-           "glide_status_string"]
+           "glide_status_string", "glide_paged_workspace_bytes", "glide_paged_prefill", "glide_paged_decode",
+           "glide_paged_evict"]
 
 
 class GlideError(RuntimeError):
@@ -58,6 +59,18 @@ class LayerLayout(ctypes.Structure):
                 ("gring_offset", ctypes.c_int64), ("layer_offset", ctypes.c_int64),
                 ("layer_bytes", ctypes.c_int64), ("window", ctypes.c_int32),
                 ("ring_slots", ctypes.c_int32)]
+
+
+class PagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "page_size",
+                                              "n_pages", "max_pages", "window", "n_sinks")]
+    _fields_ += [("sm_scale", ctypes.c_float)]
+
+
+class PagedCacheArg(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
 
 
 _lib = None
@@ -97,6 +110,17 @@ def load_library(path=None):
     lib.glide_state_flush.restype = ctypes.c_int
     lib.glide_feature_map.argtypes = [cfgp, vp, vp, ctypes.c_int64, vp, vp]
     lib.glide_feature_map.restype = ctypes.c_int
+    pcfg, pcache = ctypes.POINTER(PagedConfig), ctypes.POINTER(PagedCacheArg)
+    lib.glide_paged_workspace_bytes.argtypes = [pcfg, ctypes.c_int64, ctypes.c_int32]
+    lib.glide_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.glide_paged_prefill.argtypes = [pcfg, pcache, vp, vp, vp, ctypes.POINTER(ctypes.c_int32), ctypes.c_int64,
+                                        ctypes.c_int32, ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.glide_paged_prefill.restype = ctypes.c_int
+    lib.glide_paged_decode.argtypes = [pcfg, pcache, vp, vp, vp, ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.glide_paged_decode.restype = ctypes.c_int
+    lib.glide_paged_evict.argtypes = [pcfg, pcache, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp, ctypes.c_size_t,
+                                      vp]
+    lib.glide_paged_evict.restype = ctypes.c_int
     lib.glide_status_string.argtypes = [ctypes.c_int]
     lib.glide_status_string.restype = ctypes.c_char_p
     if path is None:

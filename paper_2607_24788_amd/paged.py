@@ -1,0 +1,193 @@
+"""Thin ctypes binding of the paged softmax cache (``glide_paged_*`` in
+include/glide.h): attention with a sliding window and sinks over a key-value
+cache held in pages, the attention weight that each cached token has received,
+and the eviction of the tokens that received least.
+
+Argument marshalling only, as in ``glide.py``: every step runs in the HIP
+kernels behind the C ABI, and there is no fallback.
+"""
+import ctypes
+
+import torch
+
+from . import glide
+
+FULL = 1 << 30   # a window that never ends: causal softmax attention
+_PTR = ctypes.c_void_p
+
+
+def _tensor(name, t, device, dtype, numel):
+    """Refuse what the library cannot see to be wrong: not a contiguous tensor
+    of the cache's device and the expected type with `numel` elements or more."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} elements, at least {numel} needed")
+    return t.data_ptr()
+
+
+class PagedCache:
+    """The cache of one layer: its tensors, and the struct that names them to
+    the library.  Made by ``Paged.cache``."""
+
+    def __init__(self, k_pool, v_pool, block_table, lens, weights, arg):
+        self.k_pool, self.v_pool, self.weights = k_pool, v_pool, weights
+        self.block_table, self.lens = block_table, lens
+        self.device = k_pool.device
+        self._arg = arg
+        self._ref = ctypes.byref(arg)
+
+
+class Paged:
+    """A configured layer over a paged cache (mirrors ``glide_paged_config``).
+
+    ``window``: tokens that a query sees, its own among them (None: all);
+    ``n_sinks``: first tokens that stay visible whatever the window.  Pools are
+    [n_pages][n_kv_heads][page_size][head_dim]; a transposed view of another
+    order works as long as a row's elements are consecutive and rows start on
+    16 bytes.
+    """
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, window=None, n_sinks=0,
+                 dtype=torch.bfloat16, sm_scale=None, lib=None):
+        self.lib = lib if lib is not None else glide.load_library()
+        if window is None:
+            window = FULL
+        if sm_scale is None:
+            sm_scale = head_dim ** -0.5
+        code = {torch.float32: glide.F32, torch.bfloat16: glide.BF16}.get(dtype, 99)
+        self.cfg = glide.PagedConfig(batch, n_q_heads, n_kv_heads, head_dim, code, page_size, n_pages, max_pages,
+                                     window, n_sinks, float(sm_scale))
+        self._ref = ctypes.byref(self.cfg)
+        self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = batch, n_q_heads, n_kv_heads, head_dim
+        self.page_size, self.n_pages, self.max_pages = page_size, n_pages, max_pages
+        self.window, self.n_sinks, self.sm_scale, self.torch_dtype = window, n_sinks, float(sm_scale), dtype
+        if self.workspace_bytes(0) == 0:
+            raise glide.GlideError(-2, "glide_paged_workspace_bytes", self.lib)
+
+    # -- buffers -------------------------------------------------------------
+    def workspace_bytes(self, max_total_tokens=0, weights=False):
+        return self.lib.glide_paged_workspace_bytes(self._ref, int(max_total_tokens), int(bool(weights)))
+
+    def new_workspace(self, max_total_tokens=0, weights=False, device="cuda"):
+        """Workspace for every call of up to max_total_tokens packed tokens;
+        weights: on a cache that keeps attention weights."""
+        n = self.workspace_bytes(max_total_tokens, weights)
+        if n == 0:
+            raise glide.GlideError(-2, "glide_paged_workspace_bytes", self.lib)
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+    def new_pools(self, weights=False, device="cuda"):
+        """K and V pools, and the weights' pool or None.  Not cleared: what no
+        token was written to is never used."""
+        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        k, v = (torch.empty(shape, dtype=self.torch_dtype, device=device) for _ in range(2))
+        return k, v, (torch.empty(shape[:3], dtype=torch.float32, device=device) if weights else None)
+
+    def cache(self, k_pool, v_pool, block_table, lens, weights=None):
+        """The cache of one layer.  The tensors are used in place: a caller
+        moves lens on and fills block_table between calls."""
+        arg = glide.PagedCacheArg()
+        shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        for name, t, strides in (("k_pool", k_pool, arg.k_strides), ("v_pool", v_pool, arg.v_strides)):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise ValueError(f"{name} must be a device tensor")
+            if t.dtype != self.torch_dtype:
+                raise ValueError(f"{name} has dtype {t.dtype}, expected {self.torch_dtype}")
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+            if t.stride(3) != 1:
+                raise ValueError(f"{name}: the elements of a row must be consecutive")
+            span = self.head_dim   # elements that the dimensions so far take
+            for stride, i in sorted((t.stride(i), i) for i in range(3) if shape[i] > 1):
+                if stride < span:
+                    raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
+                strides[i], span = stride, stride * (shape[i] - 1) + span
+        if v_pool.device != k_pool.device:
+            raise ValueError("k_pool and v_pool are on different devices")
+        dev = k_pool.device
+        arg.k, arg.v = k_pool.data_ptr(), v_pool.data_ptr()
+        arg.block_table = _tensor("block_table", block_table, dev, torch.int32, self.batch * self.max_pages)
+        arg.lens = _tensor("lens", lens, dev, torch.int32, self.batch)
+        if tuple(block_table.shape) != (self.batch, self.max_pages):
+            raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected "
+                             f"{(self.batch, self.max_pages)}")
+        if weights is not None:
+            arg.weights = _tensor("weights", weights, dev, torch.float32,
+                                  self.n_pages * self.n_kv_heads * self.page_size)
+        return PagedCache(k_pool, v_pool, block_table, lens, weights, arg)
+
+    # -- calls ---------------------------------------------------------------
+    def _rows(self, cache, q, k, v, out, lse, T):
+        """Pointers of a call over T rows of queries, checked."""
+        if not isinstance(cache, PagedCache):
+            raise ValueError("cache must come from Paged.cache")
+        dev, dt = cache.device, self.torch_dtype
+        nq, nkv = T * self.n_q_heads * self.head_dim, T * self.n_kv_heads * self.head_dim
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        return (_tensor("q", q, dev, dt, nq), None if k is None else _tensor("k", k, dev, dt, nkv),
+                None if v is None else _tensor("v", v, dev, dt, nkv), _tensor("out", out, dev, dt, nq),
+                None if lse is None else _tensor("lse", lse, dev, torch.float32, T * self.n_q_heads))
+
+    def _workspace(self, cache, workspace):
+        return _tensor("workspace", workspace, cache.device, torch.uint8, 0), workspace.numel()
+
+    def _call(self, name, cache, stream, *args):
+        dev = cache.device
+        if dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):
+                return self._call(name, cache, stream, *args)
+        if stream is None:
+            stream = torch.cuda.current_stream(dev)
+        s = getattr(self.lib, name)(self._ref, cache._ref, *args, stream.cuda_stream)
+        if s:
+            raise glide.GlideError(s, name, self.lib)
+
+    def prefill(self, cache, q, cu_seqlens, out, workspace, k=None, v=None, lse=None, n_observe=0, max_len=0,
+                stream=None):
+        """Append k, v (if given) and read out one row per token and head.
+        q, out [T][Hq][d], k, v [T][Hkv][d], lse [T][Hq] fp32; the weights of
+        the last n_observe queries of every sequence are added up."""
+        cu = [int(x) for x in cu_seqlens]
+        if len(cu) != self.batch + 1:
+            raise ValueError("cu_seqlens needs batch + 1 entries")
+        if n_observe and cache.weights is None:
+            raise ValueError("n_observe needs a cache with weights")
+        qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
+        ws, n = self._workspace(cache, workspace)
+        self._call("glide_paged_prefill", cache, stream, qp, kp, vp, (ctypes.c_int32 * len(cu))(*cu), cu[-1],
+                   int(n_observe), int(max_len), op, lp, ws, n)
+
+    def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
+        """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
+        lse [B][Hq] fp32.  On a cache with weights every query adds its."""
+        qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
+        ws, n = self._workspace(cache, workspace)
+        self._call("glide_paged_decode", cache, stream, qp, kp, vp, int(max_len), op, lp, ws, n)
+
+    def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):
+        """Keep min(len, budget) tokens per sequence and KV head, in place or
+        in dst_table's pages.  kept [B][Hkv][budget] int32: their old
+        positions; new_lens [B] int32 (may be the cache's lens)."""
+        if not isinstance(cache, PagedCache):
+            raise ValueError("cache must come from Paged.cache")
+        if cache.weights is None:
+            raise ValueError("evict needs a cache with weights")
+        dev = cache.device
+        kp = _tensor("kept", kept, dev, torch.int32, self.batch * self.n_kv_heads * max(int(budget), 0))
+        lp = _tensor("new_lens", new_lens, dev, torch.int32, self.batch)
+        dp = None
+        if dst_table is not None:
+            dp = _tensor("dst_table", dst_table, dev, torch.int32, self.batch * self.max_pages)
+            if tuple(dst_table.shape) != (self.batch, self.max_pages):
+                raise ValueError(f"dst_table has shape {tuple(dst_table.shape)}, expected "
+                                 f"{(self.batch, self.max_pages)}")
+        ws, n = self._workspace(cache, workspace)
+        self._call("glide_paged_evict", cache, stream, int(budget), int(n_recent), dp, kp, lp, ws, n)
