@@ -14,7 +14,10 @@ constexpr float kNoMax = -1e30f;
 
 // Rows of one workgroup of attend_rows: one MFMA tile of (token, head) pairs.
 constexpr int kPagedRows = 16;
-// Keys of one tile of a wave, and the granularity of a piece (four waves).
+// Rows of one workgroup of attend_tiles (four waves of 32), keys of its tiles.
+constexpr int kTileRows = 128;
+constexpr int kTileKeys = 64;
+// Keys of one tile of a wave of attend_rows, and the granularity of a piece (four waves).
 constexpr int kPagedTile = 32;
 constexpr int kPagedPieceMin = 512;
 constexpr int kPagedMaxPieces = 64;
@@ -63,7 +66,9 @@ struct EvictArgs {
 
 hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const void* k, const void* v, int d, int dtype,
                                hipStream_t stream);
-hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, hipStream_t stream);
+// tile_rows: kPagedRows (attend_rows) or kTileRows (attend_tiles, bf16 only)
+hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, int tile_rows,
+                               hipStream_t stream);
 hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs* s, int n_observe, int64_t keys, int d, int dtype,
                                 hipStream_t stream);
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream);

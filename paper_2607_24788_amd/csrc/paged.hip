@@ -284,6 +284,298 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Attention of many rows (bf16): a workgroup takes 128 rows ((token, head)
+// pairs of one KV head, 32 per wave) over the 64-key tiles that any of them
+// sees, K and V staged in LDS for the four waves.
+//   S^T = K Q^T with 32x32x16 MFMAs: a lane holds the scores of one row, 16 of
+//   each 32 keys, in the order that the right operand of O^T += V^T P^T takes
+//   (keys 8j + 4h + 0..3 of lane half h), so the weights never leave its
+//   registers; V^T comes from the transposing LDS reads.
+//   Row sums of the weights are taken before they are rounded to bf16: lse is
+//   exact to fp32.  The frame (a row's maximum) moves only when a score passes
+//   it by 2^8: weights up to 2^8 round alike, and fp32 sums hold them.
+// A 16-byte piece c of row r is kept at piece c ^ swz(r) of the row: eight
+// consecutive rows' K pieces, and four rows' 64-byte V segments, lie in
+// different banks.
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16_t mma32(uint4 a, uint4 b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                 0, 0, 0);
+}
+__device__ __forceinline__ uint4 vt_frag(const char* p, const char* q) {
+  const i16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(__attribute__((address_space(3))) char*)p);
+  const i16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(__attribute__((address_space(3))) char*)q);
+  const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+  return make_uint4(x.x, x.y, y.x, y.y);
+}
+// The block table through the scalar cache (nothing writes it during a call).
+__device__ __forceinline__ int32_t table_at(const int32_t* row, int32_t i) {
+  typedef const int32_t __attribute__((address_space(4))) * cptr;
+  return ((cptr)(uintptr_t)row)[i];
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s) {
+  constexpr int KK = D / 16, CT = D / 32, RB = 2 * D, LPR = RB / 16, RPI = 64 / LPR, NI = 16 / RPI;
+  constexpr int KB = kTileKeys * RB;  // bytes of a K (or V) tile
+  __shared__ __align__(16) char lds[2][2 * KB];
+  const int lane = threadIdx.x & 63, h = lane >> 5, q = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
+  const int si = find_seq(s, tile), b = s.seq0 + si, ntok = s.len[si];
+  const int32_t len = __builtin_amdgcn_readfirstlane(seq_len(a, b)), p0 = len - ntok;
+  const int r0 = (tile - s.tile0[si]) * kTileRows, rend = ntok * a.G;
+  const int rlast = r0 + kTileRows < rend ? r0 + kTileRows - 1 : rend - 1;
+  const int32_t t0 = p0 + r0 / a.G > 0 ? p0 + r0 / a.G : 0, t1 = p0 + rlast / a.G;
+  // this wave's rows, and this lane's
+  const int w0 = r0 + 32 * wave;
+  const bool rok = w0 + q < rend;
+  const int r = rok ? w0 + q : rend - 1, tok = r / a.G;
+  const int32_t tr = rok ? p0 + tok : -1;
+  const int64_t orow = (int64_t(s.start[si]) + tok) * a.Hq + g * a.G + (r - tok * a.G);
+  const int32_t tw0 = p0 + (w0 < rend ? w0 : rend - 1) / a.G;
+  const int32_t tw1 = w0 < rend ? p0 + (w0 + 31 < rend ? w0 + 31 : rend - 1) / a.G : -1;
+  // tiles: those of the sinks before the window's, then the window's
+  const int32_t wstart = t0 - a.W + 1 > 0 ? t0 - a.W + 1 : 0;
+  int32_t nt = 0, nsink = 0, wt0 = 0;
+  if (t1 >= 0) {
+    wt0 = wstart / kTileKeys;
+    nsink = (a.ns + kTileKeys - 1) / kTileKeys;
+    nsink = nsink < wt0 ? nsink : wt0;
+    nt = nsink + (t1 / kTileKeys >= wt0 ? t1 / kTileKeys - wt0 + 1 : 0);
+  }
+  int32_t per = (nt + a.npiece - 1) / a.npiece;
+  per = per > a.piece / kTileKeys ? per : a.piece / kTileKeys;
+  const int32_t i0 = int32_t(blockIdx.y) * per, i1 = i0 + per < nt ? i0 + per : nt;
+  auto key0 = [&](int32_t i) { return (i < nsink ? i : wt0 + i - nsink) * kTileKeys; };
+  const int32_t* trow = a.table + int64_t(b) * a.max_pages;
+  const int32_t last_entry = (t1 > 0 ? t1 : 0) >> a.shift;
+
+  uint4 qf[KK];
+  {
+    const char* qp = a.q + orow * RB + 16 * h;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      qf[kk] = *reinterpret_cast<const uint4*>(qp + 32 * kk);
+      if (!rok) qf[kk] = make_uint4(0, 0, 0, 0);
+    }
+    if (a.scale < 0) {  // scores of -q: the frame is a maximum of raw scores
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        qf[kk].x ^= 0x80008000u;
+        qf[kk].y ^= 0x80008000u;
+        qf[kk].z ^= 0x80008000u;
+        qf[kk].w ^= 0x80008000u;
+      }
+    }
+  }
+  const float c = fabsf(a.scale);
+
+  // staging: row 16 wave + RPI i + lane / LPR of a tile, piece lane % LPR
+  const int srow = lane / LPR;
+  uint32_t koff[NI], voff[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int rr = RPI * i + srow, piece = (lane % LPR) ^ swz<D>(rr);
+    koff[i] = uint32_t(rr) * uint32_t(a.ks[2]) + piece * 16;
+    voff[i] = uint32_t(rr) * uint32_t(a.vs[2]) + piece * 16;
+  }
+  struct Stage {
+    uint4 k[NI], v[NI];
+  };
+  // pages of a tile's four groups of 16 keys
+  struct Pages {
+    int32_t p[4];
+  };
+  auto pages_of = [&](int32_t i) {
+    Pages x;
+    const int32_t k0 = key0(i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int32_t at = (k0 + 16 * e) >> a.shift;
+      x.p[e] = table_at(trow, at < last_entry ? at : last_entry);
+    }
+    return x;
+  };
+  auto fetch = [&](int32_t i, const Pages& pg, Stage& st) {
+    const int32_t k0 = key0(i) + 16 * wave;
+    const int32_t page = wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3];
+    const bool ok = uint32_t(page) < uint32_t(a.n_pages);
+    const int64_t slot = k0 & ((1 << a.shift) - 1), pp = ok ? page : 0;
+    const brsrc_t kr = make_rsrc(a.kp + pp * a.ks[0] + g * a.ks[1] + slot * a.ks[2], ok ? kOOB : 0);
+    const brsrc_t vr = make_rsrc(a.vp + pp * a.vs[0] + g * a.vs[1] + slot * a.vs[2], ok ? kOOB : 0);
+    // rows that none of the workgroup's queries sees are read as zeros
+    const int32_t lo = wstart - k0, hi = t1 + 1 - k0, sk = (a.ns < t1 + 1 ? a.ns : t1 + 1) - k0;
+#pragma unroll
+    for (int e = 0; e < NI; ++e) {
+      const int32_t rr = RPI * e + srow;
+      const bool see = (rr >= lo && rr < hi) || rr < sk;
+      st.k[e] = bload16(kr, see ? koff[e] : kOOB);
+      st.v[e] = bload16(vr, see ? voff[e] : kOOB);
+    }
+  };
+  auto put = [&](char* buf, const Stage& st) {
+    char* w = buf + wave * 16 * RB + lane * 16;
+#pragma unroll
+    for (int e = 0; e < NI; ++e) {
+      *reinterpret_cast<uint4*>(w + e * 1024) = st.k[e];
+      *reinterpret_cast<uint4*>(w + KB + e * 1024) = st.v[e];
+    }
+  };
+
+  float mc = kNoMax, l = 0.f;
+  f32x16_t o[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[ct][i] = 0.f;
+
+  // per-lane LDS offsets: K row q of a 32-key half; V row i/4 (+ 4h) of a 16-key slab
+  const int klane = q * RB, ksw = h ^ swz<D>(q);
+  const int l16 = lane & 15, vrow = 4 * h + (l16 >> 2);
+  const int vlane = KB + vrow * RB + (l16 & 1) * 8;
+  const int vsw = (2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ swz<D>(vrow);
+
+  auto compute = [&](const char* buf, int32_t i, uint32_t okp) {
+    const int32_t k0 = key0(i);
+    if (k0 > tw1 || (k0 + kTileKeys <= tw0 - a.W + 1 && k0 >= a.ns)) return;  // nothing for this wave
+    f32x16_t sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[t][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint4 kf = *reinterpret_cast<const uint4*>(buf + klane + 32 * t * RB + (((2 * kk) ^ ksw) << 4));
+        sc[t] = mma32(kf, qf[kk], sc[t]);
+      }
+    }
+    const bool full = okp == 15u && k0 + kTileKeys - 1 <= tw0 && (k0 > tw1 - a.W || k0 + kTileKeys <= a.ns);
+    if (!full) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int32_t j = k0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
+          const bool see = j <= tr && (j > tr - a.W || j < a.ns) && ((okp >> (2 * t + (e >> 3))) & 1);
+          sc[t][e] = see ? sc[t][e] : -INFINITY;
+        }
+    }
+    float mx = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[t][e]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c;
+    if (__any(mx > mc + 8.f)) {
+      const float m2 = fmaxf(mc, mx), f = __builtin_amdgcn_exp2f(mc - m2);
+      mc = m2;
+      l *= f;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[ct][e] *= f;
+    }
+    uint4 pf[4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        sc[t][e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e], c, -mc));
+        l += sc[t][e];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        pf[2 * t + u] = make_uint4(pack_bf16x2(sc[t][8 * u], sc[t][8 * u + 1]), pack_bf16x2(sc[t][8 * u + 2], sc[t][8 * u + 3]),
+                                   pack_bf16x2(sc[t][8 * u + 4], sc[t][8 * u + 5]),
+                                   pack_bf16x2(sc[t][8 * u + 6], sc[t][8 * u + 7]));
+    }
+#pragma unroll
+    for (int sl = 0; sl < 4; ++sl)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const char* p = buf + vlane + 16 * sl * RB + (((4 * ct) ^ vsw) << 4);
+        const char* p2 = buf + vlane + (16 * sl + 8) * RB + (((4 * ct) ^ vsw ^ 2) << 4);
+        o[ct] = mma32(vt_frag(p, p2), pf[sl], o[ct]);
+      }
+  };
+
+  if (i0 < i1) {
+    auto okbits = [&](const Pages& p) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m |= (uint32_t(p.p[e]) < uint32_t(a.n_pages) ? 1u : 0u) << e;
+      return m;
+    };
+    Stage st;
+    Pages pg = pages_of(i0);
+    uint32_t okc = okbits(pg);
+    fetch(i0, pg, st);
+    pg = pages_of(i0 + 1 < i1 ? i0 + 1 : i0);
+    put(lds[0], st);
+    for (int32_t i = i0;; ++i) {
+      char* cur = lds[(i - i0) & 1];
+      __syncthreads();
+      const uint32_t okn = okbits(pg);
+      if (i + 1 < i1) {
+        fetch(i + 1, pg, st);
+        pg = pages_of(i + 2 < i1 ? i + 2 : i + 1);
+      }
+      compute(cur, i, okc);
+      if (i + 1 >= i1) break;
+      put(lds[(i - i0 + 1) & 1], st);
+      okc = okn;
+    }
+  }
+
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (a.npiece > 1) {
+    if (!rok) return;
+    const int64_t rec = orow * a.npiece + blockIdx.y;
+    if (h == 0) {
+      a.ml[rec * 2] = mc;
+      a.ml[rec * 2 + 1] = l;
+    }
+    float* w = a.acc + rec * D + 4 * h;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<float4*>(w + 32 * ct + 8 * e) =
+            make_float4(o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]);
+    return;
+  }
+  if (rok && h == 0) {
+    const float lse2 = l > 0.f ? mc + __builtin_amdgcn_logf(l) : l == 0.f ? -INFINITY : l;
+    if (a.lse) a.lse[orow] = lse2 * kLn2;
+    if (a.lse2) a.lse2[orow] = lse2;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  char* w = a.out + orow * RB + 16 * h;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      // elements 8e + 4h + 0..3 and 8(e+1) + 4h + 0..3 of the lane halves to 8e + 8h + 0..7
+      uint32_t x[2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        x[0][u] = pack_bf16x2(o[ct][4 * e + 2 * u] * inv, o[ct][4 * e + 2 * u + 1] * inv);
+        x[1][u] = pack_bf16x2(o[ct][4 * e + 4 + 2 * u] * inv, o[ct][4 * e + 5 + 2 * u] * inv);
+      }
+      const auto y0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+      const auto y1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+      if (rok) *reinterpret_cast<uint4*>(w + 64 * ct + 16 * e) = make_uint4(y0[0], y1[0], y0[1], y1[1]);
+    }
+}
+
 // The pieces of a row joined: a wave per row, D / 64 elements per lane.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0, int64_t rows) {
@@ -413,7 +705,7 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
 }
 
 template <typename T, int D>
-hipError_t attend_t(const PagedArgs& a, const PagedSeqs* s, hipStream_t stream) {
+hipError_t attend_t(const PagedArgs& a, const PagedSeqs* s, int tile_rows, hipStream_t stream) {
   static const PagedSeqs none = {};
   if (!s) {
     attend_rows<T, D, true><<<dim3(a.B * a.Hkv, a.npiece), 256, 0, stream>>>(a, none);
@@ -425,7 +717,13 @@ hipError_t attend_t(const PagedArgs& a, const PagedSeqs* s, hipStream_t stream) 
   }
   const int64_t tiles = s->tile0[s->nseq];
   if (tiles == 0) return hipSuccess;
-  attend_rows<T, D, false><<<dim3(uint32_t(tiles * a.Hkv), a.npiece), 256, 0, stream>>>(a, *s);
+  const dim3 grid(uint32_t(tiles * a.Hkv), a.npiece);
+  if constexpr (sizeof(T) == 2) {
+    if (tile_rows == kTileRows) attend_tiles<D><<<grid, 256, 0, stream>>>(a, *s);
+    else attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, *s);
+  } else {
+    attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, *s);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.npiece == 1) return e;
   const int64_t row0 = int64_t(s->start[0]) * a.Hq;
@@ -459,9 +757,11 @@ hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const voi
   return hipSuccess;
 }
 
-hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, hipStream_t stream) {
-  if (dtype == GLIDE_BF16) return d == 128 ? attend_t<bf16_t, 128>(a, s, stream) : attend_t<bf16_t, 64>(a, s, stream);
-  return d == 128 ? attend_t<float, 128>(a, s, stream) : attend_t<float, 64>(a, s, stream);
+hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, int tile_rows,
+                               hipStream_t stream) {
+  if (dtype == GLIDE_BF16)
+    return d == 128 ? attend_t<bf16_t, 128>(a, s, tile_rows, stream) : attend_t<bf16_t, 64>(a, s, tile_rows, stream);
+  return d == 128 ? attend_t<float, 128>(a, s, tile_rows, stream) : attend_t<float, 64>(a, s, tile_rows, stream);
 }
 
 hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs* s, int n_observe, int64_t keys, int d, int dtype,

@@ -98,12 +98,23 @@ Sections sections(const glide_paged_config* c, int64_t rows, int64_t record_rows
   return s;
 }
 
-// Row tiles of a prefill: of each sequence's rows, by 16.
-int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1) {
+// Row tiles of a prefill: of each sequence's rows.
+int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1, int rows) {
   int64_t n = 0;
   const int G = c->n_q_heads / c->n_kv_heads;
-  for (int b = b0; b < b1; ++b) n += (int64_t(cu[b + 1] - cu[b]) * G + kPagedRows - 1) / kPagedRows;
+  for (int b = b0; b < b1; ++b) n += (int64_t(cu[b + 1] - cu[b]) * G + rows - 1) / rows;
   return n;
+}
+
+// Rows per tile of a prefill of `tokens` tokens: the tiles kernel (bf16) where
+// its tiles are half full on average or more.  It takes a wave's 16 rows of a
+// page at 32-bit offsets: pages of 16 tokens or more.
+int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu) {
+  if (c->dtype != GLIDE_BF16 || c->page_size < 16) return kPagedRows;
+  const int64_t far = int64_t(1) << 26;
+  if (k->k_strides[2] > far || k->v_strides[2] > far) return kPagedRows;
+  const int64_t rows = int64_t(cu[c->batch]) * (c->n_q_heads / c->n_kv_heads);
+  return rows * 2 >= row_tiles(c, cu, 0, c->batch, kTileRows) * kTileRows ? kTileRows : kPagedRows;
 }
 
 void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a) {
@@ -127,7 +138,9 @@ void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a)
   a->cap = capacity(c);
   a->W = c->window;
   a->ns = c->n_sinks;
+  // (a scale of 0 stays a number that no -inf becomes NaN by)
   a->scale = c->sm_scale * kLog2e;
+  if (fabsf(a->scale) < 1e-30f) a->scale = 1e-30f;
 }
 
 glide_status hip_status(hipError_t e) { return e == hipSuccess ? GLIDE_OK : GLIDE_ERR_HIP; }
@@ -141,9 +154,9 @@ size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_to
   if (max_total_tokens > (int64_t(1) << 31)) return 0;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads, units = int64_t(cfg->batch) * cfg->n_kv_heads;
   int64_t n = sections(cfg, rows, record_floats(cfg, rows, units) / (cfg->head_dim + 2), weights, true).bytes;
-  // prefill: kPagedWgs tiles of 16 rows at most are split, into 2 * kPagedWgs records of tiles at most
+  // prefill: kPagedWgs tiles at most are split, into 2 * kPagedWgs records of tiles at most
   const int64_t prows = max_total_tokens * cfg->n_q_heads;
-  n = std::max(n, sections(cfg, prows, std::min(prows * kPagedMaxPieces, int64_t(2) * kPagedWgs * kPagedRows), weights,
+  n = std::max(n, sections(cfg, prows, std::min(prows * kPagedMaxPieces, int64_t(2) * kPagedWgs * kTileRows), weights,
                            false).bytes);
   return size_t(std::max<int64_t>(256, n));
 }
@@ -180,6 +193,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
   a.out = static_cast<char*>(out);
   a.lse = lse;
   hipStream_t st = hipStream_t(stream);
+  const int per_tile = tile_rows(cfg, cache, cu);
   for (int b0 = 0; b0 < cfg->batch;) {
     PagedSeqs t;
     memset(&t, 0, sizeof(t));
@@ -190,7 +204,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
       const int i = b1 - b0;
       t.start[i] = cu[b1];
       t.len[i] = cu[b1 + 1] - cu[b1];
-      t.tile0[i + 1] = t.tile0[i] + int32_t(row_tiles(cfg, cu, b1, b1 + 1));
+      t.tile0[i + 1] = t.tile0[i] + int32_t(row_tiles(cfg, cu, b1, b1 + 1, per_tile));
       ++b1;
     }
     t.nseq = b1 - b0;
@@ -206,7 +220,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
     if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
     s = hip_status(launch_paged_append(a, t, k, v, cfg->head_dim, cfg->dtype, st));
     if (s != GLIDE_OK) return s;
-    s = hip_status(launch_paged_attend(a, &t, cfg->head_dim, cfg->dtype, st));
+    s = hip_status(launch_paged_attend(a, &t, cfg->head_dim, cfg->dtype, per_tile, st));
     if (s != GLIDE_OK) return s;
     if (n_observe > 0) {
       int32_t longest = 0;
@@ -256,7 +270,7 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
     a.nv = (most_seen(cfg, 0) + 31) / 32 * 32;
   }
   hipStream_t st = hipStream_t(stream);
-  s = hip_status(launch_paged_attend(a, nullptr, cfg->head_dim, cfg->dtype, st));
+  s = hip_status(launch_paged_attend(a, nullptr, cfg->head_dim, cfg->dtype, kPagedRows, st));
   if (s != GLIDE_OK || !weights) return s;
   return hip_status(launch_paged_weights(a, nullptr, 0, most_seen(cfg, max_len), cfg->head_dim, cfg->dtype, st));
 }

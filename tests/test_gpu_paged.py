@@ -149,6 +149,9 @@ PREFILL = [
     (2, 5, 1, 64, 256, [300, 2], [299, 2], 0, 3, 5),          # sinks alone
     (1, 7, 7, 128, 64, [450], [450], 1, 0, 450),              # itself alone
     (2, 8, 2, 64, 1024, [1100, 900], [3, 5], None, 0, 4),     # few rows over a long cache: pieces joined
+    (2, 8, 2, 128, 32, [2100, 1700], [40, 33], None, 0, 7),   # more rows, pieces joined
+    (2, 8, 2, 64, 16, [1100, 1300], [70, 64], 700, 300, 64),  # the window's and the sinks' tiles overlap, or not
+    (1, 4, 1, 128, 8, [260], [200], 90, 0, 3),                # pages smaller than a wave's rows
 ]
 
 
