@@ -17,37 +17,56 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t key_at(const EvictArgs& a, const int32_t* trow, int g, int32_t j) {
-  const Slot s = paged_slot(trow, j, a.shift, a.n_pages);
-  return s.ok ? weight_key(a.wp[((int64_t(s.page) * a.Hkv + g) << a.shift) + s.slot]) : 0u;
+__device__ __forceinline__ int64_t weight_at(const EvictArgs& a, int32_t page, int g, int32_t j) {
+  return ((int64_t(page) * a.Hkv + g) << a.shift) + (j & ((1 << a.shift) - 1));
 }
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSelKeys = 32;  // keys of a thread: 32K tokens in registers
+constexpr int kBins = 2048, kCopies = 8;
 
-// Exclusive sum over the workgroup of a flag, and its total.
-__device__ __forceinline__ int block_rank(bool flag, int* wsum, int* total) {
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t y = __shfl_up(x, d);
+    if (int(threadIdx.x & 63) >= d) x += y;
+  }
+  return x;
+}
+// Exclusive sum over the workgroup's threads; wsum: one entry per wave.
+// Begins and ends with a barrier's worth of order on wsum.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t m = __ballot(flag);
+  const uint32_t inc = wave_scan(x);
   __syncthreads();
-  if (lane == 0) wsum[wave] = __popcll(m);
+  if (lane == 63) wsum[wave] = inc;
   __syncthreads();
-  int before = 0, all = 0;
-  for (int w = 0; w < kSelThreads / 64; ++w) {
-    if (w < wave) before += wsum[w];
-    all += wsum[w];
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    const uint32_t y = wsum[w];
+    before += w < wave ? y : 0;
+    all += y;
   }
   *total = all;
-  return before + __popcll(m & ((uint64_t(1) << lane) - 1));
+  return before + inc - x;
 }
 
-// Which tokens stay, one workgroup per (sequence, KV head): the need-th
-// largest key by four passes over its bytes (histograms in LDS, integer
-// counts: no order of atomics shows), then the kept positions in order.
+// Which tokens stay, one workgroup per (sequence, KV head).  The need-th
+// largest key is found by its 11, 11 and 10 bits: a histogram in LDS of the
+// keys that agree so far (integer counts, so no order of atomics shows; eight
+// copies, as weights of like size share their first bits), then the bin by a
+// sum from the top.  Then every key above it stays, and the first of those
+// equal to it; ranks come from the waves' ballots in the order of positions.
+// Keys are read once and kept in registers up to 32K tokens, read again per
+// pass above.  Bound by the latency of a dozen barriers and one read.
 __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t pick[2];
-  __shared__ int wsum[kSelThreads / 64];
-  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x;
+  __shared__ uint32_t hist[kBins * kCopies];
+  __shared__ uint32_t cnt[kSelKeys * kSelWaves];  // a row of 64 positions each
+  __shared__ uint32_t wsum[kSelWaves], pick[2];
+  static_assert(kSelKeys * kSelWaves <= kSelThreads, "a thread per count");
+  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t len = seq_len(a, b);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   int32_t* kept = a.kept + int64_t(blockIdx.x) * a.budget;
@@ -57,56 +76,183 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
     for (int32_t j = tid; j < m; j += kSelThreads) kept[j] = j;
     return;
   }
+  // tokens [0, lo) and [hi, len) stay; those between go by their weights
   const int32_t lo = a.ns < len ? a.ns : len;
   const int32_t hi = len - a.recent > lo ? len - a.recent : lo;
-  uint32_t need = uint32_t(m - lo - (len - hi)), thr = 0xffffffffu;
-  if (need > 0) {
-    thr = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-      for (int32_t j = lo + tid; j < hi; j += kSelThreads) {
-        const uint32_t k = key_at(a, trow, g, j);
-        if ((k & mask) == thr) atomicAdd(&hist[(k >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t left = need;
-        int bin = 255;
-        while (hist[bin] < left) left -= hist[bin--];
-        pick[0] = bin;
-        pick[1] = left;
-      }
-      __syncthreads();
-      thr |= pick[0] << shift;
-      need = pick[1];
+  const uint32_t quota = uint32_t(m - lo - (len - hi));
+  for (int32_t j = tid; j < lo; j += kSelThreads) kept[j] = j;
+  for (int32_t j = tid; j < len - hi; j += kSelThreads) kept[lo + quota + j] = hi + j;
+  if (quota == 0) return;
+
+  constexpr int32_t kSeg = kSelThreads * kSelKeys;
+  uint32_t key[kSelKeys];
+  auto load = [&](int32_t j0) {  // keys of positions j0 + 1024 i + tid
+#pragma unroll
+    for (int i = 0; i < kSelKeys; ++i) {
+      const int32_t j = j0 + i * kSelThreads + tid;
+      key[i] = 0xffffffffu;
+      if (j0 + i * kSelThreads < hi) key[i] = uint32_t(trow[(j < hi ? j : lo) >> a.shift]);
     }
+#pragma unroll
+    for (int i0 = 0; i0 < kSelKeys; i0 += 8) {
+      if (j0 + i0 * kSelThreads < hi) {
+        float w[8];
+#pragma unroll
+        for (int i = i0; i < i0 + 8; ++i) {
+          const int32_t j = j0 + i * kSelThreads + tid;
+          const bool ok = j < hi && key[i] < uint32_t(a.n_pages);
+          w[i - i0] = a.wp[ok ? weight_at(a, int32_t(key[i]), g, j) : 0];
+          if (!ok) w[i - i0] = NAN;
+        }
+#pragma unroll
+        for (int i = i0; i < i0 + 8; ++i) key[i] = weight_key(w[i - i0]);
+      }
+    }
+  };
+  const bool once = hi - lo <= kSeg;
+  if (once) load(lo);
+
+  uint32_t need = quota, thr = 0;
+  int shift = 32;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int bits = pass < 2 ? 11 : 10, below = shift;  // bits [below, 32) of thr are known
+    shift -= bits;
+    for (int i = tid; i < kBins * kCopies; i += kSelThreads) hist[i] = 0;
+    __syncthreads();
+    for (int32_t j0 = lo; j0 < hi; j0 += kSeg) {
+      if (!once) load(j0);
+#pragma unroll
+      for (int i = 0; i < kSelKeys; ++i) {
+        if (j0 + i * kSelThreads >= hi) continue;
+        const uint32_t k = key[i];
+        if (j0 + i * kSelThreads + tid < hi && (pass == 0 || (k >> below) == (thr >> below)))
+          atomicAdd(&hist[((k >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+      }
+    }
+    __syncthreads();
+    // two bins per thread, from the top: thread t has bins 2047 - 2t, 2046 - 2t
+    uint32_t c[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint4* h = reinterpret_cast<const uint4*>(hist + (kBins - 1 - 2 * tid - u) * kCopies);
+      const uint4 x = h[0], y = h[1];
+      c[u] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+    }
+    uint32_t total;
+    const uint32_t above = block_scan(c[0] + c[1], wsum, &total);
+    if (above < need && above + c[0] + c[1] >= need) {
+      const bool second = above + c[0] < need;
+      pick[0] = kBins - 1 - 2 * tid - (second ? 1 : 0);
+      pick[1] = need - above - (second ? c[0] : 0);
+    }
+    __syncthreads();
+    thr |= pick[0] << shift;
+    need = pick[1];
   }
-  // in order: every key above thr, and the first `need` of those equal to it
-  int32_t at = 0, equal = 0;
-  for (int32_t j0 = 0; j0 < len; j0 += kSelThreads) {
-    const int32_t j = j0 + tid;
-    bool keep = j < len && (j < lo || j >= hi);
-    const uint32_t k = j >= lo && j < hi ? key_at(a, trow, g, j) : 0u;
-    const bool eq = j >= lo && j < hi && k == thr;
-    int total;
-    const int before = block_rank(eq, wsum, &total);
-    keep = keep || (j >= lo && j < hi && (k > thr || (eq && uint32_t(equal + before) < need)));
-    equal += total;
-    const int rank = block_rank(keep, wsum, &total);
-    if (keep) kept[at + rank] = j;
-    at += total;
+
+  int32_t at = lo;         // kept so far
+  uint32_t equal = 0;      // of them equal to thr
+  for (int32_t j0 = lo; j0 < hi; j0 += kSeg) {
+    if (!once) load(j0);
+    // keys equal to thr before each row of 64 positions
+    if (tid < kSelKeys * kSelWaves) cnt[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelKeys; ++i) {
+      if (j0 + i * kSelThreads >= hi) continue;
+      const uint64_t e = __ballot(j0 + i * kSelThreads + tid < hi && key[i] == thr);
+      if (lane == 0) cnt[i * kSelWaves + wave] = __popcll(e);
+    }
+    uint32_t all, kall;
+    __syncthreads();
+    const uint32_t eq0 = block_scan(tid < kSelKeys * kSelWaves ? cnt[tid] : 0, wsum, &all);
+    if (tid < kSelKeys * kSelWaves) cnt[tid] = eq0;
+    __syncthreads();
+    // which stay (a bit per key), and their counts
+    uint32_t stay = 0;
+    const uint64_t lt = (uint64_t(1) << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kSelKeys; ++i) {
+      if (j0 + i * kSelThreads >= hi) continue;
+      const bool in = j0 + i * kSelThreads + tid < hi, eq = in && key[i] == thr;
+      const uint64_t e = __ballot(eq);
+      const uint32_t rank = equal + cnt[i * kSelWaves + wave] + __popcll(e & lt);
+      if (in && (key[i] > thr || (eq && rank < need))) stay |= 1u << i;
+    }
+    __syncthreads();
+    if (tid < kSelKeys * kSelWaves) cnt[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelKeys; ++i) {
+      if (j0 + i * kSelThreads >= hi) continue;
+      const uint64_t e = __ballot((stay >> i) & 1);
+      if (lane == 0) cnt[i * kSelWaves + wave] = __popcll(e);
+    }
+    __syncthreads();
+    const uint32_t k0 = block_scan(tid < kSelKeys * kSelWaves ? cnt[tid] : 0, wsum, &kall);
+    if (tid < kSelKeys * kSelWaves) cnt[tid] = k0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelKeys; ++i) {
+      if (j0 + i * kSelThreads >= hi) continue;
+      const bool on = (stay >> i) & 1;
+      const uint64_t e = __ballot(on);
+      if (on) kept[at + cnt[i * kSelWaves + wave] + __popcll(e & lt)] = j0 + i * kSelThreads + tid;
+    }
+    at += kall;
+    equal += all;
+    __syncthreads();
   }
 }
 
-// Kept rows to their places.  Tokens move towards the front and stay in
-// order, so a tile's rows, read before any of them is written, are never
-// behind a row written before: in place needs one barrier per tile.
-__global__ __launch_bounds__(1024) void evict_move(EvictArgs a) {
-  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, what = blockIdx.y;
+__device__ __forceinline__ Slot slot_of(const EvictArgs& a, const int32_t* row, int32_t j) {
+  return paged_slot(row, j, a.shift, a.n_pages);
+}
+
+// Kept rows to fresh pages: 32 tokens of a (sequence, KV head) per workgroup,
+// every 16-byte piece of K and V on a thread of its own.  Bound by memory.
+constexpr int kMoveRows = 32;
+__global__ __launch_bounds__(256) void evict_copy(EvictArgs a) {
+  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   const int32_t* drow = a.dst + int64_t(b) * a.max_pages;
+  const int32_t* kept = a.kept + int64_t(blockIdx.x) * a.budget;
+  if (g == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    const int32_t len = seq_len(a, b);
+    a.new_lens[b] = len < a.budget ? len : a.budget;
+  }
+  const int per = a.d * a.esize / 16, c = (threadIdx.x % per) * 16;  // 8, 16 or 32 pieces of a row
+  for (int32_t j0 = blockIdx.y * kMoveRows; j0 < a.budget; j0 += gridDim.y * kMoveRows) {
+    const int32_t jend = j0 + kMoveRows < a.budget ? j0 + kMoveRows : a.budget;
+    for (int32_t j = j0 + threadIdx.x / per; j < jend; j += 256 / per) {
+      const int32_t src = kept[j];
+      if (src < 0) continue;
+      const Slot s = slot_of(a, trow, src), t = slot_of(a, drow, j);
+      uint4 k = make_uint4(0, 0, 0, 0), v = k;
+      float w = 0.f;
+      if (s.ok) {
+        k = *reinterpret_cast<const uint4*>(a.kp + slot_offset(a.ks, s, g) + c);
+        v = *reinterpret_cast<const uint4*>(a.vp + slot_offset(a.vs, s, g) + c);
+        if (c == 0) w = a.wp[weight_at(a, s.page, g, src)];
+      }
+      if (t.ok) {
+        *reinterpret_cast<uint4*>(a.kp + slot_offset(a.ks, t, g) + c) = k;
+        *reinterpret_cast<uint4*>(a.vp + slot_offset(a.vs, t, g) + c) = v;
+        if (c == 0) a.wp[weight_at(a, t.page, g, j)] = w;
+      }
+    }
+  }
+}
+
+// Kept rows to their places in the same pages.  Tokens move towards the front
+// and stay in order, so a row read in a step (all of its rows before any is
+// written) is never behind a row written in a step before: one barrier per
+// step of up to 1024 rows.  A workgroup moves 128 bytes of every K, or V, row
+// of a (sequence, KV head), or its weights.
+__global__ __launch_bounds__(1024) void evict_move(EvictArgs a) {
+  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
+  const int slabs = a.d * a.esize / 128, what = blockIdx.y / slabs;
+  const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   const int32_t* kept = a.kept + int64_t(blockIdx.x) * a.budget;
   if (what == 2) {
     if (g == 0 && threadIdx.x == 0) {
@@ -116,33 +262,45 @@ __global__ __launch_bounds__(1024) void evict_move(EvictArgs a) {
     for (int32_t j0 = 0; j0 < a.budget; j0 += 1024) {
       const int32_t j = j0 + threadIdx.x, src = j < a.budget ? kept[j] : -1;
       float w = 0.f;
-      if (src >= 0) {
-        const Slot s = paged_slot(trow, src, a.shift, a.n_pages);
-        if (s.ok) w = a.wp[((int64_t(s.page) * a.Hkv + g) << a.shift) + s.slot];
+      if (src > j) {
+        const Slot s = slot_of(a, trow, src);
+        if (s.ok) w = a.wp[weight_at(a, s.page, g, src)];
       }
       __syncthreads();
-      if (src >= 0) {
-        const Slot s = paged_slot(drow, j, a.shift, a.n_pages);
-        if (s.ok) a.wp[((int64_t(s.page) * a.Hkv + g) << a.shift) + s.slot] = w;
+      if (src > j) {
+        const Slot t = slot_of(a, trow, j);
+        if (t.ok) a.wp[weight_at(a, t.page, g, j)] = w;
       }
     }
     return;
   }
   char* pool = what ? a.vp : a.kp;
   const int64_t* st = what ? a.vs : a.ks;
-  const int per = a.d * a.esize / 16, rows = 1024 / per;  // 16-byte pieces of a row, rows at a time
-  const int c = (threadIdx.x % per) * 16;
-  for (int32_t j0 = 0; j0 < a.budget; j0 += rows) {
-    const int32_t j = j0 + threadIdx.x / per, src = j < a.budget ? kept[j] : -1;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (src >= 0) {
-      const Slot s = paged_slot(trow, src, a.shift, a.n_pages);
-      if (s.ok) x = *reinterpret_cast<const uint4*>(pool + slot_offset(st, s, g) + c);
+  const int c = int(blockIdx.y % slabs) * 128 + (threadIdx.x & 7) * 16;
+  constexpr int N = 8;  // rows of a thread per step
+  for (int32_t j0 = 0; j0 < a.budget; j0 += 128 * N) {
+    if (kept[j0] < 0) break;  // (kept is -1 from its last entry on)
+    int32_t src[N];
+    uint4 x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int32_t j = j0 + 128 * i + (threadIdx.x >> 3);
+      src[i] = j < a.budget ? kept[j] : -1;
+      if (src[i] <= j) src[i] = -1;  // in its place already
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (src[i] < 0) continue;
+      const Slot s = slot_of(a, trow, src[i]);
+      if (s.ok) x[i] = *reinterpret_cast<const uint4*>(pool + slot_offset(st, s, g) + c);
     }
     __syncthreads();
-    if (src >= 0) {
-      const Slot s = paged_slot(drow, j, a.shift, a.n_pages);
-      if (s.ok) *reinterpret_cast<uint4*>(pool + slot_offset(st, s, g) + c) = x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (src[i] < 0) continue;
+      const Slot t = slot_of(a, trow, j0 + 128 * i + (threadIdx.x >> 3));
+      if (t.ok) *reinterpret_cast<uint4*>(pool + slot_offset(st, t, g) + c) = x[i];
     }
   }
 }
@@ -154,7 +312,12 @@ hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream) {
   evict_select<<<units, kSelThreads, 0, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  evict_move<<<dim3(units, 3), 1024, 0, stream>>>(a);
+  if (a.in_place) {
+    evict_move<<<dim3(units, 2 * uint32_t(a.d * a.esize / 128) + 1), 1024, 0, stream>>>(a);
+  } else {
+    const int64_t n = (int64_t(a.budget) + kMoveRows - 1) / kMoveRows;
+    evict_copy<<<dim3(units, uint32_t(n < 65535 ? n : 65535)), 256, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

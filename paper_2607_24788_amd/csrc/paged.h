@@ -17,12 +17,22 @@ constexpr int kPagedRows = 16;
 // Rows of one workgroup of attend_tiles (four waves of 32), keys of its tiles.
 constexpr int kTileRows = 128;
 constexpr int kTileKeys = 64;
-// Keys of one tile of a wave of attend_rows, and the granularity of a piece (four waves).
+// Keys of one tile of a wave of attend_rows.
 constexpr int kPagedTile = 32;
-constexpr int kPagedPieceMin = 512;
-constexpr int kPagedMaxPieces = 64;
-// Workgroups that a launch is split up to.
-constexpr int kPagedWgs = 1024;
+// Pieces: long rows are split over workgroups and joined.  A round of
+// workgroups is two per CU.
+//  decode: pieces as short as one round allows (at least kPieceMin keys, a tile
+//    per wave); where one round would make them longer than kPieceLong there
+//    are several rounds, which even out ragged lengths.
+//  prefill: only where the row tiles do not fill a round, into pieces of at
+//    least kPiecePrefill keys (records of 16 or 128 rows each).
+// The records of a call are at most kMaxRecords rows.
+constexpr int kPagedRound = 512;
+constexpr int kPieceMin = 128;
+constexpr int kPieceLong = 1024;
+constexpr int kPiecePrefill = 512;
+constexpr int kPagedMaxPieces = 256;
+constexpr int64_t kMaxRecords = 131072;
 
 struct PagedArgs {
   const char *q, *kn, *vn;  // queries; new rows of a decode call (NULL: in the cache)

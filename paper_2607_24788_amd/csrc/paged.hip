@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void paged_clear_weights(PagedArgs a, PagedSeq
 //   already the right operand of O^T += V^T P^T with keys in the order
 //   4g + 0..3, 16 + 4g + 0..3; V goes through LDS for its columns.
 template <typename T, int D, bool DECODE>
-__global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(PagedArgs a, PagedSeqs s) {
   constexpr int KK = D / 32, CT = D / 16, RS = D + 16 / int(sizeof(T)), ES = int(sizeof(T));
   __shared__ __align__(16) T vlds[4][kPagedTile * RS];
   __shared__ float sm[4][16], sl_[4][16];
@@ -107,7 +107,9 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
   if (t1 >= 0) sn = seen_by(t0, t1, a.W, a.ns);
   int32_t pl = (sn.n + a.npiece - 1) / a.npiece;
   pl = pl > a.piece ? (pl + 127) & ~127 : a.piece;
-  const int32_t v0 = int32_t(blockIdx.y) * pl, v1 = v0 + pl < sn.n ? v0 + pl : sn.n;
+  // (v0 in 64 bits: blockIdx.y * pl may pass 2^31 where pieces are longer than they need be)
+  const int32_t v0 = int32_t(int64_t(blockIdx.y) * pl < sn.n ? int64_t(blockIdx.y) * pl : sn.n);
+  const int32_t v1 = sn.n - v0 > pl ? v0 + pl : sn.n;
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   const char* zr = reinterpret_cast<const char*>(zero_row);
 
@@ -135,38 +137,62 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
     }
   }
 
-  for (int32_t x = v0 + wave * kPagedTile; x < v1; x += 4 * kPagedTile) {
-    Frag<T> kf[2][KK], vf[2][KK];
-    uint32_t ok[2];
+  // Tiles are read one ahead: a tile's rows are asked for as soon as the one
+  // before it is out of the registers (K in its scores, V in LDS), its page
+  // numbers a tile earlier.
+  struct At {
+    int32_t j[2], page[2];  // position (-1: behind the piece) and page of rows 16t + n
+  };
+  auto look = [&](int32_t x) {
+    At p;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int32_t vi = x + 16 * t + n;
-      bool good = vi < v1;
-      const int32_t j = good ? sn.pos(vi) : 0;
-      Slot sl = {0, 0, false};
-      if (good) sl = paged_slot(trow, j, a.shift, a.n_pages);
-      good = good && sl.ok;
+      p.j[t] = vi < v1 ? sn.pos(vi) : -1;
+      p.page[t] = trow[(vi < v1 ? p.j[t] : 0) >> a.shift];
+    }
+    return p;
+  };
+  Frag<T> kf[2][KK], vf[2][KK];
+  uint32_t ok[2];
+  auto fetch = [&](const At& p) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const Slot sl = {p.page[t], p.j[t] & ((1 << a.shift) - 1), true};
+      const bool good = p.j[t] >= 0 && uint32_t(p.page[t]) < uint32_t(a.n_pages);
       const char* kr = good ? a.kp + slot_offset(a.ks, sl, g) : zr;
       const char* vr = good ? a.vp + slot_offset(a.vs, sl, g) : zr;
       if constexpr (DECODE) {
-        if (a.kn && good && j == len - 1) {
+        if (a.kn && good && p.j[t] == len - 1) {
           kr = a.kn + (int64_t(b) * a.Hkv + g) * D * ES;
           vr = a.vn + (int64_t(b) * a.Hkv + g) * D * ES;
         }
       }
       ok[t] = uint32_t(__ballot(good)) & 0xffffu;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        kf[t][kk].load(reinterpret_cast<const T*>(kr) + 32 * kk + 8 * lg);
-        vf[t][kk].load(reinterpret_cast<const T*>(vr) + 32 * kk + 8 * lg);
-      }
+      for (int kk = 0; kk < KK; ++kk) kf[t][kk].load(reinterpret_cast<const T*>(kr) + 32 * kk + 8 * lg);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) vf[t][kk].load(reinterpret_cast<const T*>(vr) + 32 * kk + 8 * lg);
     }
+  };
+  constexpr int STEP = 4 * kPagedTile;
+  int32_t x = v0 + wave * kPagedTile;
+  At next = {};
+  if (x < v1) {
+    const At first = look(x);
+    next = look(x + STEP);
+    fetch(first);
+  }
+  for (; x < v1; x += STEP) {
     f32x4_t sc[2] = {zero4(), zero4()};
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
+      for (int kk = 0; kk < KK; ++kk) sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
         T* w = vt + (16 * t + n) * RS + 32 * kk + 8 * lg;
         if constexpr (sizeof(T) == 2) {
           *reinterpret_cast<uint4*>(w) = vf[t][kk].v;
@@ -175,6 +201,12 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
           reinterpret_cast<float4*>(w)[1] = make_float4(vf[t][kk].v[4], vf[t][kk].v[5], vf[t][kk].v[6], vf[t][kk].v[7]);
         }
       }
+    const uint32_t okc[2] = {ok[0], ok[1]};
+    if (x + STEP < v1) {
+      const At now = next;
+      next = look(x + 2 * STEP);
+      fetch(now);
+    }
     float p[8];
     float mx = m;
 #pragma unroll
@@ -182,7 +214,7 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = 4 * lg + i;
-        bool see = (ok[t] >> key) & 1;
+        bool see = (okc[t] >> key) & 1;
         if constexpr (!DECODE) {
           const int32_t j = sn.pos(x + 16 * t + key);
           see = see && j <= tr && (j > tr - a.W || j < a.ns);
@@ -208,7 +240,7 @@ __global__ __launch_bounds__(256) void attend_rows(PagedArgs a, PagedSeqs s) {
       l += p[i];
     }
     Frag<T> pf;
-    pf.set8(p);  // bf16: weights rounded to half a step, 2^-9 of each
+    pf.set8(p);  // bf16: weights rounded to half a step, 2^-8 of each at most
     wave_lds_order();
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -351,7 +383,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   }
   int32_t per = (nt + a.npiece - 1) / a.npiece;
   per = per > a.piece / kTileKeys ? per : a.piece / kTileKeys;
-  const int32_t i0 = int32_t(blockIdx.y) * per, i1 = i0 + per < nt ? i0 + per : nt;
+  const int32_t i0 = int32_t(int64_t(blockIdx.y) * per < nt ? int64_t(blockIdx.y) * per : nt);
+  const int32_t i1 = nt - i0 > per ? i0 + per : nt;
   auto key0 = [&](int32_t i) { return (i < nsink ? i : wt0 + i - nsink) * kTileKeys; };
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   const int32_t last_entry = (t1 > 0 ? t1 : 0) >> a.shift;
@@ -576,33 +609,82 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
 }
 
-// The pieces of a row joined: a wave per row, D / 64 elements per lane.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0, int64_t rows) {
+// The pieces of rows joined, a wave per row: its lanes take the pieces'
+// frames and sums (npiece <= 256, four each), then the elements.  Latency: the
+// records of eight pieces are asked for at once.
+struct Joined {
+  float M, L;
+};
+__device__ __forceinline__ float wave_max(float x) {
+  x = dpp_max_row16(x);
+  return lg_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) { return lg_sum(dpp_sum_rows<16>(x)); }
+
+// f[u]: what piece lane + 64 u counts in the row's frame.
+__device__ __forceinline__ Joined join_frames(const PagedArgs& a, int64_t r, float* f) {
   const int lane = threadIdx.x & 63;
-  const int64_t r = row0 + int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r >= row0 + rows) return;
-  const float* ml = a.ml + r * a.npiece * 2;
-  float M = kNoMax;
-  for (int i = 0; i < a.npiece; ++i) M = fmaxf(M, ml[2 * i]);
-  float L = 0.f, x[D / 64] = {};
-  for (int i = 0; i < a.npiece; ++i) {
-    const float li = ml[2 * i + 1];
-    if (li == 0.f) continue;  // no key of this piece has a part in the row
-    const float f = __builtin_amdgcn_exp2f(ml[2 * i] - M);
-    L += li * f;
+  const float2* ml = reinterpret_cast<const float2*>(a.ml) + r * a.npiece;
+  float2 x[kPagedMaxPieces / 64];
+  Joined j = {kNoMax, 0.f};
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) x[e] += f * a.acc[(r * a.npiece + i) * D + lane * (D / 64) + e];
+  for (int u = 0; u < kPagedMaxPieces / 64; ++u) {
+    x[u] = make_float2(kNoMax, 0.f);
+    if (lane + 64 * u < a.npiece) x[u] = ml[lane + 64 * u];
+    j.M = fmaxf(j.M, x[u].x);
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
+  j.M = wave_max(j.M);
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e)
-    reinterpret_cast<T*>(a.out)[r * D + lane * (D / 64) + e] = from_f32<T>(x[e] * inv);
+  for (int u = 0; u < kPagedMaxPieces / 64; ++u) {
+    // (a piece without a part in the row has no acc either)
+    f[u] = x[u].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[u].x - j.M);
+    j.L += x[u].y * f[u];
+  }
+  j.L = wave_sum(j.L);
+  return j;
+}
+__device__ __forceinline__ float log2_sum(const Joined& j) {
+  return j.L > 0.f ? j.M + __builtin_amdgcn_logf(j.L) : j.L == 0.f ? -INFINITY : j.L;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Joined& j, const float* f) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const float* acc = a.acc + r * a.npiece * D + lane * E;
+  float x[E] = {};
+  for (int i0 = 0; i0 < a.npiece; i0 += 8) {
+    const float fu = i0 < 64 ? f[0] : i0 < 128 ? f[1] : i0 < 192 ? f[2] : f[3];
+    float y[8][E], w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), (i0 + i) & 63));
+      const bool on = i0 + i < a.npiece && w[i] != 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[i][e] = on ? acc[int64_t(i0 + i) * D + e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] += (i0 + i < a.npiece ? w[i] : 0.f) * y[i][e];
+  }
+  const float inv = j.L == 0.f ? 0.f : 1.f / j.L;
+#pragma unroll
+  for (int e = 0; e < E; ++e) reinterpret_cast<T*>(a.out)[r * D + lane * E + e] = from_f32<T>(x[e] * inv);
   if (lane == 0) {
-    const float lse2 = L > 0.f ? M + __builtin_amdgcn_logf(L) : L == 0.f ? -INFINITY : L;
+    const float lse2 = log2_sum(j);
     if (a.lse) a.lse[r] = lse2 * kLn2;
     if (a.lse2) a.lse2[r] = lse2;
   }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0, int64_t rows) {
+  const int64_t r = row0 + int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= row0 + rows) return;
+  float f[kPagedMaxPieces / 64];
+  const Joined j = join_frames(a, r, f);
+  join_row<T, D>(a, r, j, f);
 }
 
 // ---------------------------------------------------------------------------

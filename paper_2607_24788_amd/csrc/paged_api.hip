@@ -63,24 +63,25 @@ int64_t most_seen(const glide_paged_config* c, int64_t max_len) {
   return std::min<int64_t>(n, int64_t(c->window) + c->n_sinks);
 }
 
-// Pieces of a row tile: as many workgroups as fill the card, none shorter
-// than kPagedPieceMin keys.  (max_len only sizes them: the kernels make
-// pieces longer where rows see more.)
-void plan_pieces(const glide_paged_config* c, int64_t tiles, int64_t max_len, PagedArgs* a) {
-  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len));
-  int64_t n = (kPagedWgs + tiles - 1) / std::max<int64_t>(tiles, 1);
-  n = std::min<int64_t>(n, (keys + kPagedPieceMin - 1) / kPagedPieceMin);
-  n = std::max<int64_t>(1, std::min<int64_t>(n, kPagedMaxPieces));
-  a->npiece = int32_t(n);
-  a->piece = int32_t(((keys + n - 1) / n + 127) / 128 * 128);
+int64_t max_pieces(int64_t tiles, int rows) {
+  return std::max<int64_t>(1, std::min<int64_t>(kPagedMaxPieces, kMaxRecords / (std::max<int64_t>(tiles, 1) * rows)));
 }
 
-// Floats of the partial records of `rows` rows in `tiles` row tiles: a launch
-// of more tiles than kPagedWgs is not split.
-int64_t record_floats(const glide_paged_config* c, int64_t rows, int64_t tiles) {
-  const int64_t n = tiles >= kPagedWgs ? 1
-                    : std::min<int64_t>(kPagedMaxPieces, (kPagedWgs + tiles - 1) / std::max<int64_t>(tiles, 1));
-  return n > 1 ? rows * n * (c->head_dim + 2) : 0;
+// Pieces of each of `tiles` row tiles (see kPagedRound).  max_len only sizes
+// them: the kernels make pieces longer where rows see more.
+void plan_pieces(const glide_paged_config* c, int64_t tiles, int rows, bool decode, int64_t max_len, PagedArgs* a) {
+  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len));
+  tiles = std::max<int64_t>(tiles, 1);
+  int64_t n;
+  if (decode) {
+    const int64_t piece = std::min<int64_t>(kPieceLong, std::max<int64_t>(kPieceMin, tiles * keys / kPagedRound));
+    n = (keys + piece - 1) / piece;
+  } else {
+    n = std::min(kPagedRound / tiles, keys / kPiecePrefill);
+  }
+  n = std::max<int64_t>(1, std::min(n, max_pieces(tiles, rows)));
+  a->npiece = int32_t(n);
+  a->piece = int32_t(((keys + n - 1) / n + 127) / 128 * 128);
 }
 
 // Sections of the workspace of one call, in bytes from its start.
@@ -106,15 +107,14 @@ int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1
   return n;
 }
 
-// Rows per tile of a prefill of `tokens` tokens: the tiles kernel (bf16) where
-// its tiles are half full on average or more.  It takes a wave's 16 rows of a
-// page at 32-bit offsets: pages of 16 tokens or more.
-int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu) {
-  if (c->dtype != GLIDE_BF16 || c->page_size < 16) return kPagedRows;
+// Rows per tile of a prefill: the tiles kernel (bf16), also where few of its
+// 128 rows are there (it reads K and V once for all of them).  It takes 16
+// keys of a page at 32-bit offsets: pages of 16 tokens or more, and no rows
+// further apart than that.
+int tile_rows(const glide_paged_config* c, const glide_paged_cache* k) {
   const int64_t far = int64_t(1) << 26;
-  if (k->k_strides[2] > far || k->v_strides[2] > far) return kPagedRows;
-  const int64_t rows = int64_t(cu[c->batch]) * (c->n_q_heads / c->n_kv_heads);
-  return rows * 2 >= row_tiles(c, cu, 0, c->batch, kTileRows) * kTileRows ? kTileRows : kPagedRows;
+  return c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far ? kTileRows
+                                                                                                         : kPagedRows;
 }
 
 void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a) {
@@ -153,11 +153,10 @@ size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_to
   if (check_cfg(cfg) != GLIDE_OK || max_total_tokens < 0) return 0;
   if (max_total_tokens > (int64_t(1) << 31)) return 0;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads, units = int64_t(cfg->batch) * cfg->n_kv_heads;
-  int64_t n = sections(cfg, rows, record_floats(cfg, rows, units) / (cfg->head_dim + 2), weights, true).bytes;
-  // prefill: kPagedWgs tiles at most are split, into 2 * kPagedWgs records of tiles at most
+  const int64_t np = max_pieces(units, kPagedRows);
+  int64_t n = sections(cfg, rows, np > 1 ? rows * np : 0, weights, true).bytes;
   const int64_t prows = max_total_tokens * cfg->n_q_heads;
-  n = std::max(n, sections(cfg, prows, std::min(prows * kPagedMaxPieces, int64_t(2) * kPagedWgs * kTileRows), weights,
-                           false).bytes);
+  n = std::max(n, sections(cfg, prows, std::min(prows * kPagedMaxPieces, kMaxRecords), weights, false).bytes);
   return size_t(std::max<int64_t>(256, n));
 }
 
@@ -193,7 +192,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
   a.out = static_cast<char*>(out);
   a.lse = lse;
   hipStream_t st = hipStream_t(stream);
-  const int per_tile = tile_rows(cfg, cache, cu);
+  const int per_tile = tile_rows(cfg, cache);
   for (int b0 = 0; b0 < cfg->batch;) {
     PagedSeqs t;
     memset(&t, 0, sizeof(t));
@@ -208,7 +207,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
       ++b1;
     }
     t.nseq = b1 - b0;
-    plan_pieces(cfg, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads, max_len, &a);
+    plan_pieces(cfg, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads, per_tile, false, max_len, &a);
     // records by the call's row number: a launch's own rows only
     const int64_t row0 = int64_t(cu[b0]) * cfg->n_q_heads, rows = int64_t(cu[b1]) * cfg->n_q_heads - row0;
     const Sections w = sections(cfg, total_tokens * cfg->n_q_heads, a.npiece > 1 ? rows * a.npiece : 0,
@@ -258,7 +257,7 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
   a.out = static_cast<char*>(out);
   a.lse = lse;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads;
-  plan_pieces(cfg, int64_t(cfg->batch) * cfg->n_kv_heads, max_len, &a);
+  plan_pieces(cfg, int64_t(cfg->batch) * cfg->n_kv_heads, kPagedRows, true, max_len, &a);
   const Sections w = sections(cfg, rows, a.npiece > 1 ? rows * a.npiece : 0, weights, true);
   if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
   char* ws = static_cast<char*>(workspace);
