@@ -87,6 +87,30 @@ hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream);
 // part in the sums, so that no bits of it reach a product.
 static __device__ const uint4 zero_row[32] = {};
 
+// Rows come through global loads.  (A pointer picked from the pools, the
+// call's new rows and zero_row is a generic one to the compiler, and generic
+// loads count as LDS accesses too: every LDS wait would wait for them.)
+typedef const char __attribute__((address_space(1))) * gptr_t;
+// NT: non-temporal, for rows that one workgroup reads once (a decode call).
+// 32 sequences of 16K..32K tokens (3.2 GB) 577 -> 536 us, and a session of 8K
+// (34 MB, in the Infinity Cache from step to step) 18.1 -> 16.8.
+template <bool NT>
+__device__ __forceinline__ uint4 gload16(gptr_t p) {
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  const auto q = (const u32x4_t __attribute__((address_space(1)))*)p;
+  if constexpr (NT) return __builtin_bit_cast(uint4, __builtin_nontemporal_load(q));
+  else return __builtin_bit_cast(uint4, *q);
+}
+// Eight elements.
+template <bool NT>
+__device__ __forceinline__ void gload_frag(Frag<bf16_t>& f, gptr_t p) { f.v = gload16<NT>(p); }
+template <bool NT>
+__device__ __forceinline__ void gload_frag(Frag<float>& f, gptr_t p) {
+  const float4 a = __builtin_bit_cast(float4, gload16<NT>(p)), b = __builtin_bit_cast(float4, gload16<NT>(p + 16));
+  f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+  f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+}
+
 // Page and slot of position j of the sequence whose table row is `row`;
 // false where its page is not allocated.
 struct Slot {

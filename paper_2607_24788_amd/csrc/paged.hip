@@ -72,8 +72,13 @@ __global__ __launch_bounds__(256) void paged_clear_weights(PagedArgs a, PagedSeq
 //   already the right operand of O^T += V^T P^T with keys in the order
 //   4g + 0..3, 16 + 4g + 0..3; V goes through LDS for its columns.
 template <typename T, int D, bool DECODE>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(PagedArgs a, PagedSeqs s) {
-  constexpr int KK = D / 32, CT = D / 16, RS = D + 16 / int(sizeof(T)), ES = int(sizeof(T));
+__global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, PagedSeqs s) {
+  constexpr int KK = D / 32, CT = D / 16, ES = int(sizeof(T));
+  // LDS rows: 32 bytes longer in bf16 (eight consecutive K rows' pieces, and
+  // four V rows' 32-byte segments, in different banks), 16 in fp32 (V alone)
+  constexpr bool KLDS = ES == 2;
+  constexpr int RS = D + (KLDS ? 16 : 4), LPR = D * ES / 16, RPI = 64 / LPR, NL = kPagedTile / RPI;
+  __shared__ __align__(16) T klds[KLDS ? 4 : 1][KLDS ? kPagedTile * RS : 1];
   __shared__ __align__(16) T vlds[4][kPagedTile * RS];
   __shared__ float sm[4][16], sl_[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, lg = lane >> 4;
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(Paged
   const int32_t v0 = int32_t(int64_t(blockIdx.y) * pl < sn.n ? int64_t(blockIdx.y) * pl : sn.n);
   const int32_t v1 = sn.n - v0 > pl ? v0 + pl : sn.n;
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
-  const char* zr = reinterpret_cast<const char*>(zero_row);
+  const gptr_t zr = (gptr_t)zero_row;
 
   Frag<T> qf[KK];
 #pragma unroll
@@ -138,41 +143,65 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(Paged
   }
 
   // Tiles are read one ahead: a tile's rows are asked for as soon as the one
-  // before it is out of the registers (K in its scores, V in LDS), its page
-  // numbers a tile earlier.
+  // before it is out of the registers, its page numbers a tile earlier.
+  // bf16: whole rows by neighbouring lanes (16 bytes each), K and V through
+  // LDS.  fp32: a K fragment's four lanes read whole lines; V alone goes
+  // through LDS.
+  constexpr int NR = KLDS ? 1 : 2;  // rows that a lane looks up: n + 16t, or lane % 32
   struct At {
-    int32_t j[2], page[2];  // position (-1: behind the piece) and page of rows 16t + n
+    int32_t j[NR], page[NR];  // position (-1: behind the piece) and page
   };
   auto look = [&](int32_t x) {
     At p;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int32_t vi = x + 16 * t + n;
+    for (int t = 0; t < NR; ++t) {
+      const int32_t vi = x + (KLDS ? lane & 31 : 16 * t + n);
       p.j[t] = vi < v1 ? sn.pos(vi) : -1;
       p.page[t] = trow[(vi < v1 ? p.j[t] : 0) >> a.shift];
     }
     return p;
   };
-  Frag<T> kf[2][KK], vf[2][KK];
-  uint32_t ok[2];
-  auto fetch = [&](const At& p) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const Slot sl = {p.page[t], p.j[t] & ((1 << a.shift) - 1), true};
-      const bool good = p.j[t] >= 0 && uint32_t(p.page[t]) < uint32_t(a.n_pages);
-      const char* kr = good ? a.kp + slot_offset(a.ks, sl, g) : zr;
-      const char* vr = good ? a.vp + slot_offset(a.vs, sl, g) : zr;
-      if constexpr (DECODE) {
-        if (a.kn && good && p.j[t] == len - 1) {
-          kr = a.kn + (int64_t(b) * a.Hkv + g) * D * ES;
-          vr = a.vn + (int64_t(b) * a.Hkv + g) * D * ES;
-        }
+  // a row's address: the cache's, the call's new row, or zeros
+  auto row_at = [&](bool good, int32_t j, int32_t page, gptr_t* kr, gptr_t* vr) {
+    const Slot sl = {page, j & ((1 << a.shift) - 1), true};
+    *kr = good ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : zr;
+    *vr = good ? (gptr_t)a.vp + slot_offset(a.vs, sl, g) : zr;
+    if constexpr (DECODE) {
+      if (a.kn && good && j == len - 1) {
+        *kr = (gptr_t)a.kn + (int64_t(b) * a.Hkv + g) * D * ES;
+        *vr = (gptr_t)a.vn + (int64_t(b) * a.Hkv + g) * D * ES;
       }
-      ok[t] = uint32_t(__ballot(good)) & 0xffffu;
+    }
+  };
+  Frag<T> kf[2][KK], vf[2][KK];  // bf16: NL pieces each, [0] and [1] in turn
+  uint32_t okm = 0;              // the tile's rows that are there
+  auto fetch = [&](const At& p, int32_t x) {
+    if constexpr (KLDS) {
+      const bool good = p.j[0] >= 0 && uint32_t(p.page[0]) < uint32_t(a.n_pages);
+      okm = uint32_t(__ballot(good));
+      const int32_t page = good ? p.page[0] : -1;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[t][kk].load(reinterpret_cast<const T*>(kr) + 32 * kk + 8 * lg);
+      for (int e = 0; e < NL; ++e) {
+        const int row = e * RPI + lane / LPR;
+        const int32_t pe = __shfl(page, row);
+        gptr_t kr, vr;
+        row_at(pe >= 0, sn.pos(x + row), pe, &kr, &vr);
+        gload_frag<DECODE>(kf[e / KK][e % KK], kr + (lane % LPR) * 16);
+        gload_frag<DECODE>(vf[e / KK][e % KK], vr + (lane % LPR) * 16);
+      }
+    } else {
+      okm = 0;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) vf[t][kk].load(reinterpret_cast<const T*>(vr) + 32 * kk + 8 * lg);
+      for (int t = 0; t < NR; ++t) {
+        const bool good = p.j[t] >= 0 && uint32_t(p.page[t]) < uint32_t(a.n_pages);
+        gptr_t kr, vr;
+        row_at(good, p.j[t], p.page[t], &kr, &vr);
+        okm |= (uint32_t(__ballot(good)) & 0xffffu) << (16 * t);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) gload_frag<DECODE>(kf[t][kk], kr + (32 * kk + 8 * lg) * ES);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) gload_frag<DECODE>(vf[t][kk], vr + (32 * kk + 8 * lg) * ES);
+      }
     }
   };
   constexpr int STEP = 4 * kPagedTile;
@@ -181,31 +210,50 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(Paged
   if (x < v1) {
     const At first = look(x);
     next = look(x + STEP);
-    fetch(first);
+    fetch(first, x);
   }
   for (; x < v1; x += STEP) {
     f32x4_t sc[2] = {zero4(), zero4()};
+    const uint32_t okc = okm;
+    if constexpr (KLDS) {
+      T* kt = klds[wave];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        T* w = vt + (16 * t + n) * RS + 32 * kk + 8 * lg;
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<uint4*>(w) = vf[t][kk].v;
-        } else {
-          reinterpret_cast<float4*>(w)[0] = make_float4(vf[t][kk].v[0], vf[t][kk].v[1], vf[t][kk].v[2], vf[t][kk].v[3]);
-          reinterpret_cast<float4*>(w)[1] = make_float4(vf[t][kk].v[4], vf[t][kk].v[5], vf[t][kk].v[6], vf[t][kk].v[7]);
-        }
+      for (int e = 0; e < NL; ++e) {
+        const int at = (e * RPI + lane / LPR) * RS + (lane % LPR) * 8;
+        *reinterpret_cast<uint4*>(kt + at) = kf[e / KK][e % KK].v;
+        *reinterpret_cast<uint4*>(vt + at) = vf[e / KK][e % KK].v;
       }
-    const uint32_t okc[2] = {ok[0], ok[1]};
-    if (x + STEP < v1) {
-      const At now = next;
-      next = look(x + 2 * STEP);
-      fetch(now);
+      wave_lds_order();
+      if (x + STEP < v1) {
+        const At now = next;
+        next = look(x + 2 * STEP);
+        fetch(now, x + STEP);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          Frag<T> k;
+          k.load(kt + (16 * t + n) * RS + 32 * kk + 8 * lg);
+          sc[t] = mma(k, qf[kk], sc[t]);
+        }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
+          float w[8];
+          vf[t][kk].to_floats(w);
+          float4* at = reinterpret_cast<float4*>(vt + (16 * t + n) * RS + 32 * kk + 8 * lg);
+          at[0] = make_float4(w[0], w[1], w[2], w[3]);
+          at[1] = make_float4(w[4], w[5], w[6], w[7]);
+        }
+      if (x + STEP < v1) {
+        const At now = next;
+        next = look(x + 2 * STEP);
+        fetch(now, x + STEP);
+      }
     }
     float p[8];
     float mx = m;
@@ -214,7 +262,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void attend_rows(Paged
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = 4 * lg + i;
-        bool see = (okc[t] >> key) & 1;
+        bool see = (okc >> (16 * t + key)) & 1;
         if constexpr (!DECODE) {
           const int32_t j = sn.pos(x + 16 * t + key);
           see = see && j <= tr && (j > tr - a.W || j < a.ns);
@@ -742,9 +790,9 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
       Slot sl = {0, 0, false};
       if (vi < sn.n) sl = paged_slot(trow, sn.pos(vi), a.shift, a.n_pages);
       ok[t] = uint32_t(__ballot(sl.ok)) & 0xffffu;
-      const char* kr = sl.ok ? a.kp + slot_offset(a.ks, sl, g) : reinterpret_cast<const char*>(zero_row);
+      const gptr_t kr = sl.ok ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : (gptr_t)zero_row;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[t][kk].load(reinterpret_cast<const T*>(kr) + 32 * kk + 8 * lg);
+      for (int kk = 0; kk < KK; ++kk) gload_frag<false>(kf[t][kk], kr + (32 * kk + 8 * lg) * int(sizeof(T)));
     }
     float w[2][4] = {};
     const int32_t rend = ntok * a.G;
