@@ -22,23 +22,17 @@ __device__ __forceinline__ int64_t weight_at(const EvictArgs& a, int32_t page, i
 }
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kSelKeys = 32;  // keys of a thread: 32K tokens in registers
-constexpr int kBins = 2048, kCopies = 8;
+constexpr int kBins = 2048, kCopies = 2;
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t y = __shfl_up(x, d);
-    if (int(threadIdx.x & 63) >= d) x += y;
-  }
-  return x;
-}
 // Exclusive sum over the workgroup's threads; wsum: one entry per wave.
-// Begins and ends with a barrier's worth of order on wsum.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t inc = wave_scan(x);
+  uint32_t inc = x;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t y = __shfl_up(inc, d);
+    if (lane >= d) inc += y;
+  }
   __syncthreads();
   if (lane == 63) wsum[wave] = inc;
   __syncthreads();
@@ -55,17 +49,22 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint3
 
 // Which tokens stay, one workgroup per (sequence, KV head).  The need-th
 // largest key is found by its 11, 11 and 10 bits: a histogram in LDS of the
-// keys that agree so far (integer counts, so no order of atomics shows; eight
-// copies, as weights of like size share their first bits), then the bin by a
-// sum from the top.  Then every key above it stays, and the first of those
-// equal to it; ranks come from the waves' ballots in the order of positions.
-// Keys are read once and kept in registers up to 32K tokens, read again per
-// pass above.  Bound by the latency of a dozen barriers and one read.
+// keys that agree so far (integer counts, so no order of atomics shows), then
+// the bin by a sum from the top.  Then every key above it stays, and the first
+// of those equal to it; ranks come from the waves' ballots in the order of
+// positions.  Keys are read once and kept in LDS up to KEYS tokens; longer
+// sequences go through LDS in segments, read again per pass.  Bound by the
+// latency of the reads and of two dozen barriers.  (Keys in registers, their
+// loops unrolled: 24 us at 8K tokens and 21 at 700, most of it the fetch of
+// the code.)
+template <int KEYS>
 __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
+  constexpr int ROWS = KEYS / kSelThreads, NC = ROWS * kSelWaves;  // counts, one per 64 positions
+  __shared__ uint32_t key[KEYS];
   __shared__ uint32_t hist[kBins * kCopies];
-  __shared__ uint32_t cnt[kSelKeys * kSelWaves];  // a row of 64 positions each
+  __shared__ uint32_t cnt[NC];
   __shared__ uint32_t wsum[kSelWaves], pick[2];
-  static_assert(kSelKeys * kSelWaves <= kSelThreads, "a thread per count");
+  static_assert(NC <= kSelThreads, "a thread per count");
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t len = seq_len(a, b);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
@@ -84,33 +83,35 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   for (int32_t j = tid; j < len - hi; j += kSelThreads) kept[lo + quota + j] = hi + j;
   if (quota == 0) return;
 
-  constexpr int32_t kSeg = kSelThreads * kSelKeys;
-  uint32_t key[kSelKeys];
-  auto load = [&](int32_t j0) {  // keys of positions j0 + 1024 i + tid
+  // keys of positions [j0, j0 + KEYS) to LDS, eight loads of a thread at once;
+  // the number of them
+  auto load = [&](int32_t j0) {
+    const int32_t n = hi - j0 < KEYS ? hi - j0 : KEYS;
+    for (int32_t i0 = 0; i0 < n; i0 += 8 * kSelThreads) {
+      int32_t page[8];
+      float w[8];
 #pragma unroll
-    for (int i = 0; i < kSelKeys; ++i) {
-      const int32_t j = j0 + i * kSelThreads + tid;
-      key[i] = 0xffffffffu;
-      if (j0 + i * kSelThreads < hi) key[i] = uint32_t(trow[(j < hi ? j : lo) >> a.shift]);
-    }
+      for (int u = 0; u < 8; ++u) {
+        const int32_t i = i0 + u * kSelThreads + tid;
+        page[u] = i < n ? trow[(j0 + i) >> a.shift] : -1;
+      }
 #pragma unroll
-    for (int i0 = 0; i0 < kSelKeys; i0 += 8) {
-      if (j0 + i0 * kSelThreads < hi) {
-        float w[8];
+      for (int u = 0; u < 8; ++u) {
+        const int32_t i = i0 + u * kSelThreads + tid;
+        w[u] = uint32_t(page[u]) < uint32_t(a.n_pages) ? a.wp[weight_at(a, page[u], g, j0 + i)] : NAN;
+      }
 #pragma unroll
-        for (int i = i0; i < i0 + 8; ++i) {
-          const int32_t j = j0 + i * kSelThreads + tid;
-          const bool ok = j < hi && key[i] < uint32_t(a.n_pages);
-          w[i - i0] = a.wp[ok ? weight_at(a, int32_t(key[i]), g, j) : 0];
-          if (!ok) w[i - i0] = NAN;
-        }
-#pragma unroll
-        for (int i = i0; i < i0 + 8; ++i) key[i] = weight_key(w[i - i0]);
+      for (int u = 0; u < 8; ++u) {
+        const int32_t i = i0 + u * kSelThreads + tid;
+        if (i < n) key[i] = weight_key(w[u]);
       }
     }
+    return n;
   };
-  const bool once = hi - lo <= kSeg;
-  if (once) load(lo);
+  // (a thread reads back the keys that it wrote: no barrier between)
+  const bool once = hi - lo <= KEYS;
+  int32_t n = 0;
+  if (once) n = load(lo);
 
   uint32_t need = quota, thr = 0;
   int shift = 32;
@@ -119,31 +120,24 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
     shift -= bits;
     for (int i = tid; i < kBins * kCopies; i += kSelThreads) hist[i] = 0;
     __syncthreads();
-    for (int32_t j0 = lo; j0 < hi; j0 += kSeg) {
-      if (!once) load(j0);
-#pragma unroll
-      for (int i = 0; i < kSelKeys; ++i) {
-        if (j0 + i * kSelThreads >= hi) continue;
+    for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
+      if (!once) n = load(j0);
+      for (int32_t i = tid; i < n; i += kSelThreads) {
         const uint32_t k = key[i];
-        if (j0 + i * kSelThreads + tid < hi && (pass == 0 || (k >> below) == (thr >> below)))
+        if (pass == 0 || ((k ^ thr) >> below) == 0)
           atomicAdd(&hist[((k >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
       }
     }
     __syncthreads();
     // two bins per thread, from the top: thread t has bins 2047 - 2t, 2046 - 2t
-    uint32_t c[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint4* h = reinterpret_cast<const uint4*>(hist + (kBins - 1 - 2 * tid - u) * kCopies);
-      const uint4 x = h[0], y = h[1];
-      c[u] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
-    }
+    const uint4 h = reinterpret_cast<const uint4*>(hist)[kBins / 2 - 1 - tid];
+    const uint32_t c0 = h.z + h.w, c1 = h.x + h.y;
     uint32_t total;
-    const uint32_t above = block_scan(c[0] + c[1], wsum, &total);
-    if (above < need && above + c[0] + c[1] >= need) {
-      const bool second = above + c[0] < need;
+    const uint32_t above = block_scan(c0 + c1, wsum, &total);
+    if (above < need && above + c0 + c1 >= need) {
+      const bool second = above + c0 < need;
       pick[0] = kBins - 1 - 2 * tid - (second ? 1 : 0);
-      pick[1] = need - above - (second ? c[0] : 0);
+      pick[1] = need - above - (second ? c0 : 0);
     }
     __syncthreads();
     thr |= pick[0] << shift;
@@ -151,57 +145,50 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   }
 
   int32_t at = lo;         // kept so far
-  uint32_t equal = 0;      // of them equal to thr
-  for (int32_t j0 = lo; j0 < hi; j0 += kSeg) {
-    if (!once) load(j0);
+  uint32_t equal = 0;      // seen so far that are equal to thr
+  const uint64_t lt = (uint64_t(1) << lane) - 1;
+  for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
+    if (!once) n = load(j0);
+    const int rows = (n + kSelThreads - 1) / kSelThreads;
     // keys equal to thr before each row of 64 positions
-    if (tid < kSelKeys * kSelWaves) cnt[tid] = 0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSelKeys; ++i) {
-      if (j0 + i * kSelThreads >= hi) continue;
-      const uint64_t e = __ballot(j0 + i * kSelThreads + tid < hi && key[i] == thr);
-      if (lane == 0) cnt[i * kSelWaves + wave] = __popcll(e);
+    for (int r = 0; r < rows; ++r) {
+      const int32_t i = r * kSelThreads + tid;
+      const uint64_t e = __ballot(i < n && key[i] == thr);
+      if (lane == 0) cnt[r * kSelWaves + wave] = __popcll(e);
     }
     uint32_t all, kall;
     __syncthreads();
-    const uint32_t eq0 = block_scan(tid < kSelKeys * kSelWaves ? cnt[tid] : 0, wsum, &all);
-    if (tid < kSelKeys * kSelWaves) cnt[tid] = eq0;
+    const bool mine = tid < rows * kSelWaves;
+    const uint32_t eq0 = block_scan(mine ? cnt[tid] : 0, wsum, &all);
+    if (mine) cnt[tid] = eq0;
     __syncthreads();
-    // which stay (a bit per key), and their counts
+    // which stay: a bit per row of this thread's keys
     uint32_t stay = 0;
-    const uint64_t lt = (uint64_t(1) << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < kSelKeys; ++i) {
-      if (j0 + i * kSelThreads >= hi) continue;
-      const bool in = j0 + i * kSelThreads + tid < hi, eq = in && key[i] == thr;
+    for (int r = 0; r < rows; ++r) {
+      const int32_t i = r * kSelThreads + tid;
+      const uint32_t k = i < n ? key[i] : 0;
+      const bool eq = i < n && k == thr;
       const uint64_t e = __ballot(eq);
-      const uint32_t rank = equal + cnt[i * kSelWaves + wave] + __popcll(e & lt);
-      if (in && (key[i] > thr || (eq && rank < need))) stay |= 1u << i;
+      const uint32_t rank = equal + cnt[r * kSelWaves + wave] + __popcll(e & lt);
+      if (i < n && (k > thr || (eq && rank < need))) stay |= 1u << r;
     }
     __syncthreads();
-    if (tid < kSelKeys * kSelWaves) cnt[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSelKeys; ++i) {
-      if (j0 + i * kSelThreads >= hi) continue;
-      const uint64_t e = __ballot((stay >> i) & 1);
-      if (lane == 0) cnt[i * kSelWaves + wave] = __popcll(e);
+    for (int r = 0; r < rows; ++r) {
+      const uint64_t e = __ballot((stay >> r) & 1);
+      if (lane == 0) cnt[r * kSelWaves + wave] = __popcll(e);
     }
     __syncthreads();
-    const uint32_t k0 = block_scan(tid < kSelKeys * kSelWaves ? cnt[tid] : 0, wsum, &kall);
-    if (tid < kSelKeys * kSelWaves) cnt[tid] = k0;
+    const uint32_t k0 = block_scan(mine ? cnt[tid] : 0, wsum, &kall);
+    if (mine) cnt[tid] = k0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSelKeys; ++i) {
-      if (j0 + i * kSelThreads >= hi) continue;
-      const bool on = (stay >> i) & 1;
+    for (int r = 0; r < rows; ++r) {
+      const bool on = (stay >> r) & 1;
       const uint64_t e = __ballot(on);
-      if (on) kept[at + cnt[i * kSelWaves + wave] + __popcll(e & lt)] = j0 + i * kSelThreads + tid;
+      if (on) kept[at + cnt[r * kSelWaves + wave] + __popcll(e & lt)] = j0 + r * kSelThreads + tid;
     }
     at += kall;
     equal += all;
-    __syncthreads();
   }
 }
 
@@ -309,7 +296,9 @@ __global__ __launch_bounds__(1024) void evict_move(EvictArgs a) {
 
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream) {
   const uint32_t units = uint32_t(a.B) * a.Hkv;
-  evict_select<<<units, kSelThreads, 0, stream>>>(a);
+  // the smaller LDS lets a CU hold several of them
+  if (a.cap <= 4096) evict_select<4096><<<units, kSelThreads, 0, stream>>>(a);
+  else evict_select<32768><<<units, kSelThreads, 0, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.in_place) {

@@ -76,10 +76,12 @@ struct EvictArgs {
 
 hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const void* k, const void* v, int d, int dtype,
                                hipStream_t stream);
+// keys: visible tokens of a sequence, at most (it sizes a grid only)
+hipError_t launch_paged_decode(const PagedArgs& a, int64_t keys, int d, int dtype, hipStream_t stream);
 // tile_rows: kPagedRows (attend_rows) or kTileRows (attend_tiles, bf16 only)
-hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, int tile_rows,
-                               hipStream_t stream);
-hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs* s, int n_observe, int64_t keys, int d, int dtype,
+hipError_t launch_paged_prefill(const PagedArgs& a, const PagedSeqs& s, int d, int dtype, int tile_rows,
+                                hipStream_t stream);
+hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs& s, int n_observe, int64_t keys, int d, int dtype,
                                 hipStream_t stream);
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream);
 

@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, PagedSeqs s) 
     }
     __syncthreads();
   }
-  const bool split = a.npiece > 1;
+  const bool split = a.npiece > 1 || (DECODE && a.scores);  // join_weights joins one piece too
   if (wave == 0 && lane < 16 && rok) {
     if (split) {
       float* ml = a.ml + (orow * a.npiece + blockIdx.y) * 2;
@@ -657,9 +657,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
 }
 
-// The pieces of rows joined, a wave per row: its lanes take the pieces'
-// frames and sums (npiece <= 256, four each), then the elements.  Latency: the
-// records of eight pieces are asked for at once.
+// The pieces of a row joined by a workgroup: a wave's lanes take the pieces'
+// frames and sums (npiece <= 256, four each).  Bound by latency.
 struct Joined {
   float M, L;
 };
@@ -695,31 +694,40 @@ __device__ __forceinline__ float log2_sum(const Joined& j) {
   return j.L > 0.f ? j.M + __builtin_amdgcn_logf(j.L) : j.L == 0.f ? -INFINITY : j.L;
 }
 
+// Row r's output by the workgroup: its four waves take every fourth piece,
+// eight records at a time; wave 0 adds their sums up in order.
 template <typename T, int D>
-__device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Joined& j, const float* f) {
+__device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Joined& j, const float* f,
+                                         float (*part)[D]) {
   constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float* acc = a.acc + r * a.npiece * D + lane * E;
   float x[E] = {};
-  for (int i0 = 0; i0 < a.npiece; i0 += 8) {
-    const float fu = i0 < 64 ? f[0] : i0 < 128 ? f[1] : i0 < 192 ? f[2] : f[3];
+  for (int i0 = wave; i0 < a.npiece; i0 += 32) {
     float y[8][E], w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      w[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), (i0 + i) & 63));
-      const bool on = i0 + i < a.npiece && w[i] != 0.f;
+      const int p = i0 + 4 * i;
+      const float fu = p < 64 ? f[0] : p < 128 ? f[1] : p < 192 ? f[2] : f[3];
+      w[i] = p < a.npiece ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), p & 63)) : 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[i][e] = on ? acc[int64_t(i0 + i) * D + e] : 0.f;
+      for (int e = 0; e < E; ++e) y[i][e] = w[i] != 0.f ? acc[int64_t(p) * D + e] : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] += (i0 + i < a.npiece ? w[i] : 0.f) * y[i][e];
+      for (int e = 0; e < E; ++e) x[e] += w[i] * y[i][e];
   }
-  const float inv = j.L == 0.f ? 0.f : 1.f / j.L;
+  __syncthreads();
 #pragma unroll
-  for (int e = 0; e < E; ++e) reinterpret_cast<T*>(a.out)[r * D + lane * E + e] = from_f32<T>(x[e] * inv);
-  if (lane == 0) {
+  for (int e = 0; e < E; ++e) part[wave][lane * E + e] = x[e];
+  __syncthreads();
+  const float inv = j.L == 0.f ? 0.f : 1.f / j.L;
+  if (int(threadIdx.x) < D) {
+    const float y = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+    reinterpret_cast<T*>(a.out)[r * D + threadIdx.x] = from_f32<T>(y * inv);
+  }
+  if (threadIdx.x == 0) {
     const float lse2 = log2_sum(j);
     if (a.lse) a.lse[r] = lse2 * kLn2;
     if (a.lse2) a.lse2[r] = lse2;
@@ -727,42 +735,59 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Jo
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0, int64_t rows) {
-  const int64_t r = row0 + int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r >= row0 + rows) return;
+__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0) {
+  __shared__ float part[4][D];
+  const int64_t r = row0 + blockIdx.x;
   float f[kPagedMaxPieces / 64];
   const Joined j = join_frames(a, r, f);
-  join_row<T, D>(a, r, j, f);
+  join_row<T, D>(a, r, j, f, part);
 }
 
 // ---------------------------------------------------------------------------
 // Decode: weights_j += sum over the group's heads of e^{s_j - lse}, from the
-// raw scores that the attention left.  One thread per visible token.
-__global__ __launch_bounds__(256) void decode_weights(PagedArgs a) {
-  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
+// raw scores that the attention left, and the rows' pieces joined in the same
+// launch.  A workgroup takes every gridDim.y-th 1024 visible tokens of a
+// (sequence, KV head) and every gridDim.y-th of its rows.  Bound by latency:
+// the scores were just written, and are read once.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
+  __shared__ float part[4][D], z[kMaxG];
+  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, wave = threadIdx.x >> 6;
+  const int64_t row0 = int64_t(b) * a.Hq + g * a.G;
+  float f[kPagedMaxPieces / 64];
+  for (int h = wave; h < a.G; h += 4) {
+    const Joined j = join_frames(a, row0 + h, f);
+    if ((threadIdx.x & 63) == 0) z[h] = log2_sum(j);
+  }
+  for (int h = blockIdx.y; h < a.G; h += gridDim.y) {
+    const Joined j = join_frames(a, row0 + h, f);
+    join_row<T, D>(a, row0 + h, j, f, part);
+  }
+  __syncthreads();
   const int32_t len = seq_len(a, b);
   if (len == 0) return;
   const Seen sn = seen_by(len - 1, len - 1, a.W, a.ns);
-  const int32_t v0 = blockIdx.y * 256 + threadIdx.x;
-  // the appended token's weight starts from 0, also where it is not seen
-  const bool fresh = a.kn && v0 == 0 && (sn.n == 0 || sn.pos(sn.n - 1) != len - 1);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
-  if (fresh) {
+  const int32_t v0 = blockIdx.y * 1024 + threadIdx.x;
+  // the appended token's weight starts from 0, also where it is not seen
+  if (a.kn && v0 == 0 && (sn.n == 0 || sn.pos(sn.n - 1) != len - 1)) {
     const Slot sl = paged_slot(trow, len - 1, a.shift, a.n_pages);
     if (sl.ok) a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] = 0.f;
   }
-  for (int32_t v = v0; v < sn.n; v += int32_t(gridDim.y) * 256) {
-    const int32_t j = sn.pos(v);
-    const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
-    if (!sl.ok) continue;
-    float w = 0.f;
-    for (int h = 0; h < a.G; ++h) {
-      const int64_t r = int64_t(b) * a.Hq + g * a.G + h;
-      const float z = a.lse2[r];
-      w += z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.scores[r * a.nv + v] - z);
+  for (int64_t v1 = v0; v1 < sn.n; v1 += int64_t(gridDim.y) * 1024) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t v = v1 + 256 * u;
+      if (v >= sn.n) break;
+      const int32_t j = sn.pos(int32_t(v));
+      const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+      if (!sl.ok) continue;
+      float* at = a.wp + ((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot;
+      float w = 0.f;
+      for (int h = 0; h < a.G; ++h)
+        w += z[h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.scores[(row0 + h) * a.nv + v] - z[h]);
+      *at = (a.kn && j == len - 1 ? 0.f : *at) + w;
     }
-    float* at = a.wp + ((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot;
-    *at = (a.kn && j == len - 1 ? 0.f : *at) + w;
   }
 }
 
@@ -835,30 +860,36 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
 }
 
 template <typename T, int D>
-hipError_t attend_t(const PagedArgs& a, const PagedSeqs* s, int tile_rows, hipStream_t stream) {
+hipError_t decode_t(const PagedArgs& a, int64_t keys, hipStream_t stream) {
   static const PagedSeqs none = {};
-  if (!s) {
-    attend_rows<T, D, true><<<dim3(a.B * a.Hkv, a.npiece), 256, 0, stream>>>(a, none);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.npiece == 1) return e;
-    const int64_t rows = int64_t(a.B) * a.Hq;
-    paged_join<T, D><<<dim3(uint32_t((rows + 3) / 4)), 256, 0, stream>>>(a, 0, rows);
-    return hipGetLastError();
+  attend_rows<T, D, true><<<dim3(a.B * a.Hkv, a.npiece), 256, 0, stream>>>(a, none);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.scores) {
+    const int64_t chunks = std::min<int64_t>((keys + 1023) / 1024, 65535);
+    join_weights<T, D><<<dim3(a.B * a.Hkv, uint32_t(chunks)), 256, 0, stream>>>(a);
+  } else if (a.npiece > 1) {
+    paged_join<T, D><<<uint32_t(a.B * a.Hq), 256, 0, stream>>>(a, 0);
   }
-  const int64_t tiles = s->tile0[s->nseq];
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t prefill_t(const PagedArgs& a, const PagedSeqs& s, int tile_rows, hipStream_t stream) {
+  const int64_t tiles = s.tile0[s.nseq];
   if (tiles == 0) return hipSuccess;
   const dim3 grid(uint32_t(tiles * a.Hkv), a.npiece);
   if constexpr (sizeof(T) == 2) {
-    if (tile_rows == kTileRows) attend_tiles<D><<<grid, 256, 0, stream>>>(a, *s);
-    else attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, *s);
+    if (tile_rows == kTileRows) attend_tiles<D><<<grid, 256, 0, stream>>>(a, s);
+    else attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, s);
   } else {
-    attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, *s);
+    attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, s);
   }
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.npiece == 1) return e;
-  const int64_t row0 = int64_t(s->start[0]) * a.Hq;
-  const int64_t rows = (int64_t(s->start[s->nseq - 1]) + s->len[s->nseq - 1]) * a.Hq - row0;
-  paged_join<T, D><<<dim3(uint32_t((rows + 3) / 4)), 256, 0, stream>>>(a, row0, rows);
+  const int64_t row0 = int64_t(s.start[0]) * a.Hq;
+  const int64_t rows = (int64_t(s.start[s.nseq - 1]) + s.len[s.nseq - 1]) * a.Hq - row0;
+  paged_join<T, D><<<uint32_t(rows), 256, 0, stream>>>(a, row0);
   return hipGetLastError();
 }
 
@@ -887,26 +918,28 @@ hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const voi
   return hipSuccess;
 }
 
-hipError_t launch_paged_attend(const PagedArgs& a, const PagedSeqs* s, int d, int dtype, int tile_rows,
-                               hipStream_t stream) {
+hipError_t launch_paged_decode(const PagedArgs& a, int64_t keys, int d, int dtype, hipStream_t stream) {
   if (dtype == GLIDE_BF16)
-    return d == 128 ? attend_t<bf16_t, 128>(a, s, tile_rows, stream) : attend_t<bf16_t, 64>(a, s, tile_rows, stream);
-  return d == 128 ? attend_t<float, 128>(a, s, tile_rows, stream) : attend_t<float, 64>(a, s, tile_rows, stream);
+    return d == 128 ? decode_t<bf16_t, 128>(a, keys, stream) : decode_t<bf16_t, 64>(a, keys, stream);
+  return d == 128 ? decode_t<float, 128>(a, keys, stream) : decode_t<float, 64>(a, keys, stream);
 }
 
-hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs* s, int n_observe, int64_t keys, int d, int dtype,
+hipError_t launch_paged_prefill(const PagedArgs& a, const PagedSeqs& s, int d, int dtype, int tile_rows,
                                 hipStream_t stream) {
-  if (!s) {
-    decode_weights<<<dim3(a.B * a.Hkv, uint32_t(std::min<int64_t>((keys + 255) / 256, 4096))), 256, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  const dim3 grid(s->nseq * a.Hkv, uint32_t(std::min<int64_t>((keys + 127) / 128, 4096)));
+  if (dtype == GLIDE_BF16)
+    return d == 128 ? prefill_t<bf16_t, 128>(a, s, tile_rows, stream) : prefill_t<bf16_t, 64>(a, s, tile_rows, stream);
+  return d == 128 ? prefill_t<float, 128>(a, s, tile_rows, stream) : prefill_t<float, 64>(a, s, tile_rows, stream);
+}
+
+hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs& s, int n_observe, int64_t keys, int d, int dtype,
+                                hipStream_t stream) {
+  const dim3 grid(s.nseq * a.Hkv, uint32_t(std::min<int64_t>((keys + 127) / 128, 4096)));
   if (dtype == GLIDE_BF16) {
-    if (d == 128) prefill_weights<bf16_t, 128><<<grid, 256, 0, stream>>>(a, *s, n_observe);
-    else prefill_weights<bf16_t, 64><<<grid, 256, 0, stream>>>(a, *s, n_observe);
+    if (d == 128) prefill_weights<bf16_t, 128><<<grid, 256, 0, stream>>>(a, s, n_observe);
+    else prefill_weights<bf16_t, 64><<<grid, 256, 0, stream>>>(a, s, n_observe);
   } else {
-    if (d == 128) prefill_weights<float, 128><<<grid, 256, 0, stream>>>(a, *s, n_observe);
-    else prefill_weights<float, 64><<<grid, 256, 0, stream>>>(a, *s, n_observe);
+    if (d == 128) prefill_weights<float, 128><<<grid, 256, 0, stream>>>(a, s, n_observe);
+    else prefill_weights<float, 64><<<grid, 256, 0, stream>>>(a, s, n_observe);
   }
   return hipGetLastError();
 }

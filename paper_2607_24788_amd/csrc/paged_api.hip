@@ -154,7 +154,7 @@ size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_to
   if (max_total_tokens > (int64_t(1) << 31)) return 0;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads, units = int64_t(cfg->batch) * cfg->n_kv_heads;
   const int64_t np = max_pieces(units, kPagedRows);
-  int64_t n = sections(cfg, rows, np > 1 ? rows * np : 0, weights, true).bytes;
+  int64_t n = sections(cfg, rows, np > 1 || weights ? rows * np : 0, weights, true).bytes;
   const int64_t prows = max_total_tokens * cfg->n_q_heads;
   n = std::max(n, sections(cfg, prows, std::min(prows * kPagedMaxPieces, kMaxRecords), weights, false).bytes);
   return size_t(std::max<int64_t>(256, n));
@@ -219,14 +219,14 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
     if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
     s = hip_status(launch_paged_append(a, t, k, v, cfg->head_dim, cfg->dtype, st));
     if (s != GLIDE_OK) return s;
-    s = hip_status(launch_paged_attend(a, &t, cfg->head_dim, cfg->dtype, per_tile, st));
+    s = hip_status(launch_paged_prefill(a, t, cfg->head_dim, cfg->dtype, per_tile, st));
     if (s != GLIDE_OK) return s;
     if (n_observe > 0) {
       int32_t longest = 0;
       for (int i = 0; i < t.nseq; ++i) longest = std::max(longest, t.len[i]);
       const int64_t seen = std::min<int64_t>(capacity(cfg), int64_t(cfg->window) + cfg->n_sinks +
                                                                 std::min(longest, n_observe));
-      s = hip_status(launch_paged_weights(a, &t, n_observe, seen, cfg->head_dim, cfg->dtype, st));
+      s = hip_status(launch_paged_weights(a, t, n_observe, seen, cfg->head_dim, cfg->dtype, st));
       if (s != GLIDE_OK) return s;
     }
     b0 = b1;
@@ -258,20 +258,17 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
   a.lse = lse;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads;
   plan_pieces(cfg, int64_t(cfg->batch) * cfg->n_kv_heads, kPagedRows, true, max_len, &a);
-  const Sections w = sections(cfg, rows, a.npiece > 1 ? rows * a.npiece : 0, weights, true);
+  const Sections w = sections(cfg, rows, a.npiece > 1 || weights ? rows * a.npiece : 0, weights, true);
   if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
   char* ws = static_cast<char*>(workspace);
   a.acc = reinterpret_cast<float*>(ws + w.acc);
   a.ml = reinterpret_cast<float*>(ws + w.ml);
   if (weights) {
-    a.lse2 = reinterpret_cast<float*>(ws + w.lse2);
     a.scores = reinterpret_cast<float*>(ws + w.scores);
     a.nv = (most_seen(cfg, 0) + 31) / 32 * 32;
   }
-  hipStream_t st = hipStream_t(stream);
-  s = hip_status(launch_paged_attend(a, nullptr, cfg->head_dim, cfg->dtype, kPagedRows, st));
-  if (s != GLIDE_OK || !weights) return s;
-  return hip_status(launch_paged_weights(a, nullptr, 0, most_seen(cfg, max_len), cfg->head_dim, cfg->dtype, st));
+  return hip_status(launch_paged_decode(a, std::max<int64_t>(1, most_seen(cfg, max_len)), cfg->head_dim, cfg->dtype,
+                                        hipStream_t(stream)));
 }
 
 glide_status glide_paged_evict(const glide_paged_config* cfg, const glide_paged_cache* cache, int32_t budget,

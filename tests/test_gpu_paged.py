@@ -79,6 +79,12 @@ def test_decode_length_hint_changes_no_result(max_len):
     run_decode(Case(2, 8, 2, 128, 16, [2100, 600], dtype=FP32, weights=True, seed=3), True, max_len)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_decode_over_many_pieces(dtype):
+    """A long sequence of one KV head: as many pieces as a join takes."""
+    run_decode(Case(1, 4, 1, 64, 64, [40001], None, 0, dtype=dtype, weights=True, seed=8), True, 40001)
+
+
 @pytest.mark.parametrize("order", ["nhd", "joined"])
 def test_decode_strided_pools(order):
     run_decode(Case(2, 8, 2, 128, 32, [300, 77], 200, 2, seed=4, order=order, weights=True), True)
@@ -256,6 +262,12 @@ def test_evict_equal_and_special_weights():
     x, y = case.w.cpu().double(), ref.w
     assert ((x == y) | (x.isnan() & y.isnan())).all()
     case.pools_equal(ref)
+
+
+@pytest.mark.parametrize("n", [4096, 4097, 33000, 70003])
+def test_evict_long(n):
+    """Keys that fill LDS, and more than it holds."""
+    run_evict(Case(1, 2, 1, 64, 64, [n], 4, 0, dtype=BF16, weights=True, seed=92, extra_pages=0), n // 3, n // 10)
 
 
 def test_evict_missing_pages():
