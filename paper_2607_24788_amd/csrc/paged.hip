@@ -746,48 +746,51 @@ __global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0) {
 // ---------------------------------------------------------------------------
 // Decode: weights_j += sum over the group's heads of e^{s_j - lse}, from the
 // raw scores that the attention left, and the rows' pieces joined in the same
-// launch.  A workgroup takes every gridDim.y-th 1024 visible tokens of a
-// (sequence, KV head) and every gridDim.y-th of its rows.  Bound by latency:
-// the scores were just written, and are read once.
+// launch: of a (sequence, KV head) the first G workgroups join a row each, the
+// others take 256 visible tokens each.  Bound by latency: the frames of the
+// rows, then one read of the scores (asked for before the frames: no faster).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
   __shared__ float part[4][D], z[kMaxG];
-  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, wave = threadIdx.x >> 6;
+  const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
   const int64_t row0 = int64_t(b) * a.Hq + g * a.G;
   float f[kPagedMaxPieces / 64];
-  for (int h = wave; h < a.G; h += 4) {
+  if (int(blockIdx.y) < a.G) {
+    const Joined j = join_frames(a, row0 + blockIdx.y, f);
+    join_row<T, D>(a, row0 + blockIdx.y, j, f, part);
+    return;
+  }
+#pragma unroll 1
+  for (int h = threadIdx.x >> 6; h < a.G; h += 4) {
     const Joined j = join_frames(a, row0 + h, f);
     if ((threadIdx.x & 63) == 0) z[h] = log2_sum(j);
   }
-  for (int h = blockIdx.y; h < a.G; h += gridDim.y) {
-    const Joined j = join_frames(a, row0 + h, f);
-    join_row<T, D>(a, row0 + h, j, f, part);
-  }
-  __syncthreads();
   const int32_t len = seq_len(a, b);
+  __syncthreads();
   if (len == 0) return;
   const Seen sn = seen_by(len - 1, len - 1, a.W, a.ns);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
-  const int32_t v0 = blockIdx.y * 1024 + threadIdx.x;
+  const int32_t v0 = (blockIdx.y - a.G) * 256 + threadIdx.x;
   // the appended token's weight starts from 0, also where it is not seen
   if (a.kn && v0 == 0 && (sn.n == 0 || sn.pos(sn.n - 1) != len - 1)) {
     const Slot sl = paged_slot(trow, len - 1, a.shift, a.n_pages);
     if (sl.ok) a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] = 0.f;
   }
-  for (int64_t v1 = v0; v1 < sn.n; v1 += int64_t(gridDim.y) * 1024) {
+#pragma unroll 1
+  for (int64_t v = v0; v < sn.n; v += int64_t(gridDim.y - a.G) * 256) {
+    const int32_t j = sn.pos(int32_t(v));
+    const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+    float s[kMaxG];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t v = v1 + 256 * u;
-      if (v >= sn.n) break;
-      const int32_t j = sn.pos(int32_t(v));
-      const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
-      if (!sl.ok) continue;
-      float* at = a.wp + ((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot;
-      float w = 0.f;
-      for (int h = 0; h < a.G; ++h)
-        w += z[h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.scores[(row0 + h) * a.nv + v] - z[h]);
-      *at = (a.kn && j == len - 1 ? 0.f : *at) + w;
-    }
+    for (int h = 0; h < kMaxG; ++h) s[h] = h < a.G ? a.scores[(row0 + h) * a.nv + v] : 0.f;
+    if (!sl.ok) continue;
+    float* at = a.wp + ((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot;
+    const float w = a.kn && j == len - 1 ? 0.f : *at;
+    float y = 0.f;
+#pragma unroll
+    for (int h = 0; h < kMaxG; ++h)
+      if (h < a.G && z[h] != -INFINITY) y += __builtin_amdgcn_exp2f(s[h] - z[h]);
+    *at = w + y;
   }
 }
 
@@ -866,8 +869,8 @@ hipError_t decode_t(const PagedArgs& a, int64_t keys, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.scores) {
-    const int64_t chunks = std::min<int64_t>((keys + 1023) / 1024, 65535);
-    join_weights<T, D><<<dim3(a.B * a.Hkv, uint32_t(chunks)), 256, 0, stream>>>(a);
+    const int64_t chunks = std::min<int64_t>((keys + 255) / 256, 32768);
+    join_weights<T, D><<<dim3(a.B * a.Hkv, uint32_t(a.G + chunks)), 256, 0, stream>>>(a);
   } else if (a.npiece > 1) {
     paged_join<T, D><<<uint32_t(a.B * a.Hq), 256, 0, stream>>>(a, 0);
   }
