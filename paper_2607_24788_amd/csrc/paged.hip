@@ -1,6 +1,7 @@
 // Softmax attention over a paged key-value cache: sliding window, sinks,
 // grouped query heads, pieces of long rows joined, attention weights.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -71,8 +72,10 @@ __global__ __launch_bounds__(256) void paged_clear_weights(PagedArgs a, PagedSeq
 //   S^T = K Q^T (keys are the MFMA rows): a lane holds 8 scores of one row,
 //   already the right operand of O^T += V^T P^T with keys in the order
 //   4g + 0..3, 16 + 4g + 0..3; V goes through LDS for its columns.
-template <typename T, int D, bool DECODE>
-__global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, PagedSeqs s) {
+struct NoSeqs {};
+template <typename T, int D, typename Seqs>  // Seqs: PagedSeqs, or NoSeqs for a decode call
+__global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
+  constexpr bool DECODE = std::is_same<Seqs, NoSeqs>::value;
   constexpr int KK = D / 32, CT = D / 16, ES = int(sizeof(T));
   // LDS rows: 32 bytes longer in bf16 (eight consecutive K rows' pieces, and
   // four V rows' 32-byte segments, in different banks), 16 in fp32 (V alone)
@@ -495,7 +498,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 #pragma unroll
     for (int e = 0; e < NI; ++e) {
       const int32_t rr = RPI * e + srow;
-      const bool see = (rr >= lo && rr < hi) || rr < sk;
+      const bool see = ((rr >= lo) & (rr < hi)) | (rr < sk);
       st.k[e] = bload16(kr, see ? koff[e] : kOOB);
       st.v[e] = bload16(vr, see ? voff[e] : kOOB);
     }
@@ -525,17 +528,36 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   auto compute = [&](const char* buf, int32_t i, uint32_t okp) {
     const int32_t k0 = key0(i);
     if (k0 > tw1 || (k0 + kTileKeys <= tw0 - a.W + 1 && k0 >= a.ns)) return;  // nothing for this wave
+    __builtin_amdgcn_s_setprio(1);
     f32x16_t sc[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[t][e] = 0.f;
+    }
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
         const uint4 kf = *reinterpret_cast<const uint4*>(buf + klane + 32 * t * RB + (((2 * kk) ^ ksw) << 4));
         sc[t] = mma32(kf, qf[kk], sc[t]);
       }
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int u = 0; u < KK - 3; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+    __builtin_amdgcn_s_setprio(0);
+    auto vfrag = [&](int sl, int ct) {
+      const char* p = buf + vlane + 16 * sl * RB + (((4 * ct) ^ vsw) << 4);
+      const char* p2 = buf + vlane + (16 * sl + 8) * RB + (((4 * ct) ^ vsw ^ 2) << 4);
+      return vt_frag(p, p2);
+    };
+    uint4 vf[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vf[ct] = vfrag(0, ct);
     const bool full = okp == 15u && k0 + kTileKeys - 1 <= tw0 && (k0 > tw1 - a.W || k0 + kTileKeys <= a.ns);
     if (!full) {
 #pragma unroll
@@ -543,7 +565,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int32_t j = k0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
-          const bool see = j <= tr && (j > tr - a.W || j < a.ns) && ((okp >> (2 * t + (e >> 3))) & 1);
+          const bool see = (j <= tr) & ((j > tr - a.W) | (j < a.ns)) & (((okp >> (2 * t + (e >> 3))) & 1) != 0);
           sc[t][e] = see ? sc[t][e] : -INFINITY;
         }
     }
@@ -563,28 +585,35 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[ct][e] *= f;
     }
-    uint4 pf[4];
+    // P V by 16-key slabs: under a slab's MFMAs the next slab's weights are
+    // taken and its V fragments read, in an order that the compiler keeps
+    auto weights2 = [&](int sl, int e) {  // elements e, e + 1 of slab sl, as a bf16 pair
+      float x = sc[sl >> 1][8 * (sl & 1) + e], y = sc[sl >> 1][8 * (sl & 1) + e + 1];
+      x = __builtin_amdgcn_exp2f(fmaf(x, c, -mc));
+      y = __builtin_amdgcn_exp2f(fmaf(y, c, -mc));
+      l += x;
+      l += y;
+      return pack_bf16x2(x, y);
+    };
+    uint32_t pw[4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int e = 0; e < 4; ++e) pw[e] = weights2(0, 2 * e);
+    uint4 pf = make_uint4(pw[0], pw[1], pw[2], pw[3]);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        sc[t][e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e], c, -mc));
-        l += sc[t][e];
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        pf[2 * t + u] = make_uint4(pack_bf16x2(sc[t][8 * u], sc[t][8 * u + 1]), pack_bf16x2(sc[t][8 * u + 2], sc[t][8 * u + 3]),
-                                   pack_bf16x2(sc[t][8 * u + 4], sc[t][8 * u + 5]),
-                                   pack_bf16x2(sc[t][8 * u + 6], sc[t][8 * u + 7]));
-    }
-#pragma unroll
-    for (int sl = 0; sl < 4; ++sl)
+    for (int sl = 0; sl < 4; ++sl) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        const char* p = buf + vlane + 16 * sl * RB + (((4 * ct) ^ vsw) << 4);
-        const char* p2 = buf + vlane + (16 * sl + 8) * RB + (((4 * ct) ^ vsw ^ 2) << 4);
-        o[ct] = mma32(vt_frag(p, p2), pf[sl], o[ct]);
+        __builtin_amdgcn_sched_barrier(0);
+        o[ct] = mma32(vf[ct], pf, o[ct]);
+        if (sl < 3) {
+          vf[ct] = vfrag(sl + 1, ct);
+#pragma unroll
+          for (int e = 0; e < 4 / CT; ++e) pw[ct * (4 / CT) + e] = weights2(sl + 1, 2 * (ct * (4 / CT) + e));
+        }
       }
+      pf = make_uint4(pw[0], pw[1], pw[2], pw[3]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   if (i0 < i1) {
@@ -864,8 +893,7 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
 
 template <typename T, int D>
 hipError_t decode_t(const PagedArgs& a, int64_t keys, hipStream_t stream) {
-  static const PagedSeqs none = {};
-  attend_rows<T, D, true><<<dim3(a.B * a.Hkv, a.npiece), 256, 0, stream>>>(a, none);
+  attend_rows<T, D, NoSeqs><<<dim3(a.B * a.Hkv, a.npiece), 256, 0, stream>>>(a, NoSeqs());
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.scores) {
@@ -884,9 +912,9 @@ hipError_t prefill_t(const PagedArgs& a, const PagedSeqs& s, int tile_rows, hipS
   const dim3 grid(uint32_t(tiles * a.Hkv), a.npiece);
   if constexpr (sizeof(T) == 2) {
     if (tile_rows == kTileRows) attend_tiles<D><<<grid, 256, 0, stream>>>(a, s);
-    else attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, s);
+    else attend_rows<T, D, PagedSeqs><<<grid, 256, 0, stream>>>(a, s);
   } else {
-    attend_rows<T, D, false><<<grid, 256, 0, stream>>>(a, s);
+    attend_rows<T, D, PagedSeqs><<<grid, 256, 0, stream>>>(a, s);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.npiece == 1) return e;

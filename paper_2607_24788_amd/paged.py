@@ -13,23 +13,23 @@ import torch
 from . import glide
 
 FULL = 1 << 30   # a window that never ends: causal softmax attention
-_PTR = ctypes.c_void_p
 
 
 def _tensor(name, t, device, dtype, numel):
     """Refuse what the library cannot see to be wrong: not a contiguous tensor
-    of the cache's device and the expected type with `numel` elements or more."""
+    of the cache's device (its index) and the expected type with `numel`
+    elements or more.  Returns its address."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    if t.get_device() == device and t.dtype is dtype and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.numel() < numel:
-        raise ValueError(f"{name} holds {t.numel()} elements, at least {numel} needed")
-    return t.data_ptr()
+    raise ValueError(f"{name} holds {t.numel()} elements, at least {numel} needed")
 
 
 class PagedCache:
@@ -40,6 +40,7 @@ class PagedCache:
         self.k_pool, self.v_pool, self.weights = k_pool, v_pool, weights
         self.block_table, self.lens = block_table, lens
         self.device = k_pool.device
+        self._dev = k_pool.get_device()
         self._arg = arg
         self._ref = ctypes.byref(arg)
 
@@ -65,6 +66,7 @@ class Paged:
         self.cfg = glide.PagedConfig(batch, n_q_heads, n_kv_heads, head_dim, code, page_size, n_pages, max_pages,
                                      window, n_sinks, float(sm_scale))
         self._ref = ctypes.byref(self.cfg)
+        self._cu = ctypes.c_int32 * (batch + 1)
         self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = batch, n_q_heads, n_kv_heads, head_dim
         self.page_size, self.n_pages, self.max_pages = page_size, n_pages, max_pages
         self.window, self.n_sinks, self.sm_scale, self.torch_dtype = window, n_sinks, float(sm_scale), dtype
@@ -111,7 +113,7 @@ class Paged:
                 strides[i], span = stride, stride * (shape[i] - 1) + span
         if v_pool.device != k_pool.device:
             raise ValueError("k_pool and v_pool are on different devices")
-        dev = k_pool.device
+        dev = k_pool.get_device()
         arg.k, arg.v = k_pool.data_ptr(), v_pool.data_ptr()
         arg.block_table = _tensor("block_table", block_table, dev, torch.int32, self.batch * self.max_pages)
         arg.lens = _tensor("lens", lens, dev, torch.int32, self.batch)
@@ -128,7 +130,7 @@ class Paged:
         """Pointers of a call over T rows of queries, checked."""
         if not isinstance(cache, PagedCache):
             raise ValueError("cache must come from Paged.cache")
-        dev, dt = cache.device, self.torch_dtype
+        dev, dt = cache._dev, self.torch_dtype
         nq, nkv = T * self.n_q_heads * self.head_dim, T * self.n_kv_heads * self.head_dim
         if (k is None) != (v is None):
             raise ValueError("k and v go together")
@@ -137,16 +139,15 @@ class Paged:
                 None if lse is None else _tensor("lse", lse, dev, torch.float32, T * self.n_q_heads))
 
     def _workspace(self, cache, workspace):
-        return _tensor("workspace", workspace, cache.device, torch.uint8, 0), workspace.numel()
+        return _tensor("workspace", workspace, cache._dev, torch.uint8, 0), workspace.numel()
 
     def _call(self, name, cache, stream, *args):
-        dev = cache.device
-        if dev.index != torch.cuda.current_device():
+        dev = cache._dev
+        if dev != torch.cuda.current_device():
             with torch.cuda.device(dev):
                 return self._call(name, cache, stream, *args)
-        if stream is None:
-            stream = torch.cuda.current_stream(dev)
-        s = getattr(self.lib, name)(self._ref, cache._ref, *args, stream.cuda_stream)
+        stream = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+        s = getattr(self.lib, name)(self._ref, cache._ref, *args, stream)
         if s:
             raise glide.GlideError(s, name, self.lib)
 
@@ -155,14 +156,14 @@ class Paged:
         """Append k, v (if given) and read out one row per token and head.
         q, out [T][Hq][d], k, v [T][Hkv][d], lse [T][Hq] fp32; the weights of
         the last n_observe queries of every sequence are added up."""
-        cu = [int(x) for x in cu_seqlens]
+        cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
         if n_observe and cache.weights is None:
             raise ValueError("n_observe needs a cache with weights")
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_prefill", cache, stream, qp, kp, vp, (ctypes.c_int32 * len(cu))(*cu), cu[-1],
+        self._call("glide_paged_prefill", cache, stream, qp, kp, vp, self._cu(*cu), cu[-1],
                    int(n_observe), int(max_len), op, lp, ws, n)
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
@@ -180,7 +181,7 @@ class Paged:
             raise ValueError("cache must come from Paged.cache")
         if cache.weights is None:
             raise ValueError("evict needs a cache with weights")
-        dev = cache.device
+        dev = cache._dev
         kp = _tensor("kept", kept, dev, torch.int32, self.batch * self.n_kv_heads * max(int(budget), 0))
         lp = _tensor("new_lens", new_lens, dev, torch.int32, self.batch)
         dp = None
