@@ -35,7 +35,7 @@ constexpr int kPagedMaxPieces = 256;
 constexpr int64_t kMaxRecords = 131072;
 
 struct PagedArgs {
-  const char *q, *kn, *vn;  // queries; new rows of a decode call (NULL: in the cache)
+  const char *q, *kn, *vn;  // queries; the call's new rows (NULL: in the cache)
   char* out;
   float* lse;               // natural log; NULL: not asked for
   char *kp, *vp;
@@ -74,8 +74,6 @@ struct EvictArgs {
   int32_t *kept, *new_lens;
 };
 
-hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const void* k, const void* v, int d, int dtype,
-                               hipStream_t stream);
 // keys: visible tokens of a sequence, at most (it sizes a grid only)
 hipError_t launch_paged_decode(const PagedArgs& a, int64_t keys, int d, int dtype, hipStream_t stream);
 // tile_rows: kPagedRows (attend_rows) or kTileRows (attend_tiles, bf16 only)

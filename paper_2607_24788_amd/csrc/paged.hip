@@ -32,38 +32,29 @@ __device__ __forceinline__ int32_t seq_len(const PagedArgs& a, int b) {
 }
 
 // ---------------------------------------------------------------------------
-// New rows into their pages: one 16-byte piece of K and of V per thread; the
-// weights of new tokens start from 0.  Copies; bound by launch and memory.
-template <int ROW>  // bytes of a row
-__global__ __launch_bounds__(256) void paged_append(PagedArgs a, PagedSeqs s, const char* k, const char* v) {
-  constexpr int P = ROW / 16;
-  const int i = blockIdx.y;  // sequence of the launch
-  const int b = s.seq0 + i;
-  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t n = int64_t(s.len[i]) * a.Hkv * P;
-  if (x >= n) return;
-  const int c = int(x % P);
-  const int64_t row = x / P;  // token, head
-  const int g = int(row % a.Hkv);
-  const int32_t j = seq_len(a, b) - s.len[i] + int32_t(row / a.Hkv);
-  if (j < 0) return;
-  const Slot sl = paged_slot(a.table + int64_t(b) * a.max_pages, j, a.shift, a.n_pages);
-  if (!sl.ok) return;
-  const int64_t src = (int64_t(s.start[i]) * a.Hkv + row) * ROW + c * 16;
-  *reinterpret_cast<uint4*>(a.kp + slot_offset(a.ks, sl, g) + c * 16) = *reinterpret_cast<const uint4*>(k + src);
-  *reinterpret_cast<uint4*>(a.vp + slot_offset(a.vs, sl, g) + c * 16) = *reinterpret_cast<const uint4*>(v + src);
+// A call's new rows of one KV head, tokens i0 <= i < i1 of a sequence, into
+// their pages, by the workgroup whose row tile has their first head; the
+// attention itself reads them where the call gave them.  Their weights start
+// from 0.
+template <int RB>  // bytes of a row
+__device__ __forceinline__ void append_rows(const PagedArgs& a, const int32_t* trow, int g, int64_t tok0, int32_t p0,
+                                            int32_t i0, int32_t i1) {
+  constexpr int P = RB / 16;
+  const int c = (threadIdx.x % P) * 16;
+  for (int32_t i = i0 + int32_t(threadIdx.x / P); i < i1; i += 256 / P) {
+    const int32_t j = p0 + i;
+    if (j < 0) continue;
+    const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+    if (!sl.ok) continue;
+    const int64_t src = ((tok0 + i) * a.Hkv + g) * RB + c;
+    const uint4 k = gload16<false>((gptr_t)a.kn + src), v = gload16<false>((gptr_t)a.vn + src);
+    *reinterpret_cast<uint4*>(a.kp + slot_offset(a.ks, sl, g) + c) = k;
+    *reinterpret_cast<uint4*>(a.vp + slot_offset(a.vs, sl, g) + c) = v;
+    if (a.wp && c == 0) a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] = 0.f;
+  }
 }
-
-__global__ __launch_bounds__(256) void paged_clear_weights(PagedArgs a, PagedSeqs s) {
-  const int i = blockIdx.y, b = s.seq0 + i;
-  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (x >= int64_t(s.len[i]) * a.Hkv) return;
-  const int g = int(x % a.Hkv);
-  const int32_t j = seq_len(a, b) - s.len[i] + int32_t(x / a.Hkv);
-  if (j < 0) return;
-  const Slot sl = paged_slot(a.table + int64_t(b) * a.max_pages, j, a.shift, a.n_pages);
-  if (sl.ok) a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] = 0.f;
-}
+// The tokens whose first head is in rows [r0, r0 + n) of a tile.
+__device__ __forceinline__ int32_t first_token(int r0, int G) { return (r0 + G - 1) / G; }
 
 // ---------------------------------------------------------------------------
 // Attention of one tile of 16 rows ((token, head) pairs of one KV head) over
@@ -133,16 +124,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
   for (int ct = 0; ct < CT; ++ct) acc[ct] = zero4();
   T* vt = vlds[wave];
 
-  if constexpr (DECODE) {
-    // the new token's rows into their page
-    if (a.kn && blockIdx.y == 0 && len > 0 && threadIdx.x < 2 * D * ES / 16) {
-      const Slot sl = paged_slot(trow, len - 1, a.shift, a.n_pages);
-      const int c = (threadIdx.x % (D * ES / 16)) * 16;
-      const bool val = threadIdx.x >= D * ES / 16;
-      const uint4 x = *reinterpret_cast<const uint4*>((val ? a.vn : a.kn) + (int64_t(b) * a.Hkv + g) * D * ES + c);
-      if (sl.ok)
-        *reinterpret_cast<uint4*>((val ? a.vp + slot_offset(a.vs, sl, g) : a.kp + slot_offset(a.ks, sl, g)) + c) = x;
-    }
+  if (a.kn && blockIdx.y == 0) {
+    const int32_t end = first_token(r0 + kPagedRows, a.G);
+    append_rows<D * ES>(a, trow, g, tok0, p0, first_token(r0, a.G), end < ntok ? end : ntok);
   }
 
   // Tiles are read one ahead: a tile's rows are asked for as soon as the one
@@ -169,11 +153,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
     const Slot sl = {page, j & ((1 << a.shift) - 1), true};
     *kr = good ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : zr;
     *vr = good ? (gptr_t)a.vp + slot_offset(a.vs, sl, g) : zr;
-    if constexpr (DECODE) {
-      if (a.kn && good && j == len - 1) {
-        *kr = (gptr_t)a.kn + (int64_t(b) * a.Hkv + g) * D * ES;
-        *vr = (gptr_t)a.vn + (int64_t(b) * a.Hkv + g) * D * ES;
-      }
+    if (a.kn && good && j >= p0) {
+      const int64_t at = ((tok0 + j - p0) * a.Hkv + g) * (D * ES);
+      *kr = (gptr_t)a.kn + at;
+      *vr = (gptr_t)a.vn + at;
     }
   };
   Frag<T> kf[2][KK], vf[2][KK];  // bf16: NL pieces each, [0] and [1] in turn
@@ -402,6 +385,11 @@ __device__ __forceinline__ int32_t table_at(const int32_t* row, int32_t i) {
   return ((cptr)(uintptr_t)row)[i];
 }
 
+// At a scalar offset more (which the check against the size counts too).
+__device__ __forceinline__ uint4 bload16_at(brsrc_t r, uint32_t off, int32_t at) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, off, at, 0));
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s) {
   constexpr int KK = D / 16, CT = D / 32, RB = 2 * D, LPR = RB / 16, RPI = 64 / LPR, NI = 16 / RPI;
@@ -462,12 +450,13 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 
   // staging: row 16 wave + RPI i + lane / LPR of a tile, piece lane % LPR
   const int srow = lane / LPR;
-  uint32_t koff[NI], voff[NI];
+  uint32_t koff[NI], voff[NI], noff[NI];  // in the pools, and among the call's new rows
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int rr = RPI * i + srow, piece = (lane % LPR) ^ swz<D>(rr);
     koff[i] = uint32_t(rr) * uint32_t(a.ks[2]) + piece * 16;
     voff[i] = uint32_t(rr) * uint32_t(a.vs[2]) + piece * 16;
+    noff[i] = uint32_t(rr) * uint32_t(a.Hkv * RB) + piece * 16;
   }
   struct Stage {
     uint4 k[NI], v[NI];
@@ -486,21 +475,47 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
     return x;
   };
+  // this sequence's new rows of the head, where the call gave them
+  const int64_t nat = (int64_t(s.start[si]) * a.Hkv + g) * RB;
+  const brsrc_t nkr = make_rsrc(a.kn + nat, kOOB), nvr = make_rsrc(a.vn + nat, kOOB);
+  const int32_t new0 = a.kn ? p0 : 0x7fffffff;  // their first position
   auto fetch = [&](int32_t i, const Pages& pg, Stage& st) {
     const int32_t k0 = key0(i) + 16 * wave;
     const int32_t page = wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3];
     const bool ok = uint32_t(page) < uint32_t(a.n_pages);
-    const int64_t slot = k0 & ((1 << a.shift) - 1), pp = ok ? page : 0;
-    const brsrc_t kr = make_rsrc(a.kp + pp * a.ks[0] + g * a.ks[1] + slot * a.ks[2], ok ? kOOB : 0);
-    const brsrc_t vr = make_rsrc(a.vp + pp * a.vs[0] + g * a.vs[1] + slot * a.vs[2], ok ? kOOB : 0);
-    // rows that none of the workgroup's queries sees are read as zeros
+    // rows that some query of the workgroup sees: [lo, hi) of the 16, and those before sk
     const int32_t lo = wstart - k0, hi = t1 + 1 - k0, sk = (a.ns < t1 + 1 ? a.ns : t1 + 1) - k0;
+    const bool whole = ok && ((lo <= 0 && hi >= 16) || sk >= 16);
+    if (whole && k0 >= new0) {
+      const int32_t at = (k0 - p0) * a.Hkv * RB;
+#pragma unroll
+      for (int e = 0; e < NI; ++e) {
+        st.k[e] = bload16_at(nkr, noff[e], at);
+        st.v[e] = bload16_at(nvr, noff[e], at);
+      }
+      return;
+    }
+    const int64_t slot = k0 & ((1 << a.shift) - 1), pp = ok ? page : 0;
+    const brsrc_t kr = make_rsrc(a.kp + pp * a.ks[0] + g * a.ks[1] + slot * a.ks[2], kOOB);
+    const brsrc_t vr = make_rsrc(a.vp + pp * a.vs[0] + g * a.vs[1] + slot * a.vs[2], kOOB);
+    if (whole && new0 - k0 >= 16) {
+#pragma unroll
+      for (int e = 0; e < NI; ++e) {
+        st.k[e] = bload16(kr, koff[e]);
+        st.v[e] = bload16(vr, voff[e]);
+      }
+      return;
+    }
+    // row by row: from the pools, or among the new, or (not seen by any) zeros
 #pragma unroll
     for (int e = 0; e < NI; ++e) {
       const int32_t rr = RPI * e + srow;
-      const bool see = ((rr >= lo) & (rr < hi)) | (rr < sk);
-      st.k[e] = bload16(kr, see ? koff[e] : kOOB);
-      st.v[e] = bload16(vr, see ? voff[e] : kOOB);
+      const bool see = ok & (((rr >= lo) & (rr < hi)) | (rr < sk)), fresh = k0 + rr >= new0;
+      const uint32_t off = (see & fresh) ? noff[e] + uint32_t((k0 - p0) * a.Hkv * RB) : kOOB;
+      const uint4 x = bload16(nkr, off), y = bload16(nvr, off);
+      const uint4 u = bload16(kr, (see & !fresh) ? koff[e] : kOOB), w = bload16(vr, (see & !fresh) ? voff[e] : kOOB);
+      st.k[e] = make_uint4(u.x | x.x, u.y | x.y, u.z | x.z, u.w | x.w);
+      st.v[e] = make_uint4(w.x | y.x, w.y | y.y, w.z | y.z, w.w | y.w);
     }
   };
   auto put = [&](char* buf, const Stage& st) {
@@ -615,6 +630,11 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
     __builtin_amdgcn_sched_barrier(0);
   };
+
+  if (a.kn && blockIdx.y == 0) {
+    const int32_t end = first_token(r0 + kTileRows, a.G);
+    append_rows<RB>(a, trow, g, s.start[si], p0, first_token(r0, a.G), end < ntok ? end : ntok);
+  }
 
   if (i0 < i1) {
     auto okbits = [&](const Pages& p) {
@@ -800,11 +820,6 @@ __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
   const Seen sn = seen_by(len - 1, len - 1, a.W, a.ns);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   const int32_t v0 = (blockIdx.y - a.G) * 256 + threadIdx.x;
-  // the appended token's weight starts from 0, also where it is not seen
-  if (a.kn && v0 == 0 && (sn.n == 0 || sn.pos(sn.n - 1) != len - 1)) {
-    const Slot sl = paged_slot(trow, len - 1, a.shift, a.n_pages);
-    if (sl.ok) a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] = 0.f;
-  }
 #pragma unroll 1
   for (int64_t v = v0; v < sn.n; v += int64_t(gridDim.y - a.G) * 256) {
     const int32_t j = sn.pos(int32_t(v));
@@ -814,7 +829,7 @@ __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
     for (int h = 0; h < kMaxG; ++h) s[h] = h < a.G ? a.scores[(row0 + h) * a.nv + v] : 0.f;
     if (!sl.ok) continue;
     float* at = a.wp + ((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot;
-    const float w = a.kn && j == len - 1 ? 0.f : *at;
+    const float w = *at;
     float y = 0.f;
 #pragma unroll
     for (int h = 0; h < kMaxG; ++h)
@@ -925,29 +940,6 @@ hipError_t prefill_t(const PagedArgs& a, const PagedSeqs& s, int tile_rows, hipS
 }
 
 }  // namespace
-
-hipError_t launch_paged_append(const PagedArgs& a, const PagedSeqs& s, const void* k, const void* v, int d, int dtype,
-                               hipStream_t stream) {
-  int32_t most = 0;
-  for (int i = 0; i < s.nseq; ++i) most = s.len[i] > most ? s.len[i] : most;
-  if (most == 0) return hipSuccess;
-  const int row = d * (dtype == GLIDE_BF16 ? 2 : 4);
-  if (k) {
-    const int64_t n = int64_t(most) * a.Hkv * (row / 16);
-    const dim3 grid(uint32_t((n + 255) / 256), s.nseq);
-    const char *kc = static_cast<const char*>(k), *vc = static_cast<const char*>(v);
-    if (row == 128) paged_append<128><<<grid, 256, 0, stream>>>(a, s, kc, vc);
-    else if (row == 256) paged_append<256><<<grid, 256, 0, stream>>>(a, s, kc, vc);
-    else paged_append<512><<<grid, 256, 0, stream>>>(a, s, kc, vc);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (k && a.wp) {
-    paged_clear_weights<<<dim3(uint32_t((int64_t(most) * a.Hkv + 255) / 256), s.nseq), 256, 0, stream>>>(a, s);
-    return hipGetLastError();
-  }
-  return hipSuccess;
-}
 
 hipError_t launch_paged_decode(const PagedArgs& a, int64_t keys, int d, int dtype, hipStream_t stream) {
   if (dtype == GLIDE_BF16)

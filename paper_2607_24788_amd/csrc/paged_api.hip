@@ -189,6 +189,8 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
   PagedArgs a;
   fill(cfg, cache, &a);
   a.q = static_cast<const char*>(q);
+  a.kn = static_cast<const char*>(k);
+  a.vn = static_cast<const char*>(v);
   a.out = static_cast<char*>(out);
   a.lse = lse;
   hipStream_t st = hipStream_t(stream);
@@ -217,8 +219,6 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
     a.ml = reinterpret_cast<float*>(ws + w.ml) - row0 * a.npiece * 2;
     a.lse2 = n_observe > 0 ? reinterpret_cast<float*>(ws + w.lse2) : nullptr;
     if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
-    s = hip_status(launch_paged_append(a, t, k, v, cfg->head_dim, cfg->dtype, st));
-    if (s != GLIDE_OK) return s;
     s = hip_status(launch_paged_prefill(a, t, cfg->head_dim, cfg->dtype, per_tile, st));
     if (s != GLIDE_OK) return s;
     if (n_observe > 0) {
