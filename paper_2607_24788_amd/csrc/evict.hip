@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   __shared__ uint32_t hist[kBins * kCopies];
   __shared__ uint32_t cnt[NC];
   __shared__ uint32_t wsum[kSelWaves], pick[2];
-  static_assert(NC <= kSelThreads, "a thread per count");
+  static_assert(NC <= kSelThreads && ROWS % 4 == 0, "a thread per count; loops take four rows at once");
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t len = seq_len(a, b);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
@@ -83,25 +83,26 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   for (int32_t j = tid; j < len - hi; j += kSelThreads) kept[lo + quota + j] = hi + j;
   if (quota == 0) return;
 
-  // keys of positions [j0, j0 + KEYS) to LDS, eight loads of a thread at once;
+  // keys of positions [j0, j0 + KEYS) to LDS, up to 16 loads of a thread at once;
   // the number of them
   auto load = [&](int32_t j0) {
     const int32_t n = hi - j0 < KEYS ? hi - j0 : KEYS;
-    for (int32_t i0 = 0; i0 < n; i0 += 8 * kSelThreads) {
-      int32_t page[8];
-      float w[8];
+    constexpr int U = ROWS < 16 ? ROWS : 16;
+    for (int32_t i0 = 0; i0 < n; i0 += U * kSelThreads) {
+      int32_t page[U];
+      float w[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int32_t i = i0 + u * kSelThreads + tid;
         page[u] = i < n ? trow[(j0 + i) >> a.shift] : -1;
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int32_t i = i0 + u * kSelThreads + tid;
         w[u] = uint32_t(page[u]) < uint32_t(a.n_pages) ? a.wp[weight_at(a, page[u], g, j0 + i)] : NAN;
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int32_t i = i0 + u * kSelThreads + tid;
         if (i < n) key[i] = weight_key(w[u]);
       }
@@ -122,10 +123,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
     __syncthreads();
     for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
       if (!once) n = load(j0);
-      for (int32_t i = tid; i < n; i += kSelThreads) {
-        const uint32_t k = key[i];
-        if (pass == 0 || ((k ^ thr) >> below) == 0)
-          atomicAdd(&hist[((k >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+      for (int32_t i0 = tid; i0 < n; i0 += 4 * kSelThreads) {
+        uint32_t k[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = key[i0 + u * kSelThreads];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i0 + u * kSelThreads < n && (pass == 0 || ((k[u] ^ thr) >> below) == 0))
+            atomicAdd(&hist[((k[u] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
       }
     }
     __syncthreads();
@@ -144,51 +149,52 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
     need = pick[1];
   }
 
-  int32_t at = lo;         // kept so far
-  uint32_t equal = 0;      // seen so far that are equal to thr
+  // In order: a key above thr stays, and of those equal to it the first
+  // `need`, so a kept key's place is the number above before it, and of the
+  // equal ones before it at most `need`.  Both counts go through one scan, a
+  // half of a word each (up to 32768).
+  int32_t above = 0, equal = 0;  // in the segments before
   const uint64_t lt = (uint64_t(1) << lane) - 1;
   for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
     if (!once) n = load(j0);
     const int rows = (n + kSelThreads - 1) / kSelThreads;
-    // keys equal to thr before each row of 64 positions
     __syncthreads();
-    for (int r = 0; r < rows; ++r) {
-      const int32_t i = r * kSelThreads + tid;
-      const uint64_t e = __ballot(i < n && key[i] == thr);
-      if (lane == 0) cnt[r * kSelWaves + wave] = __popcll(e);
+    for (int r0 = 0; r0 < rows; r0 += 4) {  // counts of each row of 64 positions
+      uint32_t k[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) k[u] = key[(r0 + u) * kSelThreads + tid];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool in = (r0 + u) * kSelThreads + tid < n;
+        const uint64_t e = __ballot(in && k[u] == thr), g2 = __ballot(in && k[u] > thr);
+        if (lane == 0) cnt[(r0 + u) * kSelWaves + wave] = uint32_t(__popcll(e)) << 16 | uint32_t(__popcll(g2));
+      }
     }
-    uint32_t all, kall;
+    uint32_t all;
     __syncthreads();
     const bool mine = tid < rows * kSelWaves;
-    const uint32_t eq0 = block_scan(mine ? cnt[tid] : 0, wsum, &all);
-    if (mine) cnt[tid] = eq0;
+    const uint32_t before = block_scan(mine ? cnt[tid] : 0, wsum, &all);
+    if (mine) cnt[tid] = before;
     __syncthreads();
-    // which stay: a bit per row of this thread's keys
-    uint32_t stay = 0;
-    for (int r = 0; r < rows; ++r) {
-      const int32_t i = r * kSelThreads + tid;
-      const uint32_t k = i < n ? key[i] : 0;
-      const bool eq = i < n && k == thr;
-      const uint64_t e = __ballot(eq);
-      const uint32_t rank = equal + cnt[r * kSelWaves + wave] + __popcll(e & lt);
-      if (i < n && (k > thr || (eq && rank < need))) stay |= 1u << r;
+    for (int r0 = 0; r0 < rows; r0 += 4) {
+      uint32_t k[4], c[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        k[u] = key[(r0 + u) * kSelThreads + tid];
+        c[u] = cnt[(r0 + u) * kSelWaves + wave];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int32_t i = (r0 + u) * kSelThreads + tid;
+        const bool eq = i < n && k[u] == thr, gt = i < n && k[u] > thr;
+        const uint64_t e = __ballot(eq), g2 = __ballot(gt);
+        const int32_t ne = equal + int32_t(c[u] >> 16) + __popcll(e & lt);
+        const int32_t ng = above + int32_t(c[u] & 0xffffu) + __popcll(g2 & lt);
+        if (gt || (eq && ne < int32_t(need))) kept[lo + ng + (ne < int32_t(need) ? ne : int32_t(need))] = j0 + i;
+      }
     }
-    __syncthreads();
-    for (int r = 0; r < rows; ++r) {
-      const uint64_t e = __ballot((stay >> r) & 1);
-      if (lane == 0) cnt[r * kSelWaves + wave] = __popcll(e);
-    }
-    __syncthreads();
-    const uint32_t k0 = block_scan(mine ? cnt[tid] : 0, wsum, &kall);
-    if (mine) cnt[tid] = k0;
-    __syncthreads();
-    for (int r = 0; r < rows; ++r) {
-      const bool on = (stay >> r) & 1;
-      const uint64_t e = __ballot(on);
-      if (on) kept[at + cnt[r * kSelWaves + wave] + __popcll(e & lt)] = j0 + r * kSelThreads + tid;
-    }
-    at += kall;
-    equal += all;
+    equal += int32_t(all >> 16);
+    above += int32_t(all & 0xffffu);
   }
 }
 

@@ -839,11 +839,17 @@ __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
 }
 
 // Prefill: the last n_observe queries of each sequence.  A wave owns 32 keys
-// (in registers) and goes through the scored rows in order: no sum's order
-// depends on timing.
+// (their K fragments in registers) and goes through the scored rows in order,
+// 64 at a time through LDS: no sum's order depends on timing.  Bound by the
+// latency of its loads where few rows are scored, else by its products and
+// exponentials.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s, int n_observe) {
-  constexpr int KK = D / 32;
+  constexpr int KK = D / 32, ES = int(sizeof(T)), RS = D + 16 / ES, NB = 64;  // rows of a block
+  constexpr int P = D * ES / 16, NP = NB * P / 256;                           // 16-byte pieces of a row, of a thread
+  __shared__ __align__(16) T qs[NB * RS];
+  __shared__ float zs[NB];
+  __shared__ int32_t ts[NB];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, lg = lane >> 4;
   const int i = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, b = s.seq0 + i;
   const int32_t len = seq_len(a, b), ntok = s.len[i], p0 = len - ntok;
@@ -853,7 +859,19 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
   const int32_t t0 = p0 + first > 0 ? p0 + first : 0;
   const Seen sn = seen_by(t0, len - 1, a.W, a.ns);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
-  for (int32_t x = blockIdx.y * 128 + wave * 32; x < sn.n; x += int32_t(gridDim.y) * 128) {
+  const int32_t row0 = first * a.G, rows = obs * a.G;
+  uint4 st[NP];
+  auto fetch = [&](int32_t rb) {  // 64 rows of q
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+      const int32_t x = rb + (e * 256 + int(threadIdx.x)) / P, r = row0 + (x < rows ? x : rows - 1);
+      const int64_t orow = (int64_t(s.start[i]) + r / a.G) * a.Hq + g * a.G + r % a.G;
+      st[e] = gload16<false>((gptr_t)a.q + orow * (D * ES) + (threadIdx.x % P) * 16);
+    }
+  };
+  for (int32_t x0 = blockIdx.y * 128; x0 < sn.n; x0 += int32_t(gridDim.y) * 128) {
+    const int32_t x = x0 + wave * 32;
+    fetch(0);
     Frag<T> kf[2][KK];
     uint32_t ok[2];
 #pragma unroll
@@ -864,42 +882,60 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
       ok[t] = uint32_t(__ballot(sl.ok)) & 0xffffu;
       const gptr_t kr = sl.ok ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : (gptr_t)zero_row;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) gload_frag<false>(kf[t][kk], kr + (32 * kk + 8 * lg) * int(sizeof(T)));
+      for (int kk = 0; kk < KK; ++kk) gload_frag<false>(kf[t][kk], kr + (32 * kk + 8 * lg) * ES);
     }
+    // positions of this lane's keys; -1 (never seen): not there
+    int32_t j[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        j[t][e] = (ok[t] >> (4 * lg + e)) & 1 ? sn.pos(x + 16 * t + 4 * lg + e) : 0x7fffffff;
     float w[2][4] = {};
-    const int32_t rend = ntok * a.G;
-    for (int32_t rb = first * a.G; rb < rend; rb += 16) {
-      const bool rok = rb + n < rend;
-      const int32_t r = rok ? rb + n : rend - 1, tr = rok ? p0 + r / a.G : -1;
-      const int64_t orow = (int64_t(s.start[i]) + r / a.G) * a.Hq + g * a.G + r % a.G;
-      const float z = a.lse2[orow];
-      Frag<T> qf[KK];
+    for (int32_t rb = 0; rb < rows; rb += NB) {
+      __syncthreads();  // the block before is read
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[kk].load(reinterpret_cast<const T*>(a.q) + orow * D + 32 * kk + 8 * lg);
-      f32x4_t sc[2] = {zero4(), zero4()};
+      for (int e = 0; e < NP; ++e) {
+        const int at = e * 256 + int(threadIdx.x);
+        *reinterpret_cast<uint4*>(reinterpret_cast<char*>(qs + (at / P) * RS) + (at % P) * 16) = st[e];
+      }
+      if (threadIdx.x < NB) {
+        const int32_t y = rb + int(threadIdx.x), r = row0 + (y < rows ? y : rows - 1);
+        const float z = a.lse2[(int64_t(s.start[i]) + r / a.G) * a.Hq + g * a.G + r % a.G];
+        zs[threadIdx.x] = z;
+        ts[threadIdx.x] = y < rows && z != -INFINITY ? p0 + r / a.G : -1;  // -1: sees nothing
+      }
+      __syncthreads();
+      if (rb + NB < rows) fetch(rb + NB);
+      const int tiles = (rows - rb < NB ? rows - rb + 15 : NB) / 16;
+      for (int rt = 0; rt < tiles; ++rt) {
+        f32x4_t sc[2] = {zero4(), zero4()};
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int kk = 0; kk < KK; ++kk) {
+          Frag<T> qf;
+          qf.load(qs + (16 * rt + n) * RS + 32 * kk + 8 * lg);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = 4 * lg + e;
-          const int32_t j = sn.pos(x + 16 * t + key);
-          const bool see = ((ok[t] >> key) & 1) && j <= tr && (j > tr - a.W || j < a.ns) && z != -INFINITY;
-          w[t][e] += see ? __builtin_amdgcn_exp2f(sc[t][e] * a.scale - z) : 0.f;
+          for (int t = 0; t < 2; ++t) sc[t] = mma(kf[t][kk], qf, sc[t]);
         }
+        const float z = zs[16 * rt + n];
+        const int32_t tr = ts[16 * rt + n];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool see = (j[t][e] <= tr) & ((j[t][e] > tr - a.W) | (j[t][e] < a.ns));
+            const float y = __builtin_amdgcn_exp2f(sc[t][e] * a.scale - z);
+            w[t][e] += see ? y : 0.f;
+          }
+      }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float y = dpp_sum_rows<16>(w[t][e]);
-        const int key = 4 * lg + e;
-        const int32_t vi = x + 16 * t + key;
-        if (n == 0 && vi < sn.n && ((ok[t] >> key) & 1)) {
-          const Slot sl = paged_slot(trow, sn.pos(vi), a.shift, a.n_pages);
+        if (n == 0 && j[t][e] != 0x7fffffff) {
+          const Slot sl = paged_slot(trow, j[t][e], a.shift, a.n_pages);
           a.wp[((int64_t(sl.page) * a.Hkv + g) << a.shift) + sl.slot] += y;
         }
       }
