@@ -24,27 +24,32 @@ __device__ __forceinline__ int64_t weight_at(const EvictArgs& a, int32_t page, i
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kBins = 2048, kCopies = 2;
 
+// Inclusive sum over the lanes of a wave: within rows of 16, then the rows'
+// last lanes (15 into rows 1 and 3, 31 into rows 2 and 3) to the rows behind.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_add(uint32_t x) {
+  return x + uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x = dpp_add<0x111, 0xf>(x);  // row_shr:1
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);     // row_bcast:15
+  return dpp_add<0x143, 0xc>(x);  // row_bcast:31
+}
 // Exclusive sum over the workgroup's threads; wsum: one entry per wave.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t inc = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t y = __shfl_up(inc, d);
-    if (lane >= d) inc += y;
-  }
+  const uint32_t inc = wave_scan(x);
   __syncthreads();
   if (lane == 63) wsum[wave] = inc;
   __syncthreads();
-  uint32_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) {
-    const uint32_t y = wsum[w];
-    before += w < wave ? y : 0;
-    all += y;
-  }
-  *total = all;
-  return before + inc - x;
+  // every wave sums the 16 waves' totals in its first row
+  const uint32_t w = wave_scan(wsum[lane & (kSelWaves - 1)]);
+  const uint32_t before = __builtin_amdgcn_readlane(w, wave ? wave - 1 : 0);
+  *total = __builtin_amdgcn_readlane(w, kSelWaves - 1);
+  return (wave ? before : 0) + inc - x;
 }
 
 // Which tokens stay, one workgroup per (sequence, KV head).  The need-th
