@@ -573,16 +573,31 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     uint4 vf[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) vf[ct] = vfrag(0, ct);
-    const bool full = okp == 15u && k0 + kTileKeys - 1 <= tw0 && (k0 > tw1 - a.W || k0 + kTileKeys <= a.ns);
-    if (!full) {
+    // what the rows do not see, where the tile may hold any (each kind tested
+    // for the wave; key 32t + 8(e/4) + e%4 of the lane's is an instruction's
+    // constant): keys after a row, keys before its window that are no sinks,
+    // groups of 16 whose page is not there
+    auto key_of = [](int t, int e) { return 32 * t + 8 * (e >> 2) + (e & 3); };
+    if (k0 + kTileKeys - 1 > tw0) {
+      const int32_t last = tr - k0 - 4 * h;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int32_t j = k0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
-          const bool see = (j <= tr) & ((j > tr - a.W) | (j < a.ns)) & (((okp >> (2 * t + (e >> 3))) & 1) != 0);
-          sc[t][e] = see ? sc[t][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) sc[t][e] = key_of(t, e) > last ? -INFINITY : sc[t][e];
+    }
+    if (k0 <= tw1 - a.W && k0 + kTileKeys > a.ns) {
+      const int32_t before = tr - a.W - k0 - 4 * h, sinks = a.ns - k0 - 4 * h;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          sc[t][e] = (key_of(t, e) <= before && key_of(t, e) >= sinks) ? -INFINITY : sc[t][e];
+    }
+    if (okp != 15u) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[t][e] = (okp >> (2 * t + (e >> 3))) & 1 ? sc[t][e] : -INFINITY;
     }
     float mx = sc[0][0];
 #pragma unroll
