@@ -24,15 +24,29 @@ constexpr int kPagedTile = 32;
 //  decode: pieces as short as one round allows (at least kPieceMin keys, a tile
 //    per wave); where one round would make them longer than kPieceLong there
 //    are several rounds, which even out ragged lengths.
-//  prefill: only where the row tiles do not fill a round, into pieces of at
-//    least kPiecePrefill keys (records of 16 or 128 rows each).
+//  prefill: by a model of the call (prefill_us).
 // The records of a call are at most kMaxRecords rows.
 constexpr int kPagedRound = 512;
 constexpr int kPieceMin = 128;
 constexpr int kPieceLong = 1024;
-constexpr int kPiecePrefill = 512;
 constexpr int kPagedMaxPieces = 256;
 constexpr int64_t kMaxRecords = 131072;
+
+// Microseconds of a prefill in n pieces per row tile, for choosing n: steps
+// (64 keys of attend_tiles, 128 of attend_rows) that a workgroup takes one
+// after another, 1.5 us each where it has a CU to itself and 2.1 where two
+// share it, in rounds; no less than K and V at 5 TB/s, drawn by as many
+// workgroups as the rounds hold on average; and the join, a launch and the
+// records written and read (8 bytes per row and element at 4 TB/s).
+// Measured: 16 tokens onto 500 (8 KV heads), one piece 19.5 us, four 12.1;
+// 1024 fresh tokens, two pieces 55 us, one 30; 3..9 tokens onto 32K (4
+// sequences), 23 pieces (1.4 rounds) 115 us, 16 (one) 100.
+inline double prefill_us(int64_t tiles, int64_t steps, int64_t n, int64_t rows, double kv_bytes, int d) {
+  const int64_t wgs = tiles * n, per = (steps + n - 1) / n, rounds = (wgs + kPagedRound - 1) / kPagedRound;
+  const double us = double(rounds * per) * (wgs <= kPagedRound / 2 ? 1.5 : 2.1);
+  const double mem = kv_bytes / 5e6 * double(rounds * kPagedRound) / wgs;
+  return (us > mem ? us : mem) + (n > 1 ? 4 + double(rows) * n * (d + 2) * 8 / 4e6 : 0);
+}
 
 struct PagedArgs {
   const char *q, *kn, *vn;  // queries; the call's new rows (NULL: in the cache)

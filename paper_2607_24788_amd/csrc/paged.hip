@@ -721,7 +721,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
 }
 
-// The pieces of a row joined by a workgroup: a wave's lanes take the pieces'
+// The pieces of a row joined: a wave's lanes take the pieces'
 // frames and sums (npiece <= 256, four each).  Bound by latency.
 struct Joined {
   float M, L;
@@ -758,20 +758,20 @@ __device__ __forceinline__ float log2_sum(const Joined& j) {
   return j.L > 0.f ? j.M + __builtin_amdgcn_logf(j.L) : j.L == 0.f ? -INFINITY : j.L;
 }
 
-// Row r's output by the workgroup: its four waves take every fourth piece,
-// eight records at a time; wave 0 adds their sums up in order.
-template <typename T, int D>
+// Row r's output by NW waves (a workgroup's four, or one): each takes every
+// NW-th piece, eight records at a time; their sums are added in order.
+template <typename T, int D, int NW>
 __device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Joined& j, const float* f,
                                          float (*part)[D]) {
   constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : threadIdx.x >> 6;
   const float* acc = a.acc + r * a.npiece * D + lane * E;
   float x[E] = {};
-  for (int i0 = wave; i0 < a.npiece; i0 += 32) {
+  for (int i0 = wave; i0 < a.npiece; i0 += 8 * NW) {
     float y[8][E], w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int p = i0 + 4 * i;
+      const int p = i0 + NW * i;
       const float fu = p < 64 ? f[0] : p < 128 ? f[1] : p < 192 ? f[2] : f[3];
       w[i] = p < a.npiece ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), p & 63)) : 0.f;
 #pragma unroll
@@ -782,29 +782,44 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Jo
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] += w[i] * y[i][e];
   }
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < E; ++e) part[wave][lane * E + e] = x[e];
-  __syncthreads();
   const float inv = j.L == 0.f ? 0.f : 1.f / j.L;
-  if (int(threadIdx.x) < D) {
-    const float y = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
-    reinterpret_cast<T*>(a.out)[r * D + threadIdx.x] = from_f32<T>(y * inv);
+  if constexpr (NW == 1) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) reinterpret_cast<T*>(a.out)[r * D + lane * E + e] = from_f32<T>(x[e] * inv);
+  } else {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[wave][lane * E + e] = x[e];
+    __syncthreads();
+    if (int(threadIdx.x) < D) {
+      const float y = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+      reinterpret_cast<T*>(a.out)[r * D + threadIdx.x] = from_f32<T>(y * inv);
+    }
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0 && wave == 0) {
     const float lse2 = log2_sum(j);
     if (a.lse) a.lse[r] = lse2 * kLn2;
     if (a.lse2) a.lse2[r] = lse2;
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0) {
+// NW waves per row: four where there are more than eight pieces (a wave's
+// loads at once), else one, and four rows per workgroup.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(256) void paged_join(PagedArgs a, int64_t row0, int64_t rows) {
   __shared__ float part[4][D];
-  const int64_t r = row0 + blockIdx.x;
+  int64_t r = int64_t(blockIdx.x) * (4 / NW);
+  if constexpr (NW == 1) r += threadIdx.x >> 6;
+  if (r >= rows) return;
   float f[kPagedMaxPieces / 64];
-  const Joined j = join_frames(a, r, f);
-  join_row<T, D>(a, r, j, f, part);
+  const Joined j = join_frames(a, row0 + r, f);
+  join_row<T, D, NW>(a, row0 + r, j, f, part);
+}
+template <typename T, int D>
+hipError_t join_t(const PagedArgs& a, int64_t row0, int64_t rows, hipStream_t stream) {
+  if (a.npiece > 8) paged_join<T, D, 4><<<uint32_t(rows), 256, 0, stream>>>(a, row0, rows);
+  else paged_join<T, D, 1><<<uint32_t((rows + 3) / 4), 256, 0, stream>>>(a, row0, rows);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
@@ -821,7 +836,7 @@ __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
   float f[kPagedMaxPieces / 64];
   if (int(blockIdx.y) < a.G) {
     const Joined j = join_frames(a, row0 + blockIdx.y, f);
-    join_row<T, D>(a, row0 + blockIdx.y, j, f, part);
+    join_row<T, D, 4>(a, row0 + blockIdx.y, j, f, part);
     return;
   }
 #pragma unroll 1
@@ -966,7 +981,7 @@ hipError_t decode_t(const PagedArgs& a, int64_t keys, hipStream_t stream) {
     const int64_t chunks = std::min<int64_t>((keys + 255) / 256, 32768);
     join_weights<T, D><<<dim3(a.B * a.Hkv, uint32_t(a.G + chunks)), 256, 0, stream>>>(a);
   } else if (a.npiece > 1) {
-    paged_join<T, D><<<uint32_t(a.B * a.Hq), 256, 0, stream>>>(a, 0);
+    return join_t<T, D>(a, 0, int64_t(a.B) * a.Hq, stream);
   }
   return hipGetLastError();
 }
@@ -986,8 +1001,7 @@ hipError_t prefill_t(const PagedArgs& a, const PagedSeqs& s, int tile_rows, hipS
   if (e != hipSuccess || a.npiece == 1) return e;
   const int64_t row0 = int64_t(s.start[0]) * a.Hq;
   const int64_t rows = (int64_t(s.start[s.nseq - 1]) + s.len[s.nseq - 1]) * a.Hq - row0;
-  paged_join<T, D><<<uint32_t(rows), 256, 0, stream>>>(a, row0);
-  return hipGetLastError();
+  return join_t<T, D>(a, row0, rows, stream);
 }
 
 }  // namespace

@@ -67,21 +67,33 @@ int64_t max_pieces(int64_t tiles, int rows) {
   return std::max<int64_t>(1, std::min<int64_t>(kPagedMaxPieces, kMaxRecords / (std::max<int64_t>(tiles, 1) * rows)));
 }
 
-// Pieces of each of `tiles` row tiles (see kPagedRound).  max_len only sizes
-// them: the kernels make pieces longer where rows see more.
-void plan_pieces(const glide_paged_config* c, int64_t tiles, int rows, bool decode, int64_t max_len, PagedArgs* a) {
-  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len));
-  tiles = std::max<int64_t>(tiles, 1);
-  int64_t n;
-  if (decode) {
-    const int64_t piece = std::min<int64_t>(kPieceLong, std::max<int64_t>(kPieceMin, tiles * keys / kPagedRound));
-    n = (keys + piece - 1) / piece;
-  } else {
-    n = std::min(kPagedRound / tiles, keys / kPiecePrefill);
-  }
-  n = std::max<int64_t>(1, std::min(n, max_pieces(tiles, rows)));
+// Pieces of each row tile (see kPagedRound).  max_len only sizes them: the
+// kernels make pieces longer where rows see more.
+void set_pieces(int64_t n, int64_t keys, PagedArgs* a) {
   a->npiece = int32_t(n);
   a->piece = int32_t(((keys + n - 1) / n + 127) / 128 * 128);
+}
+void plan_decode(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
+  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), units = int64_t(c->batch) * c->n_kv_heads;
+  const int64_t piece = std::min<int64_t>(kPieceLong, std::max<int64_t>(kPieceMin, units * keys / kPagedRound));
+  set_pieces(std::min((keys + piece - 1) / piece, max_pieces(units, kPagedRows)), keys, a);
+}
+void plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
+                  int64_t max_len, PagedArgs* a) {
+  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), step = tile_rows == kTileRows ? kTileKeys : 128;
+  const int64_t steps = (keys + step - 1) / step;
+  const double kv = 2.0 * nseq * c->n_kv_heads * double(keys) * c->head_dim * esize(c);
+  auto us = [&](int64_t m) { return prefill_us(tiles, steps, m, rows, kv, c->head_dim); };
+  int64_t n = 1;
+  double best = us(1);
+  for (int64_t m = 2; m <= std::min(steps, max_pieces(tiles, tile_rows)); ++m) {
+    const double x = us(m);
+    if (x < best) {
+      n = m;
+      best = x;
+    }
+  }
+  set_pieces(n, keys, a);
 }
 
 // Sections of the workspace of one call, in bytes from its start.
@@ -209,9 +221,9 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
       ++b1;
     }
     t.nseq = b1 - b0;
-    plan_pieces(cfg, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads, per_tile, false, max_len, &a);
     // records by the call's row number: a launch's own rows only
     const int64_t row0 = int64_t(cu[b0]) * cfg->n_q_heads, rows = int64_t(cu[b1]) * cfg->n_q_heads - row0;
+    plan_prefill(cfg, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads, per_tile, rows, t.nseq, max_len, &a);
     const Sections w = sections(cfg, total_tokens * cfg->n_q_heads, a.npiece > 1 ? rows * a.npiece : 0,
                                 n_observe > 0, false);
     char* ws = static_cast<char*>(workspace);
@@ -257,7 +269,7 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
   a.out = static_cast<char*>(out);
   a.lse = lse;
   const int64_t rows = int64_t(cfg->batch) * cfg->n_q_heads;
-  plan_pieces(cfg, int64_t(cfg->batch) * cfg->n_kv_heads, kPagedRows, true, max_len, &a);
+  plan_decode(cfg, max_len, &a);
   const Sections w = sections(cfg, rows, a.npiece > 1 || weights ? rows * a.npiece : 0, weights, true);
   if (size_t(w.bytes) > workspace_bytes) return GLIDE_ERR_SIZE;
   char* ws = static_cast<char*>(workspace);
