@@ -56,20 +56,23 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint3
 // largest key is found by its 11, 11 and 10 bits: a histogram in LDS of the
 // keys that agree so far (integer counts, so no order of atomics shows), then
 // the bin by a sum from the top.  Then every key above it stays, and the first
-// of those equal to it; ranks come from the waves' ballots in the order of
-// positions.  Keys are read once and kept in LDS up to KEYS tokens; longer
-// sequences go through LDS in segments, read again per pass.  Bound by the
-// latency of the reads and of two dozen barriers.  (Keys in registers, their
-// loops unrolled: 24 us at 8K tokens and 21 at 700, most of it the fetch of
-// the code.)
+// of those equal to it; ranks are counts before a key in the order of
+// positions.  Keys are read once and kept in LDS up to KEYS tokens, four
+// neighbours to a thread in the passes; longer sequences go through LDS in
+// segments, read again per pass.  Bound by the latency of the reads and of two
+// dozen barriers, and by the instructions of 16 waves on one CU.  (Keys in
+// registers, their loops unrolled: 24 us at 8K tokens and 21 at 700, most of
+// it the fetch of the code.)
 template <int KEYS>
 __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
-  constexpr int ROWS = KEYS / kSelThreads, NC = ROWS * kSelWaves;  // counts, one per 64 positions
-  __shared__ uint32_t key[KEYS];
+  constexpr int QUADS = KEYS / (4 * kSelThreads), NC = QUADS * kSelWaves;  // counts, one per 256 positions
+  constexpr int U = QUADS * 4 < 16 ? QUADS * 4 : 16;
+  __shared__ uint4 key4[KEYS / 4];
   __shared__ uint32_t hist[kBins * kCopies];
   __shared__ uint32_t cnt[NC];
   __shared__ uint32_t wsum[kSelWaves], pick[2];
-  static_assert(NC <= kSelThreads && ROWS % 4 == 0, "a thread per count; loops take four rows at once");
+  static_assert(NC <= kSelThreads, "a thread per count");
+  uint32_t* key = reinterpret_cast<uint32_t*>(key4);
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t len = seq_len(a, b);
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
@@ -88,12 +91,13 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   for (int32_t j = tid; j < len - hi; j += kSelThreads) kept[lo + quota + j] = hi + j;
   if (quota == 0) return;
 
-  // keys of positions [j0, j0 + KEYS) to LDS, up to 16 loads of a thread at once;
-  // the number of them
+  // Keys of positions [j0, j0 + KEYS) to LDS, up to 16 loads of a thread at
+  // once; the quads of a thread that hold any.  Behind the last key zeros, the
+  // smallest: at most equal to the threshold, and then behind every real one.
   auto load = [&](int32_t j0) {
-    const int32_t n = hi - j0 < KEYS ? hi - j0 : KEYS;
-    constexpr int U = ROWS < 16 ? ROWS : 16;
-    for (int32_t i0 = 0; i0 < n; i0 += U * kSelThreads) {
+    const int32_t n = hi - j0 < KEYS ? hi - j0 : KEYS, quads = (n + 4 * kSelThreads - 1) / (4 * kSelThreads);
+    __syncthreads();
+    for (int32_t i0 = 0; i0 < quads * 4 * kSelThreads; i0 += U * kSelThreads) {
       int32_t page[U];
       float w[U];
 #pragma unroll
@@ -107,17 +111,15 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
         w[u] = uint32_t(page[u]) < uint32_t(a.n_pages) ? a.wp[weight_at(a, page[u], g, j0 + i)] : NAN;
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int32_t i = i0 + u * kSelThreads + tid;
-        if (i < n) key[i] = weight_key(w[u]);
-      }
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * kSelThreads + tid < KEYS) key[i0 + u * kSelThreads + tid] = weight_key(w[u]);
     }
-    return n;
+    __syncthreads();
+    return quads;
   };
-  // (a thread reads back the keys that it wrote: no barrier between)
   const bool once = hi - lo <= KEYS;
-  int32_t n = 0;
-  if (once) n = load(lo);
+  int quads = 0;
+  if (once) quads = load(lo);
 
   uint32_t need = quota, thr = 0;
   int shift = 32;
@@ -127,15 +129,15 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
     for (int i = tid; i < kBins * kCopies; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
-      if (!once) n = load(j0);
-      for (int32_t i0 = tid; i0 < n; i0 += 4 * kSelThreads) {
-        uint32_t k[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = key[i0 + u * kSelThreads];
+      if (!once) quads = load(j0);
+      for (int r = 0; r < quads; ++r) {
+        const uint4 k = key4[r * kSelThreads + tid];
+        const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+        const int32_t left = hi - j0 - (r * kSelThreads + tid) * 4;  // (the zeros behind would all meet in one bin)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (i0 + u * kSelThreads < n && (pass == 0 || ((k[u] ^ thr) >> below) == 0))
-            atomicAdd(&hist[((k[u] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+          if (pass == 0 ? u < left : ((x[u] ^ thr) >> below) == 0)
+            atomicAdd(&hist[((x[u] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
       }
     }
     __syncthreads();
@@ -159,43 +161,39 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
   // equal ones before it at most `need`.  Both counts go through one scan, a
   // half of a word each (up to 32768).
   int32_t above = 0, equal = 0;  // in the segments before
-  const uint64_t lt = (uint64_t(1) << lane) - 1;
+  const int32_t most = int32_t(need);
   for (int32_t j0 = lo; j0 < hi; j0 += KEYS) {
-    if (!once) n = load(j0);
-    const int rows = (n + kSelThreads - 1) / kSelThreads;
+    if (!once) quads = load(j0);
+    uint32_t before[QUADS];  // within the wave's 256 positions
     __syncthreads();
-    for (int r0 = 0; r0 < rows; r0 += 4) {  // counts of each row of 64 positions
-      uint32_t k[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) k[u] = key[(r0 + u) * kSelThreads + tid];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const bool in = (r0 + u) * kSelThreads + tid < n;
-        const uint64_t e = __ballot(in && k[u] == thr), g2 = __ballot(in && k[u] > thr);
-        if (lane == 0) cnt[(r0 + u) * kSelWaves + wave] = uint32_t(__popcll(e)) << 16 | uint32_t(__popcll(g2));
-      }
+    for (int r = 0; r < QUADS; ++r) {
+      if (r >= quads) continue;
+      const uint4 k = key4[r * kSelThreads + tid];
+      const uint32_t e = (k.x == thr) + (k.y == thr) + (k.z == thr) + (k.w == thr);
+      const uint32_t x = e << 16 | ((k.x > thr) + (k.y > thr) + (k.z > thr) + (k.w > thr));
+      const uint32_t inc = wave_scan(x);
+      before[r] = inc - x;
+      if (lane == 63) cnt[r * kSelWaves + wave] = inc;
     }
     uint32_t all;
     __syncthreads();
-    const bool mine = tid < rows * kSelWaves;
-    const uint32_t before = block_scan(mine ? cnt[tid] : 0, wsum, &all);
-    if (mine) cnt[tid] = before;
+    const bool mine = tid < quads * kSelWaves;
+    const uint32_t sum = block_scan(mine ? cnt[tid] : 0, wsum, &all);
+    if (mine) cnt[tid] = sum;
     __syncthreads();
-    for (int r0 = 0; r0 < rows; r0 += 4) {
-      uint32_t k[4], c[4];
+#pragma unroll
+    for (int r = 0; r < QUADS; ++r) {
+      if (r >= quads) continue;
+      const uint4 k = key4[r * kSelThreads + tid];
+      const uint32_t x[4] = {k.x, k.y, k.z, k.w}, c = cnt[r * kSelWaves + wave] + before[r];
+      int32_t ne = equal + int32_t(c >> 16), ng = above + int32_t(c & 0xffffu);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        k[u] = key[(r0 + u) * kSelThreads + tid];
-        c[u] = cnt[(r0 + u) * kSelWaves + wave];
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int32_t i = (r0 + u) * kSelThreads + tid;
-        const bool eq = i < n && k[u] == thr, gt = i < n && k[u] > thr;
-        const uint64_t e = __ballot(eq), g2 = __ballot(gt);
-        const int32_t ne = equal + int32_t(c[u] >> 16) + __popcll(e & lt);
-        const int32_t ng = above + int32_t(c[u] & 0xffffu) + __popcll(g2 & lt);
-        if (gt || (eq && ne < int32_t(need))) kept[lo + ng + (ne < int32_t(need) ? ne : int32_t(need))] = j0 + i;
+        const bool gt = x[u] > thr, eq = x[u] == thr;
+        if (gt || (eq && ne < most)) kept[lo + ng + (ne < most ? ne : most)] = j0 + (r * kSelThreads + tid) * 4 + u;
+        ng += gt;
+        ne += eq;
       }
     }
     equal += int32_t(all >> 16);
