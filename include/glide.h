@@ -323,7 +323,8 @@ typedef struct {
  * [0, n_pages) is not allocated: its tokens are not visible and what is
  * written to them is dropped.  lens [B]: tokens cached, after the call's own
  * appends (taken as 0 below 0, as max_pages * page_size above it).  A page
- * that a call writes to belongs to one sequence. */
+ * that a call writes to (its new rows, weights that it adds to, rows that it
+ * moves) belongs to one sequence; pages that are only read may be shared. */
 typedef struct {
   void* k;                    /* K pool, cfg->dtype */
   void* v;                    /* V pool */
@@ -335,7 +336,8 @@ typedef struct {
 
 /* Workspace bytes that serve every glide_paged_* call of this config, prefills
  * up to max_total_tokens packed tokens; weights != 0: with cache->weights.  At
- * least 256; 0 if cfg is invalid.  Nothing in it need be cleared, and nothing
+ * least 256; 0 if cfg is invalid or max_total_tokens is not in [0, 2^31].
+ * Nothing in it need be cleared, and nothing
  * is kept in it from one call to the next; calls that overlap in time need
  * workspaces of their own. */
 size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_total_tokens, int32_t weights);
@@ -380,7 +382,7 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
  * largest weights (of equal weights the first; a NaN, and a token on a page
  * that is not allocated, counts as the smallest).  Their rows and weights
  * become tokens 0, 1, ... of the sequence in dst_table's pages.
- *   budget >= 1, budget >= n_sinks + n_recent;  n_recent >= 0
+ *   budget in [1, 2^30], budget >= n_sinks + n_recent;  n_recent >= 0
  *   dst_table  device [B][max_pages]; NULL: in place (block_table itself).
  *              Otherwise its pages of tokens 0 .. min(lens[b], budget) - 1
  *              are no pages of any sequence in block_table, which is left as

@@ -511,7 +511,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     for (int e = 0; e < NI; ++e) {
       const int32_t rr = RPI * e + srow;
       const bool see = ok & (((rr >= lo) & (rr < hi)) | (rr < sk)), fresh = k0 + rr >= new0;
-      const uint32_t off = (see & fresh) ? noff[e] + uint32_t((k0 - p0) * a.Hkv * RB) : kOOB;
+      const uint32_t off = (see & fresh) ? noff[e] + uint32_t(k0 - p0) * uint32_t(a.Hkv * RB) : kOOB;
       const uint4 x = bload16(nkr, off), y = bload16(nvr, off);
       const uint4 u = bload16(kr, (see & !fresh) ? koff[e] : kOOB), w = bload16(vr, (see & !fresh) ? voff[e] : kOOB);
       st.k[e] = make_uint4(u.x | x.x, u.y | x.y, u.z | x.z, u.w | x.w);

@@ -293,7 +293,7 @@ glide_status glide_paged_evict(const glide_paged_config* cfg, const glide_paged_
   if (!cache->weights || !kept || !new_lens || !workspace) return GLIDE_ERR_NULL;
   if (!aligned(dst_table, 4) || !aligned(kept, 4) || !aligned(new_lens, 4) || !aligned(workspace, 256))
     return GLIDE_ERR_ALIGN;
-  if (budget < 1 || n_recent < 0 || int64_t(budget) < int64_t(cfg->n_sinks) + n_recent) return GLIDE_ERR_INVALID;
+  if (budget < 1 || budget > kMaxPagedWindow || n_recent < 0 || int64_t(budget) < int64_t(cfg->n_sinks) + n_recent) return GLIDE_ERR_INVALID;
   if (workspace_bytes < 256) return GLIDE_ERR_SIZE;
   PagedArgs p;
   fill(cfg, cache, &p);

@@ -1,6 +1,7 @@
 """The paged softmax cache against its float64 definition (tests/paged_util.py):
 decode, prefill, attention weights, eviction, and all of them in a row."""
 import math
+import random
 
 import pytest
 import torch
@@ -166,6 +167,46 @@ PREFILL = [
 def test_prefill(i, dtype):
     B, Hq, Hkv, d, page, lens, new, W, ns, obs = PREFILL[i]
     run_prefill(Case(B, Hq, Hkv, d, page, lens, W, ns, dtype=dtype, weights=obs > 0, seed=50 + i), new, obs)
+
+
+@pytest.mark.parametrize("max_len", [1, 900, 1 << 20])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_prefill_length_hint_changes_no_result(dtype, max_len):
+    run_prefill(Case(2, 8, 2, 64, 16, [900, 700], 600, 4, dtype=dtype, weights=True, seed=69), [40, 9], 12,
+                max_len=max_len)
+
+
+def test_prefill_many_rows_in_pieces():
+    """Row tiles that do not fill the card over a long cache: each in pieces,
+    rows that begin and end inside tiles, new rows inside a group of 16."""
+    run_prefill(Case(1, 8, 1, 128, 64, [2777], None, 0, dtype=BF16, weights=True, seed=68), [100], 100, max_len=2777)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn(seed):
+    """Calls of every kind, drawn: sizes, windows, sinks, pages, missing pages."""
+    r = random.Random(1000 + seed)
+    dtype = r.choice([BF16, BF16, FP32])
+    Hkv, G, d = r.choice([1, 2, 3]), r.choice([1, 2, 3, 4, 7, 8]), r.choice([64, 128])
+    page = r.choice([1, 2, 8, 16, 16, 32, 64, 128])
+    B = r.randint(1, 4)
+    new = [r.choice([0, 1, 2, r.randint(1, 130)]) for _ in range(B)]
+    lens = [n + r.choice([0, 0, r.randint(0, 40), r.randint(0, 400)]) for n in new]
+    W = r.choice([None, 1, r.randint(1, 64), r.randint(1, 300), 0])
+    ns = r.choice([0, 1, 4, r.randint(1, 150)])
+    if W == 0 and ns == 0:
+        ns = 2
+    case = Case(B, Hkv * G, Hkv, d, page, lens, W, ns, dtype=dtype, weights=True, seed=200 + seed,
+                scale=r.choice([0.5, 1.0, 2.0]), order=r.choice(["hnd", "nhd", "joined"]))
+    if r.random() < 0.4 and case.table.shape[1] > 2:
+        case.table[r.randrange(B), r.randrange(case.table.shape[1] - 1)] = r.choice([-1, case.g.n_pages])
+        case.dev_table.copy_(case.table)
+    if sum(new):
+        run_prefill(case, new, r.choice([0, 1, 20, 1000]), append=r.random() < 0.7, max_len=r.choice([0, max(lens)]))
+    run_decode(case, r.random() < 0.7, r.choice([0, max(lens)]))
+    recent = r.randint(0, 30)
+    run_evict(case, min(ns, 200) + 1 + recent + r.randint(0, 60) if ns <= 200 else 400 + recent, recent,
+              alias=r.random() < 0.5)
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])

@@ -123,6 +123,8 @@ def test_ranges(lib):
     assert prefill(lib, cu=(0, 0, 1 << 21)) == UNSUPPORTED   # 2^21 tokens of 2 KiB
     assert evict(lib, budget=0, recent=0) == INVALID and evict(lib, recent=-1) == INVALID
     assert evict(lib, budget=11, recent=8) == INVALID        # 4 sinks and 8 newest do not fit
+    assert evict(lib, budget=(1 << 30) + 1) == INVALID
+    assert lib.glide_paged_workspace_bytes(ctypes.byref(cfg()), (1 << 31) + 1, 0) == 0
 
 
 def test_small_workspaces(lib):
