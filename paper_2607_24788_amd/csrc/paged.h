@@ -17,7 +17,9 @@ constexpr int kPagedRows = 16;
 // Rows of one workgroup of attend_tiles (four waves of 32), keys of its tiles.
 constexpr int kTileRows = 128;
 constexpr int kTileKeys = 64;
-// Keys of one tile of a wave of attend_rows.
+// Rows of one workgroup of attend_shared (four waves of 16).
+constexpr int kSharedRows = 64;
+// Keys of one tile of a wave of attend_rows, and of attend_shared.
 constexpr int kPagedTile = 32;
 // Pieces: long rows are split over workgroups and joined.  A round of
 // workgroups is two per CU.
@@ -32,20 +34,32 @@ constexpr int kPieceLong = 1024;
 constexpr int kPagedMaxPieces = 256;
 constexpr int64_t kMaxRecords = 131072;
 
-// Microseconds of a prefill in n pieces per row tile, for choosing n: steps
-// (64 keys of attend_tiles, 128 of attend_rows) that a workgroup takes one
-// after another, 1.5 us each where it has a CU to itself and 2.1 where two
-// share it, in rounds; no less than K and V at 5 TB/s, drawn by as many
-// workgroups as the rounds hold on average; and the join, a launch and the
+// Microseconds of a prefill in n pieces per row tile, for choosing n.  Steps of
+// a workgroup, one after another, take us1 each where it has a CU to itself and
+// us2 where two share it; row tiles see `avg` of the longest one's keys on
+// average (half in a fresh prompt), so short tiles have fewer pieces; the
+// workgroups run in rounds, or (the longest first) one into another with half a
+// piece of them uneven at the end.  No less than K and V at 5 TB/s, drawn by as
+// many workgroups as the rounds hold on average; and the join, a launch and the
 // records written and read (8 bytes per row and element at 4 TB/s).
 // Measured: 16 tokens onto 500 (8 KV heads), one piece 19.5 us, four 12.1;
 // 1024 fresh tokens, two pieces 55 us, one 30; 3..9 tokens onto 32K (4
 // sequences), 23 pieces (1.4 rounds) 115 us, 16 (one) 100.
-inline double prefill_us(int64_t tiles, int64_t steps, int64_t n, int64_t rows, double kv_bytes, int d) {
-  const int64_t wgs = tiles * n, per = (steps + n - 1) / n, rounds = (wgs + kPagedRound - 1) / kPagedRound;
-  const double us = double(rounds * per) * (wgs <= kPagedRound / 2 ? 1.5 : 2.1);
-  const double mem = kv_bytes / 5e6 * double(rounds * kPagedRound) / wgs;
-  return (us > mem ? us : mem) + (n > 1 ? 4 + double(rows) * n * (d + 2) * 8 / 4e6 : 0);
+struct StepCost {
+  int keys;
+  double us1, us2;
+};
+inline double prefill_us(double tiles, int64_t keys, double avg, const StepCost& c, int64_t n, int64_t rows,
+                         double kv_bytes, int d) {
+  const int64_t steps = (keys + c.keys - 1) / c.keys;
+  const double per = double((steps + n - 1) / n), wgs = tiles * (double(n) * avg + (1 - avg));
+  const double rounds = double(int64_t((wgs + kPagedRound - 1) / kPagedRound));
+  double t = rounds * per;
+  const double even = tiles * double(steps) * avg / kPagedRound + per / 2;
+  t = t < even ? t : even > per ? even : per;
+  t *= wgs <= kPagedRound / 2 ? c.us1 : c.us2;
+  const double mem = kv_bytes / 5e6 * rounds * kPagedRound / wgs;
+  return (t > mem ? t : mem) + (n > 1 ? 4 + double(rows) * double(n) * (d + 2) * 8 / 4e6 : 0);
 }
 
 struct PagedArgs {
@@ -90,7 +104,8 @@ struct EvictArgs {
 
 // keys: visible tokens of a sequence, at most (it sizes a grid only)
 hipError_t launch_paged_decode(const PagedArgs& a, int64_t keys, int d, int dtype, hipStream_t stream);
-// tile_rows: kPagedRows (attend_rows) or kTileRows (attend_tiles, bf16 only)
+// tile_rows: kPagedRows (attend_rows), kSharedRows (attend_shared) or kTileRows
+// (attend_tiles, bf16 only)
 hipError_t launch_paged_prefill(const PagedArgs& a, const PagedSeqs& s, int d, int dtype, int tile_rows,
                                 hipStream_t stream);
 hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs& s, int n_observe, int64_t keys, int d, int dtype,

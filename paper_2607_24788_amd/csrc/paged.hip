@@ -721,6 +721,197 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
 }
 
+// ---------------------------------------------------------------------------
+// Attention of many rows in fp32 (and in bf16 over pages of fewer than 16
+// tokens): a workgroup takes 64 rows, 16 per wave, over the 32-key tiles that
+// any of them sees, in turn; K and V go through LDS for the four waves, a tile
+// ahead.  The products are those of attend_rows.  Bound by the fp32 matrix
+// instructions (128 of 32 cycles per wave and tile at d = 128).
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s) {
+  constexpr int KK = D / 32, CT = D / 16, ES = int(sizeof(T)), RS = D + (ES == 2 ? 16 : 4);
+  constexpr int LPR = D * ES / 16, RPI = 256 / LPR, NL = kPagedTile / RPI;  // rows of a load of the workgroup, loads
+  static_assert(NL >= 1, "a tile holds a load's rows");
+  __shared__ __align__(16) T kl[2][kPagedTile * RS], vl[2][kPagedTile * RS];
+  const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
+  const int si = find_seq(s, tile), b = s.seq0 + si, ntok = s.len[si];
+  const int64_t tok0 = s.start[si];
+  const int32_t len = __builtin_amdgcn_readfirstlane(seq_len(a, b)), p0 = len - ntok;
+  const int r0 = (tile - s.tile0[si]) * kSharedRows, rend = ntok * a.G;
+  const int rlast = r0 + kSharedRows < rend ? r0 + kSharedRows - 1 : rend - 1;
+  const int32_t t0 = p0 + r0 / a.G > 0 ? p0 + r0 / a.G : 0, t1 = p0 + rlast / a.G;
+  const int w0 = r0 + 16 * wave;
+  const bool rok = w0 + n < rend;
+  const int r = rok ? w0 + n : rend - 1, tok = r / a.G;
+  const int32_t tr = rok ? p0 + tok : -1;
+  const int64_t orow = (tok0 + tok) * a.Hq + g * a.G + (r - tok * a.G);
+  const int32_t tw1 = w0 < rend ? p0 + (w0 + 15 < rend ? w0 + 15 : rend - 1) / a.G : -1;  // the wave's last position
+  Seen sn = {0, 0, 0};
+  if (t1 >= 0) sn = seen_by(t0, t1, a.W, a.ns);
+  int32_t pl = (sn.n + a.npiece - 1) / a.npiece;
+  pl = pl > a.piece ? (pl + 31) & ~31 : a.piece;
+  const int32_t v0 = int32_t(int64_t(blockIdx.y) * pl < sn.n ? int64_t(blockIdx.y) * pl : sn.n);
+  const int32_t v1 = sn.n - v0 > pl ? v0 + pl : sn.n;
+  const int32_t* trow = a.table + int64_t(b) * a.max_pages;
+
+  Frag<T> qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    qf[kk].load(reinterpret_cast<const T*>(a.q) + orow * D + 32 * kk + 8 * lg);
+    if (!rok) qf[kk].zero();
+  }
+  float m = kNoMax, l = 0.f;
+  f32x4_t acc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) acc[ct] = zero4();
+
+  // rows RPI e + thread / LPR of a tile, 16 bytes of each: pages, then K and V
+  const int srow = threadIdx.x / LPR, c16 = (threadIdx.x % LPR) * 16;
+  struct Pages {
+    int32_t p[NL];
+  };
+  auto look = [&](int32_t x) {
+    Pages pg;
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int32_t vi = x + RPI * e + srow;
+      pg.p[e] = trow[(vi < v1 ? sn.pos(vi) : 0) >> a.shift];
+      if (vi >= v1) pg.p[e] = -1;
+    }
+    return pg;
+  };
+  uint4 ks[NL], vs[NL];
+  auto fetch = [&](int32_t x, const Pages& pg) {
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int32_t j = sn.pos(x + RPI * e + srow);
+      const bool ok = uint32_t(pg.p[e]) < uint32_t(a.n_pages);
+      const Slot sl = {pg.p[e], j & ((1 << a.shift) - 1), true};
+      gptr_t kr = ok ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : (gptr_t)zero_row;
+      gptr_t vr = ok ? (gptr_t)a.vp + slot_offset(a.vs, sl, g) : (gptr_t)zero_row;
+      if (a.kn && ok && j >= p0) {
+        const int64_t at = ((tok0 + j - p0) * a.Hkv + g) * (D * ES);
+        kr = (gptr_t)a.kn + at;
+        vr = (gptr_t)a.vn + at;
+      }
+      ks[e] = gload16<false>(kr + c16);
+      vs[e] = gload16<false>(vr + c16);
+    }
+  };
+  // the tile's rows that are there, by row
+  auto there = [&](int32_t x) {
+    const int32_t vi = x + (lane & 31);
+    const int32_t page = trow[(vi < v1 ? sn.pos(vi) : 0) >> a.shift];
+    return uint32_t(__ballot(vi < v1 && uint32_t(page) < uint32_t(a.n_pages)));
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int at = (RPI * e + srow) * RS * ES + c16;
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(kl[buf]) + at) = ks[e];
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(vl[buf]) + at) = vs[e];
+    }
+  };
+
+  if (a.kn && blockIdx.y == 0) {
+    const int32_t end = first_token(r0 + kSharedRows, a.G);
+    append_rows<D * ES>(a, trow, g, tok0, p0, first_token(r0, a.G), end < ntok ? end : ntok);
+  }
+  if (v0 < v1) {
+    fetch(v0, look(v0));
+    Pages next = look(v0 + kPagedTile);
+    uint32_t okc = there(v0);
+    put(0);
+    int buf = 0;
+    for (int32_t x = v0;; x += kPagedTile, buf ^= 1) {
+      const bool more = x + kPagedTile < v1;
+      uint32_t okn = 0;
+      __syncthreads();
+      if (more) {
+        fetch(x + kPagedTile, next);
+        next = look(x + 2 * kPagedTile);
+        okn = there(x + kPagedTile);
+      }
+      if (sn.pos(x) <= tw1) {  // (a tile behind the wave's last row, in ascending order)
+        f32x4_t sc[2] = {zero4(), zero4()};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            Frag<T> k;
+            k.load(kl[buf] + (16 * t + n) * RS + 32 * kk + 8 * lg);
+            sc[t] = mma(k, qf[kk], sc[t]);
+          }
+        float p[8], mx = m;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = 16 * t + 4 * lg + i;
+            const int32_t j = sn.pos(x + key);
+            const bool see = (((okc >> key) & 1) != 0) & (j <= tr) & ((j > tr - a.W) | (j < a.ns));
+            p[4 * t + i] = see ? sc[t][i] * a.scale : -INFINITY;
+            mx = fmaxf(mx, p[4 * t + i]);
+          }
+        mx = lg_max(mx);
+        const float f = __builtin_amdgcn_exp2f(m - mx);
+        m = mx;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(p[i] - m);
+          l += p[i];
+        }
+        Frag<T> pf;
+        pf.set8(p);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[ct][i] *= f;
+          Frag<T> vc;
+          load_colfrag2(vc, vl[buf], RS, 4 * lg, 16 + 4 * lg, 16 * ct);
+          acc[ct] = mma(vc, pf, acc[ct]);
+        }
+      }
+      if (!more) break;
+      put(buf ^ 1);
+      okc = okn;
+    }
+  }
+
+  l = lg_sum(l);
+  if (!rok) return;
+  if (a.npiece > 1) {
+    const int64_t rec = orow * a.npiece + blockIdx.y;
+    if (lg == 0) {
+      a.ml[rec * 2] = m;
+      a.ml[rec * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+      *reinterpret_cast<float4*>(a.acc + rec * D + 16 * ct + 4 * lg) =
+          make_float4(acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]);
+    return;
+  }
+  if (lg == 0) {
+    const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) : l == 0.f ? -INFINITY : l;
+    if (a.lse) a.lse[orow] = lse2 * kLn2;
+    if (a.lse2) a.lse2[orow] = lse2;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* w = reinterpret_cast<T*>(a.out) + orow * D + 4 * lg;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float y[4] = {acc[ct][0] * inv, acc[ct][1] * inv, acc[ct][2] * inv, acc[ct][3] * inv};
+    if constexpr (ES == 2)
+      *reinterpret_cast<uint2*>(w + 16 * ct) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+    else
+      *reinterpret_cast<float4*>(w + 16 * ct) = make_float4(y[0], y[1], y[2], y[3]);
+  }
+}
+
 // The pieces of a row joined: a wave's lanes take the pieces'
 // frames and sums (npiece <= 256, four each).  Bound by latency.
 struct Joined {
@@ -993,10 +1184,9 @@ hipError_t prefill_t(const PagedArgs& a, const PagedSeqs& s, int tile_rows, hipS
   const dim3 grid(uint32_t(tiles * a.Hkv), a.npiece);
   if constexpr (sizeof(T) == 2) {
     if (tile_rows == kTileRows) attend_tiles<D><<<grid, 256, 0, stream>>>(a, s);
-    else attend_rows<T, D, PagedSeqs><<<grid, 256, 0, stream>>>(a, s);
-  } else {
-    attend_rows<T, D, PagedSeqs><<<grid, 256, 0, stream>>>(a, s);
   }
+  if (tile_rows == kSharedRows) attend_shared<T, D><<<grid, 256, 0, stream>>>(a, s);
+  else if (tile_rows == kPagedRows) attend_rows<T, D, PagedSeqs><<<grid, 256, 0, stream>>>(a, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.npiece == 1) return e;
   const int64_t row0 = int64_t(s.start[0]) * a.Hq;

@@ -80,13 +80,20 @@ void plan_decode(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
 }
 void plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
                   int64_t max_len, PagedArgs* a) {
-  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), step = tile_rows == kTileRows ? kTileKeys : 128;
-  const int64_t steps = (keys + step - 1) / step;
+  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len));
+  const double fp32 = c->dtype == GLIDE_F32 ? c->head_dim / 128.0 : 0.25;  // of attend_shared's product time
+  const StepCost cost = tile_rows == kTileRows     ? StepCost{kTileKeys, 1.5, 2.1}
+                        : tile_rows == kSharedRows ? StepCost{kPagedTile, 0.4 + 1.8 * fp32, 0.4 + 3.4 * fp32}
+                                                   : StepCost{4 * kPagedTile, 1.5, 2.1};
   const double kv = 2.0 * nseq * c->n_kv_heads * double(keys) * c->head_dim * esize(c);
-  auto us = [&](int64_t m) { return prefill_us(tiles, steps, m, rows, kv, c->head_dim); };
+  // new tokens of a sequence, against the keys that the last of them sees
+  const double T = double(rows) / (double(nseq) * c->n_q_heads), K = double(keys);
+  const double avg = T <= K ? 1 - T / (2 * K) : 1 - K / (2 * T);
+  auto us = [&](int64_t m) { return prefill_us(double(tiles), keys, avg, cost, m, rows, kv, c->head_dim); };
   int64_t n = 1;
   double best = us(1);
-  for (int64_t m = 2; m <= std::min(steps, max_pieces(tiles, tile_rows)); ++m) {
+  const int64_t most = std::min((keys + cost.keys - 1) / cost.keys, max_pieces(tiles, tile_rows));
+  for (int64_t m = 2; m <= most; ++m) {
     const double x = us(m);
     if (x < best) {
       n = m;
@@ -119,14 +126,17 @@ int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1
   return n;
 }
 
-// Rows per tile of a prefill: the tiles kernel (bf16), also where few of its
-// 128 rows are there (it reads K and V once for all of them).  It takes 16
-// keys of a page at 32-bit offsets: pages of 16 tokens or more, and no rows
-// further apart than that.
-int tile_rows(const glide_paged_config* c, const glide_paged_cache* k) {
+// Rows per tile of a prefill.
+//  attend_tiles (bf16), also where few of its 128 rows are there (it reads K
+//    and V once for all of them).  It takes 16 keys of a page at 32-bit
+//    offsets: pages of 16 tokens or more, no rows further apart than that.
+//  Else attend_shared, where 64-row tiles make half a round or more; with fewer
+//    rows attend_rows, whose waves share the keys of 16 rows.
+int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu) {
   const int64_t far = int64_t(1) << 26;
-  return c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far ? kTileRows
-                                                                                                         : kPagedRows;
+  if (c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far)
+    return kTileRows;
+  return row_tiles(c, cu, 0, c->batch, kSharedRows) * c->n_kv_heads * 2 >= kPagedRound ? kSharedRows : kPagedRows;
 }
 
 void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a) {
@@ -206,7 +216,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
   a.out = static_cast<char*>(out);
   a.lse = lse;
   hipStream_t st = hipStream_t(stream);
-  const int per_tile = tile_rows(cfg, cache);
+  const int per_tile = tile_rows(cfg, cache, cu);
   for (int b0 = 0; b0 < cfg->batch;) {
     PagedSeqs t;
     memset(&t, 0, sizeof(t));

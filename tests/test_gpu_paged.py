@@ -176,6 +176,21 @@ def test_prefill_length_hint_changes_no_result(dtype, max_len):
                 max_len=max_len)
 
 
+@pytest.mark.parametrize("dtype,page,d,W,ns,hist", [(FP32, 16, 128, None, 0, 0), (FP32, 64, 64, 200, 70, 90),
+                                                    (BF16, 8, 128, 333, 4, 50), (BF16, 1, 64, None, 0, 0)])
+def test_prefill_rows_shared(dtype, page, d, W, ns, hist):
+    """fp32, and bf16 on small pages, with rows enough for 64-row tiles."""
+    new = [900, 0, 141]
+    case = Case(3, 32, 16, d, page, [n + (hist if n else 0) for n in new], W, ns, dtype=dtype, weights=True, seed=67)
+    case.table[0, 3] = -1
+    case.dev_table.copy_(case.table)
+    run_prefill(case, new, 7)
+
+
+def test_prefill_rows_shared_in_pieces():
+    run_prefill(Case(1, 64, 64, 64, 32, [1503], None, 0, dtype=FP32, seed=66), [260], append=False, max_len=1503)
+
+
 def test_prefill_many_rows_in_pieces():
     """Row tiles that do not fill the card over a long cache: each in pieces,
     rows that begin and end inside tiles, new rows inside a group of 16."""
