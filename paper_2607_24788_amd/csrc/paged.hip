@@ -782,6 +782,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
     }
     return pg;
   };
+  const bool same = a.ks[0] == a.vs[0] && a.ks[1] == a.vs[1] && a.ks[2] == a.vs[2];
   uint4 ks[NL], vs[NL];
   auto fetch = [&](int32_t x, const Pages& pg) {
 #pragma unroll
@@ -789,8 +790,11 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
       const int32_t j = sn.pos(x + RPI * e + srow);
       const bool ok = uint32_t(pg.p[e]) < uint32_t(a.n_pages);
       const Slot sl = {pg.p[e], j & ((1 << a.shift) - 1), true};
-      gptr_t kr = ok ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : (gptr_t)zero_row;
-      gptr_t vr = ok ? (gptr_t)a.vp + slot_offset(a.vs, sl, g) : (gptr_t)zero_row;
+      const int64_t ko = slot_offset(a.ks, sl, g);
+      int64_t vo = ko;
+      if (!same) vo = slot_offset(a.vs, sl, g);
+      gptr_t kr = ok ? (gptr_t)a.kp + ko : (gptr_t)zero_row;
+      gptr_t vr = ok ? (gptr_t)a.vp + vo : (gptr_t)zero_row;
       if (a.kn && ok && j >= p0) {
         const int64_t at = ((tok0 + j - p0) * a.Hkv + g) * (D * ES);
         kr = (gptr_t)a.kn + at;
@@ -856,9 +860,15 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
             mx = fmaxf(mx, p[4 * t + i]);
           }
         mx = lg_max(mx);
-        const float f = __builtin_amdgcn_exp2f(m - mx);
-        m = mx;
-        l *= f;
+        if (__any(mx > m)) {
+          const float f = __builtin_amdgcn_exp2f(m - mx);
+          m = mx;
+          l *= f;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[ct][i] *= f;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[i] = __builtin_amdgcn_exp2f(p[i] - m);
@@ -868,8 +878,6 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
         pf.set8(p);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[ct][i] *= f;
           Frag<T> vc;
           load_colfrag2(vc, vl[buf], RS, 4 * lg, 16 + 4 * lg, 16 * ct);
           acc[ct] = mma(vc, pf, acc[ct]);
