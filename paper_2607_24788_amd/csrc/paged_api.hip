@@ -78,13 +78,20 @@ void plan_decode(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
   const int64_t piece = std::min<int64_t>(kPieceLong, std::max<int64_t>(kPieceMin, units * keys / kPagedRound));
   set_pieces(std::min((keys + piece - 1) / piece, max_pieces(units, kPagedRows)), keys, a);
 }
-void plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
-                  int64_t max_len, PagedArgs* a) {
-  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len));
-  const double fp32 = c->dtype == GLIDE_F32 ? c->head_dim / 128.0 : 0.25;  // of attend_shared's product time
-  const StepCost cost = tile_rows == kTileRows     ? StepCost{kTileKeys, 1.5, 2.1}
-                        : tile_rows == kSharedRows ? StepCost{kPagedTile, 0.4 + 1.8 * fp32, 0.4 + 3.4 * fp32}
-                                                   : StepCost{4 * kPagedTile, 1.5, 2.1};
+// Steps of the prefill kernels, timed with one and with two workgroups per CU.
+StepCost step_cost(const glide_paged_config* c, int tile_rows) {
+  const double d = c->head_dim / 128.0;
+  if (tile_rows == kTileRows) return {kTileKeys, 1.5, 2.1};
+  if (c->dtype == GLIDE_BF16)  // pages of fewer than 16 tokens
+    return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.0, 1.3} : StepCost{4 * kPagedTile, 1.5, 3.0};
+  return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.2 + 1.8 * d, 0.4 + 5.1 * d}
+                                  : StepCost{4 * kPagedTile, 0.5 + 3.5 * d, 0.7 + 7 * d};
+}
+// The best number of pieces of a prefill of `rows` rows in `tiles` row tiles
+// (nseq sequences), and the time that the model gives it.
+double plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
+                    int64_t keys, int64_t* pieces) {
+  const StepCost cost = step_cost(c, tile_rows);
   const double kv = 2.0 * nseq * c->n_kv_heads * double(keys) * c->head_dim * esize(c);
   // new tokens of a sequence, against the keys that the last of them sees
   const double T = double(rows) / (double(nseq) * c->n_q_heads), K = double(keys);
@@ -100,7 +107,8 @@ void plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int
       best = x;
     }
   }
-  set_pieces(n, keys, a);
+  *pieces = n;
+  return best;
 }
 
 // Sections of the workspace of one call, in bytes from its start.
@@ -130,13 +138,22 @@ int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1
 //  attend_tiles (bf16), also where few of its 128 rows are there (it reads K
 //    and V once for all of them).  It takes 16 keys of a page at 32-bit
 //    offsets: pages of 16 tokens or more, no rows further apart than that.
-//  Else attend_shared, where 64-row tiles make half a round or more; with fewer
-//    rows attend_rows, whose waves share the keys of 16 rows.
-int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu) {
+//  Else attend_shared (64 rows, each wave 16 of them over every key) or
+//    attend_rows (16 rows, each wave a quarter of the keys), whichever the
+//    model gives less time.  fp32, 40 tokens onto 16000: 146 / 175 us; four
+//    512-token prompts of 4 heads, d = 64, W = 64: 16.6 / 10.6 us.
+int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu, int64_t max_len) {
   const int64_t far = int64_t(1) << 26;
   if (c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far)
     return kTileRows;
-  return row_tiles(c, cu, 0, c->batch, kSharedRows) * c->n_kv_heads * 2 >= kPagedRound ? kSharedRows : kPagedRows;
+  const int64_t rows = int64_t(cu[c->batch]) * c->n_q_heads, keys = std::max<int64_t>(1, most_seen(c, max_len));
+  int64_t nseq = 0, n;
+  for (int32_t b = 0; b < c->batch; ++b) nseq += cu[b + 1] > cu[b];
+  auto us = [&](int r) {
+    return plan_prefill(c, std::max<int64_t>(1, row_tiles(c, cu, 0, c->batch, r) * c->n_kv_heads), r, rows, nseq, keys,
+                        &n);
+  };
+  return us(kSharedRows) < us(kPagedRows) ? kSharedRows : kPagedRows;
 }
 
 void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a) {
@@ -216,7 +233,7 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
   a.out = static_cast<char*>(out);
   a.lse = lse;
   hipStream_t st = hipStream_t(stream);
-  const int per_tile = tile_rows(cfg, cache, cu);
+  const int per_tile = tile_rows(cfg, cache, cu, max_len);
   for (int b0 = 0; b0 < cfg->batch;) {
     PagedSeqs t;
     memset(&t, 0, sizeof(t));
@@ -233,7 +250,11 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
     t.nseq = b1 - b0;
     // records by the call's row number: a launch's own rows only
     const int64_t row0 = int64_t(cu[b0]) * cfg->n_q_heads, rows = int64_t(cu[b1]) * cfg->n_q_heads - row0;
-    plan_prefill(cfg, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads, per_tile, rows, t.nseq, max_len, &a);
+    const int64_t keys = std::max<int64_t>(1, most_seen(cfg, max_len));
+    int64_t n;
+    plan_prefill(cfg, std::max<int64_t>(1, int64_t(t.tile0[t.nseq]) * cfg->n_kv_heads), per_tile, rows, t.nseq, keys,
+                 &n);
+    set_pieces(n, keys, &a);
     const Sections w = sections(cfg, total_tokens * cfg->n_q_heads, a.npiece > 1 ? rows * a.npiece : 0,
                                 n_observe > 0, false);
     char* ws = static_cast<char*>(workspace);
