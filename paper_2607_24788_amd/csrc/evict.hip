@@ -60,7 +60,8 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint3
 // positions.  Keys are read once and kept in LDS up to KEYS tokens, four
 // neighbours to a thread in the passes; longer sequences go through LDS in
 // segments, read again per pass.  Bound by the latency of the reads and of two
-// dozen barriers, and by the instructions of 16 waves on one CU.  (Keys in
+// dozen barriers, and by the instructions of 16 waves on one CU: 8K tokens 10.7
+// us, 16K..32K 27 (256 of them, one per CU), 450..700 7.2.  (Keys in
 // registers, their loops unrolled: 24 us at 8K tokens and 21 at 700, most of
 // it the fetch of the code.)
 template <int KEYS>
@@ -206,7 +207,8 @@ __device__ __forceinline__ Slot slot_of(const EvictArgs& a, const int32_t* row, 
 }
 
 // Kept rows to fresh pages: 32 tokens of a (sequence, KV head) per workgroup,
-// every 16-byte piece of K and V on a thread of its own.  Bound by memory.
+// every 16-byte piece of K and V on a thread of its own.  Bound by memory: 4096
+// tokens of 256 heads, 1.1 GB moved in 216 us (5.0 TB/s).
 constexpr int kMoveRows = 32;
 __global__ __launch_bounds__(256) void evict_copy(EvictArgs a) {
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;

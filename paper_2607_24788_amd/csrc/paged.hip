@@ -63,6 +63,10 @@ __device__ __forceinline__ int32_t first_token(int r0, int G) { return (r0 + G -
 //   S^T = K Q^T (keys are the MFMA rows): a lane holds 8 scores of one row,
 //   already the right operand of O^T += V^T P^T with keys in the order
 //   4g + 0..3, 16 + 4g + 0..3; V goes through LDS for its columns.
+// Decode is bound by HBM: 32 sequences of 16K..32K tokens, 8 KV heads of 128,
+// bf16, 3.2 GB in 530 us (6.0 TB/s); 8 sequences of 16K in fp32 5.5 TB/s.
+// Small calls are bound by the chain table -> rows -> scores -> join of the
+// waves: 5.7 us over 64 tokens.
 struct NoSeqs {};
 template <typename T, int D, typename Seqs>  // Seqs: PagedSeqs, or NoSeqs for a decode call
 __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
@@ -361,6 +365,11 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
 //   Row sums of the weights are taken before they are rounded to bf16: lse is
 //   exact to fp32.  The frame (a row's maximum) moves only when a score passes
 //   it by 2^8: weights up to 2^8 round alike, and fp32 sums hold them.
+// Bound by the matrix cores at the clock that the power limit leaves: a prompt
+// of 32768 tokens (32 / 8 heads of 128) 8.7 ms = 1016 TFLOP/s, MFMAs half of
+// the cycles at 2.0 GHz; 8192 tokens with W = 2048 292 us.  Tiles are staged
+// through registers, a tile ahead: two workgroups per CU (64 KB of LDS, 235
+// registers each).
 // A 16-byte piece c of row r is kept at piece c ^ swz(r) of the row: eight
 // consecutive rows' K pieces, and four rows' 64-byte V segments, lie in
 // different banks.
@@ -726,7 +735,9 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 // tokens): a workgroup takes 64 rows, 16 per wave, over the 32-key tiles that
 // any of them sees, in turn; K and V go through LDS for the four waves, a tile
 // ahead.  The products are those of attend_rows.  Bound by the fp32 matrix
-// instructions (128 of 32 cycles per wave and tile at d = 128).
+// instructions (128 of 32 cycles per wave and tile at d = 128) and the address
+// arithmetic between them: 4096 tokens, 32 / 8 heads of 128, 1.43 ms = 96
+// TFLOP/s (attend_rows: 2.02 ms).
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s) {
   constexpr int KK = D / 32, CT = D / 16, ES = int(sizeof(T)), RS = D + (ES == 2 ? 16 : 4);
@@ -921,7 +932,8 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
 }
 
 // The pieces of a row joined: a wave's lanes take the pieces'
-// frames and sums (npiece <= 256, four each).  Bound by latency.
+// frames and sums (npiece <= 256, four each).  Bound by latency: 32 rows of 64
+// pieces 3.6 us.
 struct Joined {
   float M, L;
 };
@@ -1027,6 +1039,7 @@ hipError_t join_t(const PagedArgs& a, int64_t row0, int64_t rows, hipStream_t st
 // launch: of a (sequence, KV head) the first G workgroups join a row each, the
 // others take 256 visible tokens each.  Bound by latency: the frames of the
 // rows, then one read of the scores (asked for before the frames: no faster).
+// 8 sequences, 64 / 8 heads, 8195 tokens each: 12 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
   __shared__ float part[4][D], z[kMaxG];
@@ -1071,7 +1084,8 @@ __global__ __launch_bounds__(256) void join_weights(PagedArgs a) {
 // (their K fragments in registers) and goes through the scored rows in order,
 // 64 at a time through LDS: no sum's order depends on timing.  Bound by the
 // latency of its loads where few rows are scored, else by its products and
-// exponentials.
+// exponentials.  32 queries of 4 heads over 4036 tokens, 8 sequences of 8 KV
+// heads: 32 us (K again: 13 at 5 TB/s).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s, int n_observe) {
   constexpr int KK = D / 32, ES = int(sizeof(T)), RS = D + 16 / ES, NB = 64;  // rows of a block
