@@ -32,6 +32,65 @@ __device__ __forceinline__ int32_t seq_len(const PagedArgs& a, int b) {
 }
 
 // ---------------------------------------------------------------------------
+// NaN and infinities in value rows.  In a tile that some rows of a workgroup
+// see and others do not (an "edge"), a weight of 0 must leave out what it
+// multiplies, and 0 times infinity does not.  There such elements are staged as
+// zeros, and the rows that do see them add their products one by one: work for
+// nothing but such values.
+__device__ __forceinline__ bool finite16(uint4 v, bf16_t) {
+  auto two = [](uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; };
+  return two(v.x) && two(v.y) && two(v.z) && two(v.w);
+}
+__device__ __forceinline__ bool finite16(uint4 v, float) {
+  auto one = [](uint32_t x) { return (x & 0x7f800000u) != 0x7f800000u; };
+  return one(v.x) && one(v.y) && one(v.z) && one(v.w);
+}
+__device__ __forceinline__ uint4 without_nonfinite(uint4 v, bf16_t) {
+  auto two = [](uint32_t x) {
+    return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+  };
+  return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
+}
+__device__ __forceinline__ uint4 without_nonfinite(uint4 v, float) {
+  auto one = [](uint32_t x) { return (x & 0x7f800000u) == 0x7f800000u ? 0u : x; };
+  return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
+}
+// Four consecutive elements of a row, where not finite times w, added to y.
+// (Nothing moves across: a batch of these loads would take the registers of
+// the path that never comes here.)
+__device__ __forceinline__ void add_nonfinite4(float* y, gptr_t p, float w, bf16_t) {
+  const uint64_t x = *(const uint64_t __attribute__((address_space(1)))*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t e = uint32_t(x >> (16 * i)) & 0xffffu;
+    if ((e & 0x7f80u) == 0x7f80u) y[i] += w * to_f32(bf16_t(e));
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void add_nonfinite4(float* y, gptr_t p, float w, float) {
+  const uint4 x = gload16<false>(p);
+  const uint32_t e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if ((e[i] & 0x7f800000u) == 0x7f800000u) y[i] += w * __uint_as_float(e[i]);
+  __builtin_amdgcn_sched_barrier(0);
+}
+// Bit r of the answer: some lane of r's LPR lanes, from lane r * LPR on, is set in m.
+template <int LPR>
+__device__ __forceinline__ uint32_t rows_of(uint64_t m) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int r = 0; r < 64 / LPR; ++r)
+    x |= ((m >> (r * LPR)) & (LPR == 64 ? ~uint64_t(0) : (uint64_t(1) << (LPR & 63)) - 1)) ? 1u << r : 0u;
+  return x;
+}
+// Whether a tile of keys at positions j0 .. j1 holds any that one of the rows at
+// t0 .. t1 does not see (and another may).
+__device__ __forceinline__ bool edge_tile(const PagedArgs& a, int32_t j0, int32_t j1, int32_t t0, int32_t t1) {
+  return j1 > t0 || (j0 <= t1 - a.W && j1 >= a.ns);
+}
+
+// ---------------------------------------------------------------------------
 // A call's new rows of one KV head, tokens i0 <= i < i1 of a sequence, into
 // their pages, by the workgroup whose row tile has their first head; the
 // attention itself reads them where the call gave them.  Their weights start
@@ -163,6 +222,22 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       *vr = (gptr_t)a.vn + at;
     }
   };
+  // the values of key `key` of a tile (position j) that are not finite
+  auto add_nonfinite = [&](int key, int32_t j, const float* p) {
+    float w = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w = i == ((key >> 4) * 4 + (key & 3)) ? p[i] : w;
+    w = __shfl(w, ((key >> 2) & 3) * 16 + n);
+    gptr_t kr, vr;
+    row_at(true, j, trow[j >> a.shift], &kr, &vr);
+    if (w == 0.f) return;  // not seen
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
+      add_nonfinite4(y, vr + (16 * ct + 4 * lg) * ES, w, T());
+      acc[ct] = f32x4_t{y[0], y[1], y[2], y[3]};
+    }
+  };
   Frag<T> kf[2][KK], vf[2][KK];  // bf16: NL pieces each, [0] and [1] in turn
   uint32_t okm = 0;              // the tile's rows that are there
   auto fetch = [&](const At& p, int32_t x) {
@@ -205,6 +280,37 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
   for (; x < v1; x += STEP) {
     f32x4_t sc[2] = {zero4(), zero4()};
     const uint32_t okc = okm;
+    uint32_t bad = 0;  // rows of an edge with values that are not finite
+    if constexpr (!DECODE) {
+      if (edge_tile(a, sn.pos(x), sn.pos(x + kPagedTile - 1), t0, t1)) {
+        if constexpr (KLDS) {
+#pragma unroll
+          for (int e = 0; e < NL; ++e) {
+            uint4& v = vf[e / KK][e % KK].v;
+            const uint64_t nf = __ballot(!finite16(v, T()));
+            if (nf) {
+              bad |= rows_of<LPR>(nf) << (e * RPI);
+              v = without_nonfinite(v, T());
+            }
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            bool nf = false;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const bool no = (__float_as_uint(vf[t][kk].v[e]) & 0x7f800000u) == 0x7f800000u;
+                nf |= no;
+                vf[t][kk].v[e] = no ? 0.f : vf[t][kk].v[e];
+              }
+            const uint64_t m4 = __ballot(nf);
+            bad |= uint32_t((m4 | m4 >> 16 | m4 >> 32 | m4 >> 48) & 0xffffu) << (16 * t);
+          }
+        }
+      }
+    }
     if constexpr (KLDS) {
       T* kt = klds[wave];
 #pragma unroll
@@ -289,6 +395,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       acc[ct] = mma(vc, pf, acc[ct]);
     }
     wave_lds_order();
+    if constexpr (!DECODE) {
+      while (bad) {
+        const int key = __builtin_ctz(bad);
+        bad &= bad - 1;
+        add_nonfinite(key, sn.pos(x + key), p);
+      }
+    }
   }
 
   // the four waves' parts: each row's frame, then the sums in it
@@ -404,6 +517,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   constexpr int KK = D / 16, CT = D / 32, RB = 2 * D, LPR = RB / 16, RPI = 64 / LPR, NI = 16 / RPI;
   constexpr int KB = kTileKeys * RB;  // bytes of a K (or V) tile
   __shared__ __align__(16) char lds[2][2 * KB];
+  __shared__ uint32_t bad[2][4];  // rows (of a wave's 16) of an edge with values that are not finite
   const int lane = threadIdx.x & 63, h = lane >> 5, q = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
@@ -527,8 +641,21 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
       st.v[e] = make_uint4(w.x | y.x, w.y | y.y, w.z | y.z, w.w | y.w);
     }
   };
-  auto put = [&](char* buf, const Stage& st) {
-    char* w = buf + wave * 16 * RB + lane * 16;
+  auto edge = [&](int32_t i) { return edge_tile(a, key0(i), key0(i) + kTileKeys - 1, t0, t1); };
+  auto put = [&](int at, int32_t i, Stage& st) {
+    char* w = lds[at] + wave * 16 * RB + lane * 16;
+    if (edge(i)) {
+      uint32_t rows = 0;
+#pragma unroll
+      for (int e = 0; e < NI; ++e) {
+        const uint64_t nf = __ballot(!finite16(st.v[e], bf16_t()));
+        if (nf) {
+          rows |= rows_of<LPR>(nf) << (e * RPI);
+          st.v[e] = without_nonfinite(st.v[e], bf16_t());
+        }
+      }
+      if (lane == 0) bad[at][wave] = rows;
+    }
 #pragma unroll
     for (int e = 0; e < NI; ++e) {
       *reinterpret_cast<uint4*>(w + e * 1024) = st.k[e];
@@ -549,7 +676,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   const int vlane = KB + vrow * RB + (l16 & 1) * 8;
   const int vsw = (2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ swz<D>(vrow);
 
-  auto compute = [&](const char* buf, int32_t i, uint32_t okp) {
+  auto compute = [&](int at, int32_t i, uint32_t okp) {
+    const char* buf = lds[at];
     const int32_t k0 = key0(i);
     if (k0 > tw1 || (k0 + kTileKeys <= tw0 - a.W + 1 && k0 >= a.ns)) return;  // nothing for this wave
     __builtin_amdgcn_s_setprio(1);
@@ -624,6 +752,39 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[ct][e] *= f;
     }
+    if (edge(i)) {
+#pragma unroll 1
+      for (int u = 0; u < 4; ++u) {
+        uint32_t m = __builtin_amdgcn_readfirstlane(bad[at][u]);
+        while (m) {
+          const int key = 16 * u + __builtin_ctz(m);
+          m &= m - 1;
+          // the key's weight: in lane half (key / 4) % 2, element 4 (key % 32 / 8) + key % 4 of half tile key / 32
+          float x = -INFINITY;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x = (key & ~4) == key_of(t, e) ? sc[t][e] : x;
+          x = __builtin_amdgcn_exp2f(fmaf(x, c, -mc));
+          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+          x = __uint_as_float((key >> 2) & 1 ? both[1] : both[0]);
+          const int32_t j = k0 + key;
+          const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+          const gptr_t vr = j >= new0 ? (gptr_t)a.vn + nat + int64_t(j - p0) * a.Hkv * RB
+                                      : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
+          if (x == 0.f) continue;  // not seen
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float y[4] = {o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
+              add_nonfinite4(y, vr + (32 * ct + 8 * e + 4 * h) * 2, x, bf16_t());
+#pragma unroll
+              for (int w = 0; w < 4; ++w) o[ct][4 * e + w] = y[w];
+            }
+        }
+      }
+    }
     // P V by 16-key slabs: under a slab's MFMAs the next slab's weights are
     // taken and its V fragments read, in an order that the compiler keeps
     auto weights2 = [&](int sl, int e) {  // elements e, e + 1 of slab sl, as a bf16 pair
@@ -672,9 +833,9 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     uint32_t okc = okbits(pg);
     fetch(i0, pg, st);
     pg = pages_of(i0 + 1 < i1 ? i0 + 1 : i0);
-    put(lds[0], st);
+    put(0, i0, st);
     for (int32_t i = i0;; ++i) {
-      char* cur = lds[(i - i0) & 1];
+      const int cur = (i - i0) & 1;
       __syncthreads();
       const uint32_t okn = okbits(pg);
       if (i + 1 < i1) {
@@ -683,7 +844,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
       }
       compute(cur, i, okc);
       if (i + 1 >= i1) break;
-      put(lds[(i - i0 + 1) & 1], st);
+      put(cur ^ 1, i + 1, st);
       okc = okn;
     }
   }
@@ -744,6 +905,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
   constexpr int LPR = D * ES / 16, RPI = 256 / LPR, NL = kPagedTile / RPI;  // rows of a load of the workgroup, loads
   static_assert(NL >= 1, "a tile holds a load's rows");
   __shared__ __align__(16) T kl[2][kPagedTile * RS], vl[2][kPagedTile * RS];
+  __shared__ uint32_t bad[2][4];  // rows of an edge with values that are not finite, by the wave that read them
   const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
@@ -821,7 +983,20 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
     const int32_t page = trow[(vi < v1 ? sn.pos(vi) : 0) >> a.shift];
     return uint32_t(__ballot(vi < v1 && uint32_t(page) < uint32_t(a.n_pages)));
   };
-  auto put = [&](int buf) {
+  auto edge = [&](int32_t x) { return edge_tile(a, sn.pos(x), sn.pos(x + kPagedTile - 1), t0, t1); };
+  auto put = [&](int buf, int32_t x) {
+    if (edge(x)) {
+      uint32_t rows = 0;
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        const uint64_t nf = __ballot(!finite16(vs[e], T()));
+        if (nf) {
+          rows |= rows_of<LPR>(nf) << (RPI * e + wave * (64 / LPR));
+          vs[e] = without_nonfinite(vs[e], T());
+        }
+      }
+      if (lane == 0) bad[buf][wave] = rows;
+    }
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
       const int at = (RPI * e + srow) * RS * ES + c16;
@@ -838,7 +1013,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
     fetch(v0, look(v0));
     Pages next = look(v0 + kPagedTile);
     uint32_t okc = there(v0);
-    put(0);
+    put(0, v0);
     int buf = 0;
     for (int32_t x = v0;; x += kPagedTile, buf ^= 1) {
       const bool more = x + kPagedTile < v1;
@@ -893,9 +1068,31 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
           load_colfrag2(vc, vl[buf], RS, 4 * lg, 16 + 4 * lg, 16 * ct);
           acc[ct] = mma(vc, pf, acc[ct]);
         }
+        if (edge(x)) {
+          uint32_t m4 = __builtin_amdgcn_readfirstlane(bad[buf][0] | bad[buf][1] | bad[buf][2] | bad[buf][3]);
+          while (m4) {
+            const int key = __builtin_ctz(m4);
+            m4 &= m4 - 1;
+            float w = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w = i == ((key >> 4) * 4 + (key & 3)) ? p[i] : w;
+            w = __shfl(w, ((key >> 2) & 3) * 16 + n);
+            const int32_t j = sn.pos(x + key);
+            const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+            const gptr_t vr = a.kn && j >= p0 ? (gptr_t)a.vn + ((tok0 + j - p0) * a.Hkv + g) * (D * ES)
+                                              : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
+            if (w == 0.f) continue;  // not seen
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+              float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
+              add_nonfinite4(y, vr + (16 * ct + 4 * lg) * ES, w, T());
+              acc[ct] = f32x4_t{y[0], y[1], y[2], y[3]};
+            }
+          }
+        }
       }
       if (!more) break;
-      put(buf ^ 1);
+      put(buf ^ 1, x + kPagedTile);
       okc = okn;
     }
   }

@@ -187,6 +187,49 @@ def test_prefill_rows_shared(dtype, page, d, W, ns, hist):
     run_prefill(case, new, 7)
 
 
+@pytest.mark.parametrize("values", ["k", "v"])
+@pytest.mark.parametrize("dtype,page,Hq,Hkv,d,new,hist,W", [
+    (BF16, 16, 8, 2, 128, [150, 70], 90, 40), (BF16, 32, 4, 4, 64, [200, 33], 100, None),
+    (FP32, 16, 4, 2, 128, [50, 37], 61, 30), (FP32, 16, 4, 2, 64, [40, 7], 90, None), (BF16, 4, 4, 2, 128, [60, 9], 70, 25),
+    (FP32, 64, 32, 16, 64, [600, 450], 100, 300), (BF16, 8, 32, 16, 128, [600, 450], 0, None)])
+def test_nan_and_infinity_in_unseen_places(dtype, page, Hq, Hkv, d, new, hist, W, values):
+    """Keys or values that are not finite, among the new tokens and the cached
+    ones: rows that see them have what the definition gives, all others are as
+    if they were not there."""
+    case = Case(2, Hq, Hkv, d, page, [n + hist for n in new], W, 2, dtype=dtype, seed=65)
+    g = case.g
+    cu = [0, new[0], sum(new)]
+    q, k, v = (case.normal(cu[-1], h, d) for h in (Hq, Hkv, Hkv))
+    x = k if values == "k" else v
+    for i, y in ((0, math.nan), (1, math.inf), (17, math.nan), (new[0] - 1, -math.inf), (new[0] - 2, math.nan)):
+        x[i, i % Hkv, 3 * i % d] = y
+    if hist:      # in the cache: before the window, at its edge, in the sinks
+        pool = case.k if values == "k" else case.v
+        for j in (1, 5, hist - 30, hist - 1):
+            pool[int(case.table[0, j // page]), 0, j % page, j % d] = math.nan
+    ref = case.ref()
+    want = []
+    for b, n in enumerate(new):
+        for i in range(n):
+            ref.append(b, hist + i, k[cu[b] + i], v[cu[b] + i])
+        for i in range(n):
+            want.append(ref.row(b, hist + i, q[cu[b] + i], False))
+    out, lse = nan_like(cu[-1], Hq, d, dtype=dtype), nan_like(cu[-1], Hq, dtype=FP32)
+    g.prefill(case.cache, q.cuda(), cu, out, g.new_workspace(cu[-1]), k=k.cuda(), v=v.cuda(), lse=lse,
+              max_len=max(new) + hist)
+    got, lse = out.cpu().double(), lse.cpu().double()
+    clean = 0
+    for i, (o, z, tol, ztol) in enumerate(want):
+        fine = o.isfinite()
+        clean += int(fine.all())
+        assert torch.equal(got[i].isnan(), o.isnan()) and torch.equal(got[i][o.isinf()], o[o.isinf()]), f"row {i}"
+        assert ((got[i] - o).abs()[fine] <= tol[fine]).all(), f"row {i}"
+        assert torch.equal(lse[i].isfinite(), z.isfinite()) and ((lse[i] - z).abs()[z.isfinite()]
+                                                                <= ztol[z.isfinite()]).all(), f"row {i}: lse"
+    assert clean > 0
+    case.pools_equal(ref)
+
+
 def test_prefill_rows_shared_in_pieces():
     run_prefill(Case(1, 64, 64, 64, 32, [1503], None, 0, dtype=FP32, seed=66), [260], append=False, max_len=1503)
 
