@@ -517,7 +517,9 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   constexpr int KK = D / 16, CT = D / 32, RB = 2 * D, LPR = RB / 16, RPI = 64 / LPR, NI = 16 / RPI;
   constexpr int KB = kTileKeys * RB;  // bytes of a K (or V) tile
   __shared__ __align__(16) char lds[2][2 * KB];
-  __shared__ uint32_t bad[2][4];  // rows (of a wave's 16) of an edge with values that are not finite
+  // edges with values that are not finite: whether there are any; those of a
+  // tile, by the 16 rows of a wave
+  __shared__ uint32_t any_bad, bad[4];
   const int lane = threadIdx.x & 63, h = lane >> 5, q = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
@@ -645,16 +647,12 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   auto put = [&](int at, int32_t i, Stage& st) {
     char* w = lds[at] + wave * 16 * RB + lane * 16;
     if (edge(i)) {
-      uint32_t rows = 0;
 #pragma unroll
-      for (int e = 0; e < NI; ++e) {
-        const uint64_t nf = __ballot(!finite16(st.v[e], bf16_t()));
-        if (nf) {
-          rows |= rows_of<LPR>(nf) << (e * RPI);
+      for (int e = 0; e < NI; ++e)
+        if (__any(!finite16(st.v[e], bf16_t()))) {
           st.v[e] = without_nonfinite(st.v[e], bf16_t());
+          any_bad = 1;
         }
-      }
-      if (lane == 0) bad[at][wave] = rows;
     }
 #pragma unroll
     for (int e = 0; e < NI; ++e) {
@@ -676,12 +674,12 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
   const int vlane = KB + vrow * RB + (l16 & 1) * 8;
   const int vsw = (2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ swz<D>(vrow);
 
-  auto compute = [&](int at, int32_t i, uint32_t okp) {
-    const char* buf = lds[at];
-    const int32_t k0 = key0(i);
-    if (k0 > tw1 || (k0 + kTileKeys <= tw0 - a.W + 1 && k0 >= a.ns)) return;  // nothing for this wave
+  auto key_of = [](int t, int e) { return 32 * t + 8 * (e >> 2) + (e & 3); };
+  auto nothing = [&](int32_t k0) {  // for this wave in a tile
+    return k0 > tw1 || (k0 + kTileKeys <= tw0 - a.W + 1 && k0 >= a.ns);
+  };
+  auto products = [&](const char* buf, f32x16_t* sc) {
     __builtin_amdgcn_s_setprio(1);
-    f32x16_t sc[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -702,19 +700,12 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     }
     __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
     __builtin_amdgcn_s_setprio(0);
-    auto vfrag = [&](int sl, int ct) {
-      const char* p = buf + vlane + 16 * sl * RB + (((4 * ct) ^ vsw) << 4);
-      const char* p2 = buf + vlane + (16 * sl + 8) * RB + (((4 * ct) ^ vsw ^ 2) << 4);
-      return vt_frag(p, p2);
-    };
-    uint4 vf[CT];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) vf[ct] = vfrag(0, ct);
+  };
+  auto masks = [&](int32_t k0, uint32_t okp, f32x16_t* sc) {
     // what the rows do not see, where the tile may hold any (each kind tested
     // for the wave; key 32t + 8(e/4) + e%4 of the lane's is an instruction's
     // constant): keys after a row, keys before its window that are no sinks,
     // groups of 16 whose page is not there
-    auto key_of = [](int t, int e) { return 32 * t + 8 * (e >> 2) + (e & 3); };
     if (k0 + kTileKeys - 1 > tw0) {
       const int32_t last = tr - k0 - 4 * h;
 #pragma unroll
@@ -736,6 +727,22 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[t][e] = (okp >> (2 * t + (e >> 3))) & 1 ? sc[t][e] : -INFINITY;
     }
+  };
+  auto compute = [&](int at, int32_t i, uint32_t okp) {
+    const char* buf = lds[at];
+    const int32_t k0 = key0(i);
+    if (nothing(k0)) return;
+    f32x16_t sc[2];
+    products(buf, sc);
+    auto vfrag = [&](int sl, int ct) {
+      const char* p = buf + vlane + 16 * sl * RB + (((4 * ct) ^ vsw) << 4);
+      const char* p2 = buf + vlane + (16 * sl + 8) * RB + (((4 * ct) ^ vsw ^ 2) << 4);
+      return vt_frag(p, p2);
+    };
+    uint4 vf[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vf[ct] = vfrag(0, ct);
+    masks(k0, okp, sc);
     float mx = sc[0][0];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -751,39 +758,6 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[ct][e] *= f;
-    }
-    if (edge(i)) {
-#pragma unroll 1
-      for (int u = 0; u < 4; ++u) {
-        uint32_t m = __builtin_amdgcn_readfirstlane(bad[at][u]);
-        while (m) {
-          const int key = 16 * u + __builtin_ctz(m);
-          m &= m - 1;
-          // the key's weight: in lane half (key / 4) % 2, element 4 (key % 32 / 8) + key % 4 of half tile key / 32
-          float x = -INFINITY;
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x = (key & ~4) == key_of(t, e) ? sc[t][e] : x;
-          x = __builtin_amdgcn_exp2f(fmaf(x, c, -mc));
-          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-          x = __uint_as_float((key >> 2) & 1 ? both[1] : both[0]);
-          const int32_t j = k0 + key;
-          const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
-          const gptr_t vr = j >= new0 ? (gptr_t)a.vn + nat + int64_t(j - p0) * a.Hkv * RB
-                                      : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
-          if (x == 0.f) continue;  // not seen
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float y[4] = {o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
-              add_nonfinite4(y, vr + (32 * ct + 8 * e + 4 * h) * 2, x, bf16_t());
-#pragma unroll
-              for (int w = 0; w < 4; ++w) o[ct][4 * e + w] = y[w];
-            }
-        }
-      }
     }
     // P V by 16-key slabs: under a slab's MFMAs the next slab's weights are
     // taken and its V fragments read, in an order that the compiler keeps
@@ -821,6 +795,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
     append_rows<RB>(a, trow, g, s.start[si], p0, first_token(r0, a.G), end < ntok ? end : ntok);
   }
 
+  if (threadIdx.x == 0) any_bad = 0;
+  __syncthreads();
   if (i0 < i1) {
     auto okbits = [&](const Pages& p) {
       uint32_t m = 0;
@@ -846,6 +822,60 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
       if (i + 1 >= i1) break;
       put(cur ^ 1, i + 1, st);
       okc = okn;
+    }
+    __syncthreads();
+    // Nearly never: the edges that were staged without some of their values,
+    // once more, for the products that those values have.
+    if (any_bad) {
+#pragma unroll 1
+      for (int32_t i = i0; i < i1; ++i) {
+        if (!edge(i)) continue;
+        pg = pages_of(i);
+        fetch(i, pg, st);
+        uint32_t rows = 0;
+#pragma unroll
+        for (int e = 0; e < NI; ++e) rows |= rows_of<LPR>(__ballot(!finite16(st.v[e], bf16_t()))) << (e * RPI);
+        __syncthreads();
+        if (lane == 0) bad[wave] = rows;
+        put(0, i, st);
+        __syncthreads();
+        const int32_t k0 = key0(i);
+        if (nothing(k0)) continue;
+        f32x16_t sc[2];
+        products(lds[0], sc);
+        masks(k0, okbits(pg), sc);
+#pragma unroll 1
+        for (int u = 0; u < 4; ++u) {
+          uint32_t m = __builtin_amdgcn_readfirstlane(bad[u]);
+          while (m) {
+            const int key = 16 * u + __builtin_ctz(m);
+            m &= m - 1;
+            // the key's weight: in lane half (key / 4) % 2, element 4 (key % 32 / 8) + key % 4 of half tile key / 32
+            float x = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x = (key & ~4) == key_of(t, e) ? sc[t][e] : x;
+            x = __builtin_amdgcn_exp2f(fmaf(x, c, -mc));
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+            x = __uint_as_float((key >> 2) & 1 ? both[1] : both[0]);
+            const int32_t j = k0 + key;
+            const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+            const gptr_t vr = j >= new0 ? (gptr_t)a.vn + nat + int64_t(j - p0) * a.Hkv * RB
+                                        : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
+            if (x == 0.f) continue;  // not seen
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float y[4] = {o[ct][4 * e], o[ct][4 * e + 1], o[ct][4 * e + 2], o[ct][4 * e + 3]};
+                add_nonfinite4(y, vr + (32 * ct + 8 * e + 4 * h) * 2, x, bf16_t());
+#pragma unroll
+                for (int w = 0; w < 4; ++w) o[ct][4 * e + w] = y[w];
+              }
+          }
+        }
+      }
     }
   }
 
