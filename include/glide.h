@@ -292,11 +292,10 @@ glide_status glide_feature_map(const glide_config* cfg, const void* phi_w, const
  *   lse_t = log sum_{visible} e^{tau q_t.k_j}
  * O_t = 0 and lse_t = -inf where nothing is visible.  W at or beyond the
  * context gives causal softmax attention, as for a GLIDE layer; W = 0 leaves
- * the sinks alone.  What a query does not see, page slots behind a sequence's
- * last token and pages that are not allocated have no part in its row,
- * whatever bits they hold; but a NaN or infinity in a value row that some
- * query of a call sees may reach the rows of other queries of that call (not
- * of other sequences or KV heads).
+ * the sinks alone.  What a query does not see (later tokens, tokens before its
+ * window, page slots behind a sequence's last token, pages that are not
+ * allocated) has no part in its row, whatever bits it holds, NaN and infinities
+ * among them.
  *
  * A sequence is its cached tokens in order: after an eviction, positions (and
  * with them W, n_sinks) count the tokens that were kept. */
@@ -321,7 +320,8 @@ typedef struct {
  * contiguous.  block_table [B][max_pages]: token j of sequence b is in slot
  * j % page_size of page block_table[b][j / page_size]; an entry outside
  * [0, n_pages) is not allocated: its tokens are not visible and what is
- * written to them is dropped.  lens [B]: tokens cached, after the call's own
+ * written to them is dropped; the allocated entries of a sequence's tokens are
+ * distinct pages.  lens [B]: tokens cached, after the call's own
  * appends (taken as 0 below 0, as max_pages * page_size above it).  A page
  * that a call writes to (its new rows, weights that it adds to, rows that it
  * moves) belongs to one sequence; pages that are only read may be shared. */

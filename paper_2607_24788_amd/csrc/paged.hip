@@ -935,7 +935,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
   constexpr int LPR = D * ES / 16, RPI = 256 / LPR, NL = kPagedTile / RPI;  // rows of a load of the workgroup, loads
   static_assert(NL >= 1, "a tile holds a load's rows");
   __shared__ __align__(16) T kl[2][kPagedTile * RS], vl[2][kPagedTile * RS];
-  __shared__ uint32_t bad[2][4];  // rows of an edge with values that are not finite, by the wave that read them
+  __shared__ uint32_t any_bad, bad[4];  // as in attend_tiles; by the wave that read them
   const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = s.tile0[s.nseq] - 1 - int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
@@ -1016,16 +1016,12 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
   auto edge = [&](int32_t x) { return edge_tile(a, sn.pos(x), sn.pos(x + kPagedTile - 1), t0, t1); };
   auto put = [&](int buf, int32_t x) {
     if (edge(x)) {
-      uint32_t rows = 0;
 #pragma unroll
-      for (int e = 0; e < NL; ++e) {
-        const uint64_t nf = __ballot(!finite16(vs[e], T()));
-        if (nf) {
-          rows |= rows_of<LPR>(nf) << (RPI * e + wave * (64 / LPR));
+      for (int e = 0; e < NL; ++e)
+        if (__any(!finite16(vs[e], T()))) {
           vs[e] = without_nonfinite(vs[e], T());
+          any_bad = 1;
         }
-      }
-      if (lane == 0) bad[buf][wave] = rows;
     }
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
@@ -1035,6 +1031,30 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
     }
   };
 
+  // scores of a tile's 16 t + 4 lg + i in p[4 t + i], -inf where the lane's row does not see them
+  auto scores = [&](int buf, int32_t x, uint32_t okc, float* p) {
+    f32x4_t sc[2] = {zero4(), zero4()};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Frag<T> k;
+        k.load(kl[buf] + (16 * t + n) * RS + 32 * kk + 8 * lg);
+        sc[t] = mma(k, qf[kk], sc[t]);
+      }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = 16 * t + 4 * lg + i;
+        const int32_t j = sn.pos(x + key);
+        const bool see = (((okc >> key) & 1) != 0) & (j <= tr) & ((j > tr - a.W) | (j < a.ns));
+        p[4 * t + i] = see ? sc[t][i] * a.scale : -INFINITY;
+      }
+  };
+
+  if (threadIdx.x == 0) any_bad = 0;
+  __syncthreads();
   if (a.kn && blockIdx.y == 0) {
     const int32_t end = first_token(r0 + kSharedRows, a.G);
     append_rows<D * ES>(a, trow, g, tok0, p0, first_token(r0, a.G), end < ntok ? end : ntok);
@@ -1055,26 +1075,11 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
         okn = there(x + kPagedTile);
       }
       if (sn.pos(x) <= tw1) {  // (a tile behind the wave's last row, in ascending order)
-        f32x4_t sc[2] = {zero4(), zero4()};
+        float p[8];
+        scores(buf, x, okc, p);
+        float mx = m;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            Frag<T> k;
-            k.load(kl[buf] + (16 * t + n) * RS + 32 * kk + 8 * lg);
-            sc[t] = mma(k, qf[kk], sc[t]);
-          }
-        float p[8], mx = m;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = 16 * t + 4 * lg + i;
-            const int32_t j = sn.pos(x + key);
-            const bool see = (((okc >> key) & 1) != 0) & (j <= tr) & ((j > tr - a.W) | (j < a.ns));
-            p[4 * t + i] = see ? sc[t][i] * a.scale : -INFINITY;
-            mx = fmaxf(mx, p[4 * t + i]);
-          }
+        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
         mx = lg_max(mx);
         if (__any(mx > m)) {
           const float f = __builtin_amdgcn_exp2f(m - mx);
@@ -1098,32 +1103,50 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
           load_colfrag2(vc, vl[buf], RS, 4 * lg, 16 + 4 * lg, 16 * ct);
           acc[ct] = mma(vc, pf, acc[ct]);
         }
-        if (edge(x)) {
-          uint32_t m4 = __builtin_amdgcn_readfirstlane(bad[buf][0] | bad[buf][1] | bad[buf][2] | bad[buf][3]);
-          while (m4) {
-            const int key = __builtin_ctz(m4);
-            m4 &= m4 - 1;
-            float w = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w = i == ((key >> 4) * 4 + (key & 3)) ? p[i] : w;
-            w = __shfl(w, ((key >> 2) & 3) * 16 + n);
-            const int32_t j = sn.pos(x + key);
-            const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
-            const gptr_t vr = a.kn && j >= p0 ? (gptr_t)a.vn + ((tok0 + j - p0) * a.Hkv + g) * (D * ES)
-                                              : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
-            if (w == 0.f) continue;  // not seen
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-              float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
-              add_nonfinite4(y, vr + (16 * ct + 4 * lg) * ES, w, T());
-              acc[ct] = f32x4_t{y[0], y[1], y[2], y[3]};
-            }
-          }
-        }
       }
       if (!more) break;
       put(buf ^ 1, x + kPagedTile);
       okc = okn;
+    }
+    __syncthreads();
+    if (any_bad) {
+#pragma unroll 1
+      for (int32_t x = v0; x < v1; x += kPagedTile) {
+        if (!edge(x)) continue;
+        fetch(x, look(x));
+        const uint32_t okc = there(x);
+        uint32_t rows = 0;
+#pragma unroll
+        for (int e = 0; e < NL; ++e)
+          rows |= rows_of<LPR>(__ballot(!finite16(vs[e], T()))) << (RPI * e + wave * (64 / LPR));
+        __syncthreads();
+        if (lane == 0) bad[wave] = rows;
+        put(0, x);
+        __syncthreads();
+        if (sn.pos(x) > tw1) continue;
+        float p[8];
+        scores(0, x, okc, p);
+        uint32_t m4 = __builtin_amdgcn_readfirstlane(bad[0] | bad[1] | bad[2] | bad[3]);
+        while (m4) {
+          const int key = __builtin_ctz(m4);
+          m4 &= m4 - 1;
+          float w = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w = i == ((key >> 4) * 4 + (key & 3)) ? p[i] : w;
+          w = __shfl(__builtin_amdgcn_exp2f(w - m), ((key >> 2) & 3) * 16 + n);
+          const int32_t j = sn.pos(x + key);
+          const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
+          const gptr_t vr = a.kn && j >= p0 ? (gptr_t)a.vn + ((tok0 + j - p0) * a.Hkv + g) * (D * ES)
+                                            : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
+          if (w == 0.f) continue;  // not seen
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
+            add_nonfinite4(y, vr + (16 * ct + 4 * lg) * ES, w, T());
+            acc[ct] = f32x4_t{y[0], y[1], y[2], y[3]};
+          }
+        }
+      }
     }
   }
 
