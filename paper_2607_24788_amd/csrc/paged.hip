@@ -224,10 +224,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
   };
   // the values of key `key` of a tile (position j) that are not finite
   auto add_nonfinite = [&](int key, int32_t j, const float* p) {
-    float w = 0.f;
+    float w = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) w = i == ((key >> 4) * 4 + (key & 3)) ? p[i] : w;
-    w = __shfl(w, ((key >> 2) & 3) * 16 + n);
+    w = __shfl(__builtin_amdgcn_exp2f(w - m), ((key >> 2) & 3) * 16 + n);
     gptr_t kr, vr;
     row_at(true, j, trow[j >> a.shift], &kr, &vr);
     if (w == 0.f) return;  // not seen
@@ -269,6 +269,62 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       }
     }
   };
+  // rows of the fetched tile with values that are not finite (lane: of its pieces)
+  auto edge = [&](int32_t x) { return edge_tile(a, sn.pos(x), sn.pos(x + kPagedTile - 1), t0, t1); };
+  auto nonfinite_rows = [&]() {
+    uint32_t bad = 0;
+    if constexpr (KLDS) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e)
+        bad |= rows_of<LPR>(__ballot(!finite16(vf[e / KK][e % KK].v, T()))) << (e * RPI);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        bool nf = false;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) nf |= (__float_as_uint(vf[t][kk].v[e]) & 0x7f800000u) == 0x7f800000u;
+        const uint64_t m4 = __ballot(nf);
+        bad |= uint32_t((m4 | m4 >> 16 | m4 >> 32 | m4 >> 48) & 0xffffu) << (16 * t);
+      }
+    }
+    return bad;
+  };
+  auto drop_nonfinite = [&]() {
+    const bool any = nonfinite_rows() != 0;
+    if (any) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          if constexpr (KLDS) {
+            vf[t][kk].v = without_nonfinite(vf[t][kk].v, T());
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              vf[t][kk].v[e] = (__float_as_uint(vf[t][kk].v[e]) & 0x7f800000u) == 0x7f800000u ? 0.f : vf[t][kk].v[e];
+          }
+        }
+    }
+    return any;
+  };
+  // scores of the lane's keys 16 t + 4 lg + i in p[4 t + i], -inf where its row does not see them
+  auto masked = [&](const f32x4_t* sc, uint32_t okc, int32_t x, float* p) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = 4 * lg + i;
+        bool see = (okc >> (16 * t + key)) & 1;
+        if constexpr (!DECODE) {
+          const int32_t j = sn.pos(x + 16 * t + key);
+          see = see && j <= tr && (j > tr - a.W || j < a.ns);
+        }
+        p[4 * t + i] = see ? sc[t][i] * a.scale : -INFINITY;
+      }
+  };
+  bool any_bad = false;
   constexpr int STEP = 4 * kPagedTile;
   int32_t x = v0 + wave * kPagedTile;
   At next = {};
@@ -280,36 +336,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
   for (; x < v1; x += STEP) {
     f32x4_t sc[2] = {zero4(), zero4()};
     const uint32_t okc = okm;
-    uint32_t bad = 0;  // rows of an edge with values that are not finite
     if constexpr (!DECODE) {
-      if (edge_tile(a, sn.pos(x), sn.pos(x + kPagedTile - 1), t0, t1)) {
-        if constexpr (KLDS) {
-#pragma unroll
-          for (int e = 0; e < NL; ++e) {
-            uint4& v = vf[e / KK][e % KK].v;
-            const uint64_t nf = __ballot(!finite16(v, T()));
-            if (nf) {
-              bad |= rows_of<LPR>(nf) << (e * RPI);
-              v = without_nonfinite(v, T());
-            }
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            bool nf = false;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const bool no = (__float_as_uint(vf[t][kk].v[e]) & 0x7f800000u) == 0x7f800000u;
-                nf |= no;
-                vf[t][kk].v[e] = no ? 0.f : vf[t][kk].v[e];
-              }
-            const uint64_t m4 = __ballot(nf);
-            bad |= uint32_t((m4 | m4 >> 16 | m4 >> 32 | m4 >> 48) & 0xffffu) << (16 * t);
-          }
-        }
-      }
+      if (edge(x)) any_bad |= drop_nonfinite();
     }
     if constexpr (KLDS) {
       T* kt = klds[wave];
@@ -352,20 +380,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       }
     }
     float p[8];
+    masked(sc, okc, x, p);
     float mx = m;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = 4 * lg + i;
-        bool see = (okc >> (16 * t + key)) & 1;
-        if constexpr (!DECODE) {
-          const int32_t j = sn.pos(x + 16 * t + key);
-          see = see && j <= tr && (j > tr - a.W || j < a.ns);
-        }
-        p[4 * t + i] = see ? sc[t][i] * a.scale : -INFINITY;
-        mx = fmaxf(mx, p[4 * t + i]);
-      }
+    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
     if constexpr (DECODE) {
       if (a.scores && rok) {
         float* w = a.scores + (int64_t(b) * a.Hq + g * a.G + r) * a.nv + x + 4 * lg;
@@ -395,11 +413,39 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       acc[ct] = mma(vc, pf, acc[ct]);
     }
     wave_lds_order();
-    if constexpr (!DECODE) {
-      while (bad) {
-        const int key = __builtin_ctz(bad);
-        bad &= bad - 1;
-        add_nonfinite(key, sn.pos(x + key), p);
+  }
+  if constexpr (!DECODE) {
+    // Nearly never: the edges that were staged without some of their values.
+    if (any_bad) {
+#pragma unroll 1
+      for (x = v0 + wave * kPagedTile; x < v1; x += STEP) {
+        if (!edge(x)) continue;
+        fetch(look(x), x);
+        uint32_t bad = nonfinite_rows();
+        f32x4_t sc[2] = {zero4(), zero4()};
+        if constexpr (KLDS) {
+          T* kt = klds[wave];
+#pragma unroll
+          for (int e = 0; e < NL; ++e)
+            *reinterpret_cast<uint4*>(kt + (e * RPI + lane / LPR) * RS + (lane % LPR) * 8) = kf[e / KK][e % KK].v;
+          wave_lds_order();
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            Frag<T> k = kf[t][kk];
+            if constexpr (KLDS) k.load(klds[wave] + (16 * t + n) * RS + 32 * kk + 8 * lg);
+            sc[t] = mma(k, qf[kk], sc[t]);
+          }
+        wave_lds_order();
+        float p[8];
+        masked(sc, okm, x, p);
+        while (bad) {
+          const int key = __builtin_ctz(bad);
+          bad &= bad - 1;
+          add_nonfinite(key, sn.pos(x + key), p);
+        }
       }
     }
   }
