@@ -525,9 +525,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
 //   exact to fp32.  The frame (a row's maximum) moves only when a score passes
 //   it by 2^8: weights up to 2^8 round alike, and fp32 sums hold them.
 // Bound by the matrix cores at the clock that the power limit leaves: a prompt
-// of 32768 tokens (32 / 8 heads of 128) 8.7 ms = 1016 TFLOP/s, MFMAs half of
-// the cycles at 2.0 GHz; 8192 tokens with W = 2048 292 us.  Tiles are staged
-// through registers, a tile ahead: two workgroups per CU (64 KB of LDS, 235
+// of 32768 tokens (32 / 8 heads of 128) 9.1 ms = 969 TFLOP/s, MFMAs half of
+// the cycles at 1.94 GHz; 8192 tokens with W = 2048 305 us.  Tiles are staged
+// through registers, a tile ahead: two workgroups per CU (64 KB of LDS, 241
 // registers each).
 // A 16-byte piece c of row r is kept at piece c ^ swz(r) of the row: eight
 // consecutive rows' K pieces, and four rows' 64-byte V segments, lie in
@@ -973,7 +973,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
 // any of them sees, in turn; K and V go through LDS for the four waves, a tile
 // ahead.  The products are those of attend_rows.  Bound by the fp32 matrix
 // instructions (128 of 32 cycles per wave and tile at d = 128) and the address
-// arithmetic between them: 4096 tokens, 32 / 8 heads of 128, 1.43 ms = 96
+// arithmetic between them: 4096 tokens, 32 / 8 heads of 128, 1.44 ms = 95
 // TFLOP/s (attend_rows: 2.02 ms).
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s) {

@@ -140,8 +140,8 @@ int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1
 //    offsets: pages of 16 tokens or more, no rows further apart than that.
 //  Else attend_shared (64 rows, each wave 16 of them over every key) or
 //    attend_rows (16 rows, each wave a quarter of the keys), whichever the
-//    model gives less time.  fp32, 40 tokens onto 16000: 146 / 175 us; four
-//    512-token prompts of 4 heads, d = 64, W = 64: 16.6 / 10.6 us.
+//    model gives less time.  fp32, 40 tokens onto 16000: 148 / 176 us; four
+//    512-token prompts of 4 heads, d = 64, W = 64: 17.7 / 11.2 us.
 int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu, int64_t max_len) {
   const int64_t far = int64_t(1) << 26;
   if (c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far)
