@@ -83,9 +83,9 @@ StepCost step_cost(const glide_paged_config* c, int tile_rows) {
   const double d = c->head_dim / 128.0;
   if (tile_rows == kTileRows) return {kTileKeys, 1.5, 2.1};
   if (c->dtype == GLIDE_BF16)  // pages of fewer than 16 tokens
-    return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.0, 1.3} : StepCost{4 * kPagedTile, 1.5, 3.0};
-  return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.2 + 1.8 * d, 0.4 + 5.1 * d}
-                                  : StepCost{4 * kPagedTile, 0.5 + 3.5 * d, 0.7 + 7 * d};
+    return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.0, 1.3} : StepCost{4 * kPagedTile, 1.5 + d, 3.3};
+  return tile_rows == kSharedRows ? StepCost{kPagedTile, 1.2 + 1.8 * d, 0.4 + 4.9 * d}
+                                  : StepCost{4 * kPagedTile, 0.5 + 4 * d, 0.7 + 7.4 * d};
 }
 // The best number of pieces of a prefill of `rows` rows in `tiles` row tiles
 // (nseq sequences), and the time that the model gives it.
@@ -141,7 +141,8 @@ int64_t row_tiles(const glide_paged_config* c, const int32_t* cu, int b0, int b1
 //  Else attend_shared (64 rows, each wave 16 of them over every key) or
 //    attend_rows (16 rows, each wave a quarter of the keys), whichever the
 //    model gives less time.  fp32, 40 tokens onto 16000: 148 / 176 us; four
-//    512-token prompts of 4 heads, d = 64, W = 64: 17.7 / 11.2 us.
+//    512-token prompts of 4 heads, d = 64, W = 64: 17.7 / 11.2 us; 600 tokens
+//    61 / 72 us; bf16, pages of 4, 100 tokens onto 900: 20.6 / 26.9 us.
 int tile_rows(const glide_paged_config* c, const glide_paged_cache* k, const int32_t* cu, int64_t max_len) {
   const int64_t far = int64_t(1) << 26;
   if (c->dtype == GLIDE_BF16 && c->page_size >= 16 && k->k_strides[2] <= far && k->v_strides[2] <= far)
