@@ -191,7 +191,9 @@ def test_prefill_rows_shared(dtype, page, d, W, ns, hist):
 @pytest.mark.parametrize("dtype,page,Hq,Hkv,d,new,hist,W", [
     (BF16, 16, 8, 2, 128, [150, 70], 90, 40), (BF16, 32, 4, 4, 64, [200, 33], 100, None),
     (FP32, 16, 4, 2, 128, [50, 37], 61, 30), (FP32, 16, 4, 2, 64, [40, 7], 90, None), (BF16, 4, 4, 2, 128, [60, 9], 70, 25),
-    (FP32, 64, 32, 16, 64, [600, 450], 100, 300), (BF16, 8, 32, 16, 128, [600, 450], 0, None)])
+    (FP32, 64, 32, 16, 64, [600, 450], 100, 300), (BF16, 8, 32, 16, 128, [600, 450], 0, None),
+    (FP32, 16, 4, 2, 128, [40, 7], 90, None), (FP32, 8, 4, 1, 128, [21, 40], 200, 170),
+    (BF16, 4, 4, 2, 128, [60, 9], 200, None), (BF16, 8, 4, 2, 64, [40, 7], 210, 180)])
 def test_nan_and_infinity_in_unseen_places(dtype, page, Hq, Hkv, d, new, hist, W, values):
     """Keys or values that are not finite, among the new tokens and the cached
     ones: rows that see them have what the definition gives, all others are as
