@@ -402,16 +402,33 @@ def batch1_block(wl, no_detail):
     return out
 
 
+# The sources of the kernels that a step launches; what they include from
+# csrc/ belongs to them.
+STEP_SOURCES = ("decode.hip", "glide_api.hip", "phi.hip", "prefill.hip")
+
+
+def kernel_sources():
+    """STEP_SOURCES and the csrc/ headers that they include, sorted.  Kernels
+    of other calls (the paged cache) and the declarations and comments of
+    include/glide.h have no part in a step's traffic."""
+    import re
+    csrc = os.path.join(os.path.dirname(os.path.abspath(__file__)), "paper_2607_24788_amd", "csrc")
+    todo, seen = list(STEP_SOURCES), set()
+    while todo:
+        path = os.path.join(csrc, todo.pop())
+        if path in seen or not os.path.exists(path):
+            continue
+        seen.add(path)
+        with open(path) as fh:
+            todo += re.findall(r'^#include "([^"]+)"', fh.read(), re.M)
+    return sorted(seen)
+
+
 def kernel_sources_hash():
-    """sha256 prefix over the kernel sources (csrc/*.hip, csrc/*.h, include/glide.h)."""
-    import glob
+    """sha256 prefix over kernel_sources()."""
     import hashlib
-    root = os.path.dirname(os.path.abspath(__file__))
-    files = sorted(glob.glob(os.path.join(root, "paper_2607_24788_amd", "csrc", "*.hip")) +
-                   glob.glob(os.path.join(root, "paper_2607_24788_amd", "csrc", "*.h")))
-    files.append(os.path.join(root, "include", "glide.h"))
     h = hashlib.sha256()
-    for f in files:
+    for f in kernel_sources():
         with open(f, "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
