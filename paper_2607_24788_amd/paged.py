@@ -33,13 +33,15 @@ def _tensor(name, t, device, dtype, numel):
 
 
 class PagedCache:
-    """The cache of one layer: its tensors, and the struct that names them to
-    the library.  Made by ``Paged.cache``."""
+    """The cache of one layer: its tensors, the struct that names them to the
+    library, and the geometry that they were checked for.  Made by
+    ``Paged.cache``; every ``Paged`` of the same geometry takes it."""
 
-    def __init__(self, k_pool, v_pool, block_table, lens, weights, arg):
+    def __init__(self, k_pool, v_pool, block_table, lens, weights, arg, geometry):
         self.k_pool, self.v_pool, self.weights = k_pool, v_pool, weights
         self.block_table, self.lens = block_table, lens
         self.device = k_pool.device
+        self.geometry = geometry
         self._dev = k_pool.get_device()
         self._arg = arg
         self._ref = ctypes.byref(arg)
@@ -70,6 +72,8 @@ class Paged:
         self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = batch, n_q_heads, n_kv_heads, head_dim
         self.page_size, self.n_pages, self.max_pages = page_size, n_pages, max_pages
         self.window, self.n_sinks, self.sm_scale, self.torch_dtype = window, n_sinks, float(sm_scale), dtype
+        # what a cache's tensors are laid out by (query heads, window and sinks are not)
+        self.geometry = (batch, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype)
         if self.workspace_bytes(0) == 0:
             raise glide.GlideError(-2, "glide_paged_workspace_bytes", self.lib)
 
@@ -123,13 +127,21 @@ class Paged:
         if weights is not None:
             arg.weights = _tensor("weights", weights, dev, torch.float32,
                                   self.n_pages * self.n_kv_heads * self.page_size)
-        return PagedCache(k_pool, v_pool, block_table, lens, weights, arg)
+        return PagedCache(k_pool, v_pool, block_table, lens, weights, arg, self.geometry)
 
     # -- calls ---------------------------------------------------------------
-    def _rows(self, cache, q, k, v, out, lse, T):
-        """Pointers of a call over T rows of queries, checked."""
+    def _check_cache(self, cache):
+        """Refuse a cache whose tensors another geometry was checked for: the
+        library would follow its addresses with this layer's sizes."""
         if not isinstance(cache, PagedCache):
             raise ValueError("cache must come from Paged.cache")
+        if cache.geometry != self.geometry:
+            names = ("batch", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "dtype")
+            off = [f"{n} {x}, this layer has {y}" for n, x, y in zip(names, cache.geometry, self.geometry) if x != y]
+            raise ValueError("cache was made for " + "; ".join(off))
+
+    def _rows(self, cache, q, k, v, out, lse, T):
+        """Pointers of a call over T rows of queries, checked."""
         dev, dt = cache._dev, self.torch_dtype
         nq, nkv = T * self.n_q_heads * self.head_dim, T * self.n_kv_heads * self.head_dim
         if (k is None) != (v is None):
@@ -159,9 +171,9 @@ class Paged:
         cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
+        qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
         if n_observe and cache.weights is None:
             raise ValueError("n_observe needs a cache with weights")
-        qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_prefill", cache, stream, qp, kp, vp, self._cu(*cu), cu[-1],
                    int(n_observe), int(max_len), op, lp, ws, n)
@@ -169,6 +181,7 @@ class Paged:
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
         lse [B][Hq] fp32.  On a cache with weights every query adds its."""
+        self._check_cache(cache)
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_decode", cache, stream, qp, kp, vp, int(max_len), op, lp, ws, n)
@@ -177,8 +190,7 @@ class Paged:
         """Keep min(len, budget) tokens per sequence and KV head, in place or
         in dst_table's pages.  kept [B][Hkv][budget] int32: their old
         positions; new_lens [B] int32 (may be the cache's lens)."""
-        if not isinstance(cache, PagedCache):
-            raise ValueError("cache must come from Paged.cache")
+        self._check_cache(cache)
         if cache.weights is None:
             raise ValueError("evict needs a cache with weights")
         dev = cache._dev
