@@ -142,6 +142,7 @@ class Paged:
 
     def _rows(self, cache, q, k, v, out, lse, T):
         """Pointers of a call over T rows of queries, checked."""
+        self._check_cache(cache)
         dev, dt = cache._dev, self.torch_dtype
         nq, nkv = T * self.n_q_heads * self.head_dim, T * self.n_kv_heads * self.head_dim
         if (k is None) != (v is None):
@@ -181,7 +182,6 @@ class Paged:
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
         lse [B][Hq] fp32.  On a cache with weights every query adds its."""
-        self._check_cache(cache)
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_decode", cache, stream, qp, kp, vp, int(max_len), op, lp, ws, n)
