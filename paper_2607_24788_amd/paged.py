@@ -7,12 +7,21 @@ Argument marshalling only, as in ``glide.py``: every step runs in the HIP
 kernels behind the C ABI, and there is no fallback.
 """
 import ctypes
+import operator
 
 import torch
 
 from . import glide
 
 FULL = 1 << 30   # a window that never ends: causal softmax attention
+
+
+def _fits(name, x, bits=32):
+    """x, refused where the library's integer would hold another number (ctypes
+    drops the bits that do not fit)."""
+    if not -(1 << (bits - 1)) <= x < 1 << (bits - 1):
+        raise ValueError(f"{name} = {x} is not a {bits}-bit number")
+    return x
 
 
 def _tensor(name, t, device, dtype, numel):
@@ -62,6 +71,11 @@ class Paged:
         self.lib = lib if lib is not None else glide.load_library()
         if window is None:
             window = FULL
+        batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, window, n_sinks = (
+            _fits(name, operator.index(x)) for name, x in (
+                ("batch", batch), ("n_q_heads", n_q_heads), ("n_kv_heads", n_kv_heads), ("head_dim", head_dim),
+                ("page_size", page_size), ("n_pages", n_pages), ("max_pages", max_pages), ("window", window),
+                ("n_sinks", n_sinks)))
         if sm_scale is None:
             sm_scale = head_dim ** -0.5
         code = {torch.float32: glide.F32, torch.bfloat16: glide.BF16}.get(dtype, 99)
@@ -79,7 +93,8 @@ class Paged:
 
     # -- buffers -------------------------------------------------------------
     def workspace_bytes(self, max_total_tokens=0, weights=False):
-        return self.lib.glide_paged_workspace_bytes(self._ref, int(max_total_tokens), int(bool(weights)))
+        return self.lib.glide_paged_workspace_bytes(self._ref, _fits("max_total_tokens", int(max_total_tokens), 64),
+                                                    int(bool(weights)))
 
     def new_workspace(self, max_total_tokens=0, weights=False, device="cuda"):
         """Workspace for every call of up to max_total_tokens packed tokens;
@@ -172,19 +187,22 @@ class Paged:
         cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
+        _fits("cu_seqlens' least", min(cu))
+        _fits("cu_seqlens' largest", max(cu))
+        n_observe, max_len = _fits("n_observe", int(n_observe)), _fits("max_len", int(max_len), 64)
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
         if n_observe and cache.weights is None:
             raise ValueError("n_observe needs a cache with weights")
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_prefill", cache, stream, qp, kp, vp, self._cu(*cu), cu[-1],
-                   int(n_observe), int(max_len), op, lp, ws, n)
+                   n_observe, max_len, op, lp, ws, n)
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
         lse [B][Hq] fp32.  On a cache with weights every query adds its."""
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_decode", cache, stream, qp, kp, vp, int(max_len), op, lp, ws, n)
+        self._call("glide_paged_decode", cache, stream, qp, kp, vp, _fits("max_len", int(max_len), 64), op, lp, ws, n)
 
     def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):
         """Keep min(len, budget) tokens per sequence and KV head, in place or
@@ -193,8 +211,9 @@ class Paged:
         self._check_cache(cache)
         if cache.weights is None:
             raise ValueError("evict needs a cache with weights")
+        budget, n_recent = _fits("budget", int(budget)), _fits("n_recent", int(n_recent))
         dev = cache._dev
-        kp = _tensor("kept", kept, dev, torch.int32, self.batch * self.n_kv_heads * max(int(budget), 0))
+        kp = _tensor("kept", kept, dev, torch.int32, self.batch * self.n_kv_heads * max(budget, 0))
         lp = _tensor("new_lens", new_lens, dev, torch.int32, self.batch)
         dp = None
         if dst_table is not None:
@@ -203,4 +222,4 @@ class Paged:
                 raise ValueError(f"dst_table has shape {tuple(dst_table.shape)}, expected "
                                  f"{(self.batch, self.max_pages)}")
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_evict", cache, stream, int(budget), int(n_recent), dp, kp, lp, ws, n)
+        self._call("glide_paged_evict", cache, stream, budget, n_recent, dp, kp, lp, ws, n)

@@ -58,3 +58,54 @@ def test_not_a_cache():
     for call in calls(g, object()):
         with pytest.raises(ValueError, match="Paged.cache"):
             call()
+
+
+# the 32 bits that are left of it: another number, in range or out of it
+BIG = [1 << 32, (1 << 32) + 3, (1 << 31) + 16, -(1 << 32) + 2]
+
+
+@pytest.mark.parametrize("x", BIG)
+@pytest.mark.parametrize("name", [*SIZES, "window", "n_sinks"])
+def test_sizes_past_32_bits(name, x):
+    with pytest.raises(ValueError, match=f"{name} = {x} is not a 32-bit"):
+        layer(**{"window": 64, "n_sinks": 4, name: x})
+
+
+def test_a_window_in_range_is_the_library_s():
+    for w in (None, 1, 1 << 30):
+        g = layer(window=w)
+        assert g.window == g.cfg.window == (paged.FULL if w is None else w)
+
+
+@pytest.mark.parametrize("x", BIG)
+def test_arguments_past_32_bits(cache_of, x):
+    g = layer()
+    c = cache_of(g)
+    with pytest.raises(ValueError, match="n_observe.*32-bit"):
+        g.prefill(c, None, [0, 1, 2], None, None, n_observe=x)
+    for cu in ([0, x, 2], [0, 1, x]):
+        with pytest.raises(ValueError, match="cu_seqlens.*32-bit"):
+            g.prefill(c, None, cu, None, None)
+    with pytest.raises(ValueError, match="n_recent.*32-bit"):
+        g.evict(c, 40, x, None, None, None)
+    with pytest.raises(ValueError, match="budget.*32-bit"):
+        g.evict(c, x, 2, None, None, None)
+
+
+@pytest.mark.parametrize("x", [1 << 64, (1 << 63) + 5])
+def test_arguments_past_64_bits(cache_of, x):
+    g = layer()
+    q = torch.zeros(2, 8, 64, dtype=torch.bfloat16)
+    ws = g.new_workspace(2, device="cpu")
+    with pytest.raises(ValueError, match="max_len.*64-bit"):
+        g.prefill(cache_of(g), q, [0, 1, 2], q, ws, max_len=x)
+    with pytest.raises(ValueError, match="max_len.*64-bit"):
+        g.decode(cache_of(g), q, q, ws, max_len=x)
+    with pytest.raises(ValueError, match="max_total_tokens.*64-bit"):
+        g.new_workspace(x, device="cpu")
+
+
+def test_sizes_are_whole_numbers():
+    for kw in (dict(window=64.0), dict(batch="2"), dict(n_sinks=1.5)):
+        with pytest.raises(TypeError):
+            layer(**kw)
