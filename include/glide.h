@@ -344,12 +344,14 @@ size_t glide_paged_workspace_bytes(const glide_paged_config* cfg, int64_t max_to
 
 /* Appends T_b = cu[b+1] - cu[b] >= 0 tokens to every sequence b and reads out
  * one row per appended token and query head: token i of sequence b is at
- * position lens[b] - T_b + i.  With cache->weights, the weights of the
- * appended tokens start from 0, and the last min(T_b, n_observe) queries of
- * every sequence add theirs,
+ * position lens[b] - T_b + i.  With cache->weights, the last
+ * min(T_b, n_observe) queries of every sequence add theirs,
  *   weights_j += sum over those queries t and the G heads of e^{tau q_t.k_j - lse_t}.
  *   q        device [T][Hq][d]      T = total_tokens, packed by sequence
- *   k, v     device [T][Hkv][d]; both NULL: the tokens are in the cache
+ *   k, v     device [T][Hkv][d]: the call writes them to their pages, their
+ *            weights (if kept) from 0.  Both NULL: the tokens are in the cache,
+ *            and every weight there is added to as it is: who wrote their rows
+ *            has set their weights too
  *   cu_seqlens_host  HOST [B+1], cu[0] = 0, non-decreasing, cu[B] = T; one
  *            sequence's T_b * Hq * d * element bytes < 2^31, else
  *            GLIDE_ERR_UNSUPPORTED
@@ -368,7 +370,8 @@ glide_status glide_paged_prefill(const glide_paged_config* cfg, const glide_page
 /* One token per sequence: appends it (k, v given), at position lens[b] - 1,
  * and reads out its row.  A sequence of lens[b] = 0 has no token: nothing is
  * appended, its row is 0.  With cache->weights every sequence's query adds its
- * weights (the appended token's from 0).
+ * weights (those of a token given by k, v from 0; with k, v NULL to what is
+ * there, as in a prefill).
  *   q device [B][Hq][d];  k, v device [B][Hkv][d], or both NULL
  *   out device [B][Hq][d];  lse device fp32 [B][Hq], or NULL
  * max_len, alignment and errors as for glide_paged_prefill. */

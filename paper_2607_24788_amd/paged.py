@@ -105,11 +105,14 @@ class Paged:
         return torch.empty(n, dtype=torch.uint8, device=device)
 
     def new_pools(self, weights=False, device="cuda"):
-        """K and V pools, and the weights' pool or None.  Not cleared: what no
-        token was written to is never used."""
+        """K and V pools, and the weights' pool or None.  K and V are not
+        cleared: slots that no token was written to are never used.  Weights
+        are 0; tokens that a call appends start from 0, but those that a caller
+        writes into pages of earlier tokens (and reads with k, v None) have the
+        weights that the caller leaves there."""
         shape = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
         k, v = (torch.empty(shape, dtype=self.torch_dtype, device=device) for _ in range(2))
-        return k, v, (torch.empty(shape[:3], dtype=torch.float32, device=device) if weights else None)
+        return k, v, (torch.zeros(shape[:3], dtype=torch.float32, device=device) if weights else None)
 
     def cache(self, k_pool, v_pool, block_table, lens, weights=None):
         """The cache of one layer.  The tensors are used in place: a caller
@@ -183,7 +186,9 @@ class Paged:
                 stream=None):
         """Append k, v (if given) and read out one row per token and head.
         q, out [T][Hq][d], k, v [T][Hkv][d], lse [T][Hq] fp32; the weights of
-        the last n_observe queries of every sequence are added up."""
+        the last n_observe queries of every sequence are added up, from 0 for
+        the tokens of k, v.  Without k, v the tokens are in the cache, and
+        their weights are added to as they are."""
         cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
@@ -199,7 +204,8 @@ class Paged:
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
-        lse [B][Hq] fp32.  On a cache with weights every query adds its."""
+        lse [B][Hq] fp32.  On a cache with weights every query adds its (see
+        prefill)."""
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_decode", cache, stream, qp, kp, vp, _fits("max_len", int(max_len), 64), op, lp, ws, n)

@@ -109,3 +109,19 @@ def test_sizes_are_whole_numbers():
     for kw in (dict(window=64.0), dict(batch="2"), dict(n_sinks=1.5)):
         with pytest.raises(TypeError):
             layer(**kw)
+
+
+@pytest.fixture
+def empty_is_nan():
+    """torch.empty gives NaN, as memory of an earlier use may."""
+    torch.use_deterministic_algorithms(True)
+    yield
+    torch.use_deterministic_algorithms(False)
+
+
+def test_new_weights_are_zero(empty_is_nan):
+    """Tokens that a caller writes itself into new pools add up from 0."""
+    k, v, w = layer().new_pools(weights=True, device="cpu")
+    assert k.isnan().all()      # (the fixture's doing)
+    assert torch.equal(w, torch.zeros(12, 2, 16))
+    assert layer().new_pools(device="cpu")[2] is None
