@@ -384,7 +384,13 @@ glide_status glide_paged_decode(const glide_paged_config* cfg, const glide_paged
  * order: the first n_sinks, the last n_recent, and of the others those of the
  * largest weights (of equal weights the first; a NaN, and a token on a page
  * that is not allocated, counts as the smallest).  Their rows and weights
- * become tokens 0, 1, ... of the sequence in dst_table's pages.
+ * become tokens 0, 1, ... of the sequence in dst_table's pages; a row whose
+ * new page is not allocated is dropped.  A kept token on a page that is not
+ * allocated (a sink, one of the newest, or where fewer than the budget are
+ * allocated) has no row: where its new place is another one and allocated, that
+ * place gets zeros for K, V and the weight, and is a token like any other from
+ * then on, seen with a score of 0.  A budget within the allocated tokens, with
+ * sinks and newest among them, keeps none such.
  *   budget in [1, 2^30], budget >= n_sinks + n_recent;  n_recent >= 0
  *   dst_table  device [B][max_pages]; NULL: in place (block_table itself).
  *              Otherwise its pages of tokens 0 .. min(lens[b], budget) - 1

@@ -213,7 +213,9 @@ class Paged:
     def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):
         """Keep min(len, budget) tokens per sequence and KV head, in place or
         in dst_table's pages.  kept [B][Hkv][budget] int32: their old
-        positions; new_lens [B] int32 (may be the cache's lens)."""
+        positions; new_lens [B] int32 (may be the cache's lens).  A kept token
+        whose page is not allocated becomes a row of zeros (see glide.h): keep
+        the budget within the tokens that are."""
         self._check_cache(cache)
         if cache.weights is None:
             raise ValueError("evict needs a cache with weights")

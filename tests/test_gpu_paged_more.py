@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from .paged_util import Case
-from .test_gpu_paged import run_decode, run_prefill
+from .test_gpu_paged import run_decode, run_evict, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +32,19 @@ def test_tokens_written_by_the_caller(dtype, call):
     else:
         run_decode(case, False)
     assert case.w.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("sinks,recent,budget", [(20, 0, 90), (0, 30, 60), (0, 0, 150), (4, 8, 500)])
+def test_kept_tokens_on_missing_pages(dtype, sinks, recent, budget):
+    """Sinks, newest tokens or all of a budget on pages that are not
+    allocated: rows of zeros where they move, which the next query sees with a
+    score of 0; tokens that stay where they are stay missing."""
+    case = Case(2, 8, 2, 128, 16, [160, 100], None, sinks, dtype=dtype, weights=True, seed=121)
+    for i in (1, 4, 9):
+        case.table[0, i] = -1
+    case.table[1, 5] = case.g.n_pages
+    case.dev_table.copy_(case.table)
+    ref = run_evict(case, budget, recent, alias=True)
+    case.lens_host = list(ref.lens)
+    run_decode(case, False)
