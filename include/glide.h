@@ -295,7 +295,8 @@ glide_status glide_feature_map(const glide_config* cfg, const void* phi_w, const
  * the sinks alone.  What a query does not see (later tokens, tokens before its
  * window, page slots behind a sequence's last token, pages that are not
  * allocated) has no part in its row, whatever bits it holds, NaN and infinities
- * among them.
+ * among them.  A value that is NaN or infinite and seen, at a score above -inf,
+ * makes its element of the row NaN or infinite, however small its weight.
  *
  * A sequence is its cached tokens in order: after an eviction, positions (and
  * with them W, n_sinks) count the tokens that were kept. */

@@ -84,6 +84,10 @@ __device__ __forceinline__ uint32_t rows_of(uint64_t m) {
     x |= ((m >> (r * LPR)) & (LPR == 64 ? ~uint64_t(0) : (uint64_t(1) << (LPR & 63)) - 1)) ? 1u << r : 0u;
   return x;
 }
+// Whether the query at position t sees a cached token at position j.
+__device__ __forceinline__ bool sees(const PagedArgs& a, int32_t j, int32_t t) {
+  return (j <= t) & ((j > t - a.W) | (j < a.ns));
+}
 // Whether a tile of keys at positions j0 .. j1 holds any that one of the rows at
 // t0 .. t1 does not see (and another may).
 __device__ __forceinline__ bool edge_tile(const PagedArgs& a, int32_t j0, int32_t j1, int32_t t0, int32_t t1) {
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
       *vr = (gptr_t)a.vn + at;
     }
   };
-  // the values of key `key` of a tile (position j) that are not finite
+  // the values of key `key` of a tile (position j) that are not finite, for the rows that see it
   auto add_nonfinite = [&](int key, int32_t j, const float* p) {
     float w = -INFINITY;
 #pragma unroll
@@ -230,7 +234,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
     w = __shfl(__builtin_amdgcn_exp2f(w - m), ((key >> 2) & 3) * 16 + n);
     gptr_t kr, vr;
     row_at(true, j, trow[j >> a.shift], &kr, &vr);
-    if (w == 0.f) return;  // not seen
+    if (!sees(a, j, tr)) return;  // (not by the weight, which may underflow)
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
@@ -909,7 +913,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles(PagedArgs a, PagedSeqs s)
             const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
             const gptr_t vr = j >= new0 ? (gptr_t)a.vn + nat + int64_t(j - p0) * a.Hkv * RB
                                         : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
-            if (x == 0.f) continue;  // not seen
+            if (!sees(a, j, tr)) continue;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -1184,7 +1188,7 @@ __global__ __launch_bounds__(256, 2) void attend_shared(PagedArgs a, PagedSeqs s
           const Slot sl = paged_slot(trow, j, a.shift, a.n_pages);
           const gptr_t vr = a.kn && j >= p0 ? (gptr_t)a.vn + ((tok0 + j - p0) * a.Hkv + g) * (D * ES)
                                             : (gptr_t)a.vp + slot_offset(a.vs, sl, g);
-          if (w == 0.f) continue;  // not seen
+          if (!sees(a, j, tr)) continue;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
             float y[4] = {acc[ct][0], acc[ct][1], acc[ct][2], acc[ct][3]};
@@ -1239,7 +1243,7 @@ __device__ __forceinline__ float wave_max(float x) {
 }
 __device__ __forceinline__ float wave_sum(float x) { return lg_sum(dpp_sum_rows<16>(x)); }
 
-// f[u]: what piece lane + 64 u counts in the row's frame.
+// f[u]: what piece lane + 64 u counts in the row's frame; -1: no part in it.
 __device__ __forceinline__ Joined join_frames(const PagedArgs& a, int64_t r, float* f) {
   const int lane = threadIdx.x & 63;
   const float2* ml = reinterpret_cast<const float2*>(a.ml) + r * a.npiece;
@@ -1254,8 +1258,10 @@ __device__ __forceinline__ Joined join_frames(const PagedArgs& a, int64_t r, flo
   j.M = wave_max(j.M);
 #pragma unroll
   for (int u = 0; u < kPagedMaxPieces / 64; ++u) {
-    // (a piece without a part in the row has no acc either)
-    f[u] = x[u].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[u].x - j.M);
+    // a piece without a part in the row has no acc either.  (Not one whose
+    // factor underflows: infinities and NaN among its values show in the row
+    // whatever their weight, as in a row of one piece.)
+    f[u] = x[u].y == 0.f ? -1.f : __builtin_amdgcn_exp2f(x[u].x - j.M);
     j.L += x[u].y * f[u];
   }
   j.L = wave_sum(j.L);
@@ -1280,9 +1286,9 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, int64_t r, const Jo
     for (int i = 0; i < 8; ++i) {
       const int p = i0 + NW * i;
       const float fu = p < 64 ? f[0] : p < 128 ? f[1] : p < 192 ? f[2] : f[3];
-      w[i] = p < a.npiece ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), p & 63)) : 0.f;
+      w[i] = p < a.npiece ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fu), p & 63)) : -1.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[i][e] = w[i] != 0.f ? acc[int64_t(p) * D + e] : 0.f;
+      for (int e = 0; e < E; ++e) y[i][e] = w[i] < 0.f ? 0.f : acc[int64_t(p) * D + e];
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)

@@ -1,10 +1,12 @@
 """Calls of the paged softmax cache beside tests/test_gpu_paged.py's, against
 the same float64 definition (tests/paged_util.py)."""
+import math
+
 import pytest
 import torch
 
 from .paged_util import Case
-from .test_gpu_paged import run_decode, run_evict, run_prefill
+from .test_gpu_paged import nan_like, run_decode, run_evict, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +50,65 @@ def test_kept_tokens_on_missing_pages(dtype, sinks, recent, budget):
     ref = run_evict(case, budget, recent, alias=True)
     case.lens_host = list(ref.lens)
     run_decode(case, False)
+
+
+@pytest.mark.parametrize("dtype,page,Hq,Hkv,new,hist,W", [
+    (BF16, 16, 8, 2, 0, 2100, None), (FP32, 16, 8, 2, 0, 2100, None), (BF16, 1, 4, 4, 0, 700, 500),   # decode
+    (BF16, 16, 8, 2, 7, 2100, None), (BF16, 32, 8, 2, 150, 200, 70),      # attend_tiles
+    (FP32, 16, 8, 2, 7, 1500, None), (FP32, 16, 4, 2, 40, 61, 30),        # attend_rows
+    (BF16, 4, 4, 2, 33, 600, None),
+    (FP32, 64, 32, 16, 450, 100, 300), (BF16, 8, 32, 16, 450, 0, None)])  # attend_shared
+@pytest.mark.parametrize("hint", [True, False])
+def test_nonfinite_values_of_underflowed_weight(dtype, page, Hq, Hkv, new, hist, W, hint):
+    """Infinite and NaN values of tokens that a row sees at a score far below
+    its largest (2^-185 of its weight): their elements are not finite, however
+    a row is split and whatever its tiles hold beside them; all others have
+    what the definition gives."""
+    d, n = 64, hist + max(new, 1)
+    case = Case(1, Hq, Hkv, d, page, [n], W, 3, dtype=dtype, seed=122)
+    T = max(new, 1)
+    q = torch.full((T, Hq, d), 2.0, dtype=dtype)
+    k, v = (case.normal(T, Hkv, d) for _ in range(2))
+    k.mul_(0.01)
+
+    def put(j, key=None, at=0, value=0.0):
+        """Token j: a key of one value, a value element; in the pool or among the new tokens."""
+        for pool, fresh, x in ((case.k, k, key), (case.v, v, value)):
+            row = pool[int(case.table[0, j // page]), :, j % page] if j < hist else fresh[j - hist]
+            if pool is case.k and x is not None:
+                row[:] = x
+            elif pool is case.v:
+                row[:, at] = x
+    for j in range(hist):
+        case.k[int(case.table[0, j // page]), :, j % page] *= 0.01
+    put(2, key=8.0)                       # a sink with a score of 128
+    bad = {(hist - 40, 5, math.inf), (hist - 3, 9, math.nan), (hist + new // 2, 17, -math.inf), (n - 2, 30, math.inf),
+           (n // 2, 33, math.nan), (n // 3, 41, math.inf)}
+    for j, at, x in bad:
+        if j > 2:
+            put(j, at=at, value=x)
+    ref = case.ref()
+    for i in range(T):
+        ref.append(0, n - T + i, k[i], v[i])
+    want = [ref.row(0, n - T + i, q[i], False) for i in range(T)]
+    out, lse = nan_like(T, Hq, d, dtype=dtype), nan_like(T, Hq, dtype=FP32)
+    ws = case.g.new_workspace(T).fill_(0xff)
+    kw = dict(k=k.cuda(), v=v.cuda(), lse=lse, max_len=n if hint else 1)
+    if new:
+        case.g.prefill(case.cache, q.cuda(), [0, T], out, ws, **kw)
+    else:
+        case.g.decode(case.cache, q.cuda(), out, ws, **kw)
+    got, lse = out.cpu().double(), lse.cpu().double()
+    lost = 0
+    for i, (o, z, tol, ztol) in enumerate(want):
+        fine = o.isfinite()
+        lost += int((~fine).sum())
+        assert torch.equal(got[i].isfinite(), fine), f"row {i}"
+        # a weight below 2^-126 of the row's largest is 0 in fp32: n of them, of values below 8, are less than
+        # 2^12 * 2^-126 * 2^3 = 2^-111 (element 0 of the sink's value is 0: that row element holds nothing else)
+        off = (got[i] - o).abs()[fine] > tol[fine] + 2.0 ** -111
+        assert not off.any(), f"row {i}: {int(off.sum())} elements"
+        seen = z.isfinite()
+        assert ((lse[i] - z).abs()[seen] <= ztol[seen]).all(), f"row {i}: lse"
+    assert lost > 0
+    case.pools_equal(ref)
