@@ -1429,7 +1429,7 @@ __global__ __launch_bounds__(256) void prefill_weights(PagedArgs a, PagedSeqs s,
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) gload_frag<false>(kf[t][kk], kr + (32 * kk + 8 * lg) * ES);
     }
-    // positions of this lane's keys; -1 (never seen): not there
+    // positions of this lane's keys; not there: behind every query
     int32_t j[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)

@@ -112,3 +112,24 @@ def test_nonfinite_values_of_underflowed_weight(dtype, page, Hq, Hkv, new, hist,
         assert ((lse[i] - z).abs()[seen] <= ztol[seen]).all(), f"row {i}: lse"
     assert lost > 0
     case.pools_equal(ref)
+
+
+@pytest.mark.parametrize("past", [0, 8])
+def test_rows_of_a_page_far_apart(past):
+    """Pools stored [slot][page][head][d] whose slots are 2^26 elements apart,
+    the most that a prefill's 32-bit offsets within a page take (15 rows:
+    15 * 2^27 bytes and a row, below 2^31), and 8 more: another kernel."""
+    case = Case(2, 8, 2, 128, 16, [150, 77], 90, 3, weights=True, seed=123)
+    g, S = case.g, (1 << 26) + past
+    shape = case.k.shape
+    pools = []
+    for x in (case.k, case.v):
+        far = torch.empty(15 * S + shape[0] * shape[1] * shape[3], dtype=BF16, device="cuda").as_strided(
+            shape, (shape[1] * shape[3], shape[3], S, 1))
+        far.copy_(x)
+        pools.append(far)
+    case.k, case.v = pools
+    case.cache = g.cache(*pools, case.dev_table, case.lens, case.w)
+    run_prefill(case, [70, 33], 9)
+    run_decode(case, True)
+    run_evict(case, 60, 20)
