@@ -160,7 +160,8 @@ class Paged:
 
     def _rows(self, cache, q, k, v, out, lse, T):
         """Pointers of a call over T rows of queries, checked."""
-        self._check_cache(cache)
+        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
         dev, dt = cache._dev, self.torch_dtype
         nq, nkv = T * self.n_q_heads * self.head_dim, T * self.n_kv_heads * self.head_dim
         if (k is None) != (v is None):
@@ -192,9 +193,12 @@ class Paged:
         cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
-        _fits("cu_seqlens' least", min(cu))
-        _fits("cu_seqlens' largest", max(cu))
-        n_observe, max_len = _fits("n_observe", int(n_observe)), _fits("max_len", int(max_len), 64)
+        n_observe, max_len = int(n_observe), int(max_len)
+        if min(cu) < 0 or max(cu) >> 31 or n_observe >> 31 or max_len >> 63:   # (one test on a short call's path)
+            for x in cu:
+                _fits("cu_seqlens entry", x)
+            _fits("n_observe", n_observe)
+            _fits("max_len", max_len, 64)
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, max(cu[-1], 0))
         if n_observe and cache.weights is None:
             raise ValueError("n_observe needs a cache with weights")
@@ -206,9 +210,12 @@ class Paged:
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
         lse [B][Hq] fp32.  On a cache with weights every query adds its (see
         prefill)."""
+        max_len = int(max_len)
+        if max_len >> 63:
+            _fits("max_len", max_len, 64)
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_decode", cache, stream, qp, kp, vp, _fits("max_len", int(max_len), 64), op, lp, ws, n)
+        self._call("glide_paged_decode", cache, stream, qp, kp, vp, max_len, op, lp, ws, n)
 
     def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):
         """Keep min(len, budget) tokens per sequence and KV head, in place or
@@ -216,10 +223,14 @@ class Paged:
         positions; new_lens [B] int32 (may be the cache's lens).  A kept token
         whose page is not allocated becomes a row of zeros (see glide.h): keep
         the budget within the tokens that are."""
-        self._check_cache(cache)
+        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
         if cache.weights is None:
             raise ValueError("evict needs a cache with weights")
-        budget, n_recent = _fits("budget", int(budget)), _fits("n_recent", int(n_recent))
+        budget, n_recent = int(budget), int(n_recent)
+        if budget >> 31 or n_recent >> 31:
+            _fits("budget", budget)
+            _fits("n_recent", n_recent)
         dev = cache._dev
         kp = _tensor("kept", kept, dev, torch.int32, self.batch * self.n_kv_heads * max(budget, 0))
         lp = _tensor("new_lens", new_lens, dev, torch.int32, self.batch)
