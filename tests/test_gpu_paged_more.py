@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from .paged_util import Case
+from .paged_util import EPS16, EPS32, Case
 from .test_gpu_paged import nan_like, run_decode, run_evict, run_prefill
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +133,45 @@ def test_rows_of_a_page_far_apart(past):
     run_prefill(case, [70, 33], 9)
     run_decode(case, True)
     run_evict(case, 60, 20)
+
+
+@pytest.mark.parametrize("dtype,page,Hq,Hkv,new,hist", [
+    (BF16, 16, 8, 2, 0, 700), (FP32, 16, 8, 2, 0, 700),                              # decode
+    (BF16, 16, 8, 2, 150, 90), (FP32, 16, 4, 2, 40, 61), (FP32, 64, 32, 16, 450, 0)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_2_to_28(dtype, page, Hq, Hkv, new, hist, sign):
+    """Scores near the ends of their range: one token that carries all the
+    weight, or equal scores far below 0.  q, k and their products are powers
+    of two, so scores carry no error but the scale's (tau log2(e), rounded)."""
+    d, T = 64, max(new, 1)
+    n = hist + T
+    case = Case(1, Hq, Hkv, d, page, [n], None, 0, dtype=dtype, seed=124)
+    q = torch.full((T, Hq, d), 2.0 ** 11, dtype=dtype)
+    k = torch.zeros(T, Hkv, d, dtype=dtype)
+    v = case.normal(T, Hkv, d)
+    case.k.zero_()
+    hot = 1 if hist else 0
+    if sign > 0:
+        (case.k[int(case.table[0, 0]), :, 1] if hist else k[0])[:] = 2.0 ** 14
+    else:
+        case.k.fill_(-2.0 ** 14)
+        k.fill_(-2.0 ** 14)
+    out, lse = nan_like(T, Hq, d, dtype=dtype), nan_like(T, Hq, dtype=FP32)
+    kw = dict(k=k.cuda(), v=v.cuda(), lse=lse)
+    if new:
+        case.g.prefill(case.cache, q.cuda(), [0, T], out, case.g.new_workspace(T), **kw)
+    else:
+        case.g.decode(case.cache, q.cuda(), out, case.g.new_workspace(T), **kw)
+    ref = case.ref()
+    vs = torch.stack([ref.v[ref.slot(0, j)[0], :, ref.slot(0, j)[1]] for j in range(n)])     # [n][Hkv][d]
+    G = Hq // Hkv
+    for i in range(T):
+        m = hist + i + 1
+        seen = vs[hot:hot + 1] if sign > 0 else vs[:m]
+        want, size = seen.mean(0).repeat_interleave(G, 0), seen.abs().mean(0).repeat_interleave(G, 0)
+        # sums of m products in fp32, exponentials and a division; in bf16 two roundings (weights, output) more
+        tol = size * ((m + 16) * EPS32 + (2 * EPS16 * (1 + EPS16) if dtype == BF16 else 0.0))
+        assert ((out[i].cpu().double() - want).abs() <= tol).all(), f"row {i}"
+        z = sign * 2.0 ** 28 + (0.0 if sign > 0 else math.log(m))
+        # tau and tau log2(e) rounded, the score, the sum with the logarithm, and ln 2 and its product: 8 half steps
+        assert ((lse[i].cpu().double() - z).abs() <= 8 * EPS32 * abs(z)).all(), f"row {i}: lse"
