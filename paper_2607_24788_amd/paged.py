@@ -193,8 +193,8 @@ class Paged:
         cu = list(map(int, cu_seqlens))
         if len(cu) != self.batch + 1:
             raise ValueError("cu_seqlens needs batch + 1 entries")
-        n_observe, max_len = int(n_observe), int(max_len)
-        if min(cu) < 0 or max(cu) >> 31 or n_observe >> 31 or max_len >> 63:   # (one test on a short call's path)
+        n_observe, max_len, cu_arg = int(n_observe), int(max_len), self._cu(*cu)
+        if cu_arg[:] != cu or n_observe >> 31 or max_len >> 63:   # (one test on a short call's path)
             for x in cu:
                 _fits("cu_seqlens entry", x)
             _fits("n_observe", n_observe)
@@ -203,7 +203,7 @@ class Paged:
         if n_observe and cache.weights is None:
             raise ValueError("n_observe needs a cache with weights")
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_prefill", cache, stream, qp, kp, vp, self._cu(*cu), cu[-1],
+        self._call("glide_paged_prefill", cache, stream, qp, kp, vp, cu_arg, cu[-1],
                    n_observe, max_len, op, lp, ws, n)
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
