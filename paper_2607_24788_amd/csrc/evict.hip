@@ -246,7 +246,9 @@ __global__ __launch_bounds__(256) void evict_copy(EvictArgs a) {
 // and stay in order, so a row read in a step (all of its rows before any is
 // written) is never behind a row written in a step before: one barrier per
 // step of up to 1024 rows.  A workgroup moves 128 bytes of every K, or V, row
-// of a (sequence, KV head), or its weights.
+// of a (sequence, KV head), or its weights.  32 sequences of 16K..32K tokens to
+// 4096 (8 heads of 128, bf16) 230 us = 4.7 TB/s; one of 32K to 16K 102 us (1.3
+// TB/s): the chain kept -> table -> row -> barrier of 40 workgroups.
 __global__ __launch_bounds__(1024) void evict_move(EvictArgs a) {
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
   const int slabs = a.d * a.esize / 128, what = blockIdx.y / slabs;
