@@ -414,6 +414,86 @@ glide_status glide_paged_evict(const glide_paged_config* cfg, const glide_paged_
                                int32_t* kept, int32_t* new_lens, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Filling a paged cache with the position rotation applied on the way.
+ *
+ * The first rot_dim elements of a row of q or k at position p are rotated in
+ * pairs (x, y), pair i by the angle a = p freqs[i]:
+ *   (x, y) -> (x cos a - y sin a, y cos a + x sin a)
+ * Pair i is elements (i, i + rot_dim / 2), or (2i, 2i + 1) with interleaved.
+ * Angles are taken in fp64 and as a part of a turn, so that far positions lose
+ * nothing; each element is rounded once, to cfg->dtype. */
+typedef struct {
+  const float* freqs;       /* device [rot_dim / 2]: radians per position, 16-byte aligned */
+  const int32_t* positions; /* device [total_tokens], or NULL: each token's position in the cache
+                               (an evicted cache's positions run on past it) */
+  int32_t rot_dim;          /* a multiple of 16 in [0, d]; 0: nothing is rotated */
+  int32_t interleaved;      /* 0 or 1 */
+} glide_rotation;
+
+/* Writes T_b = cu[b+1] - cu[b] >= 0 new tokens' rows to the pages of every
+ * sequence b, at positions lens[b] - T_b .. lens[b] - 1: k rotated, v as it is
+ * (their weights, where kept, 0).  The tokens are then in the cache, for a
+ * glide_paged_prefill or _decode with k, v NULL.  What has no page is dropped.
+ *   rotation  NULL: nothing is rotated
+ *   q, q_out  device [T][Hq][d]: the queries, and where they go rotated (may be
+ *             q itself); both NULL: no queries
+ *   k, v      device [T][Hkv][d]
+ *   cu_seqlens_host  as for glide_paged_prefill
+ *   bounds    device [n_pages][Hkv][2][d] in cfg->dtype, or NULL: per page, the
+ *             least and the largest of its keys by element, as the cache holds
+ *             them (NaN left out), brought up to date with the new keys; those
+ *             of a page whose first token is not among them are added to (they
+ *             are of earlier appends, or of glide_paged_bounds)
+ * Device pointers 16-byte aligned (positions: 4). */
+glide_status glide_paged_append(const glide_paged_config* cfg, const glide_paged_cache* cache,
+                                const glide_rotation* rotation, const void* q, const void* k, const void* v,
+                                const int32_t* cu_seqlens_host, int64_t total_tokens, void* q_out, void* bounds,
+                                void* stream);
+
+/* The bounds of every page of the sequences from the keys in the cache: where
+ * rows were written otherwise, and after an eviction.  max_len: the caller's
+ * upper bound of lens (0: the table's capacity); a wrong one costs time only. */
+glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged_cache* cache, int64_t max_len,
+                                void* bounds, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A paged cache held in 4 bits: 17/64 of a bf16 cache's bytes.
+ *
+ * 32 consecutive elements of a row share a factor 2^e, e the least integer in
+ * [-124, 125] with max |x| <= 7 * 2^e.  An element is held as the nearest of
+ *   0, 1/2, 1, 3/2, 2, 3, 4, 6   (ties to the even place in this list)
+ * to |x| / 2^e, with its sign: off by at most a quarter of 2^e below 2 * 2^e,
+ * by 2^e at most.  NaN is held as 0, an infinity (and what lies beyond
+ * 7 * 2^125) as 6 * 2^125: the cache holds finite numbers only, each of them a
+ * bf16 number, so that attention over it rounds no key and no value.
+ * A code is the place in the list in bits 0..2 and the sign in bit 3; element
+ * 2i of a row is in bits 0..3 of its byte i, 2i + 1 in bits 4..7.  A scale is
+ * the byte e + 127 (any other byte than 3 .. 252 counts as the nearest of
+ * them).  K and V are held alike, each pool contiguous:
+ *   codes  [n_pages][Hkv][page_size][d/2],  scales  [n_pages][Hkv][page_size][d/32]
+ * block_table and lens as in glide_paged_cache.  cfg->dtype is the type of q,
+ * k, v and out. */
+typedef struct {
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales; /* device, 16-byte aligned */
+  const int32_t* block_table;
+  const int32_t* lens;
+} glide_nibble_cache;
+
+/* As glide_paged_append: k (after its rotation) and v are rounded to 4 bits.
+ * Pairs that are not interleaved: rot_dim a multiple of 64, else
+ * GLIDE_ERR_UNSUPPORTED. */
+glide_status glide_nibble_append(const glide_paged_config* cfg, const glide_nibble_cache* cache,
+                                 const glide_rotation* rotation, const void* q, const void* k, const void* v,
+                                 const int32_t* cu_seqlens_host, int64_t total_tokens, void* q_out, void* stream);
+
+/* The values that the cache holds of the last T_b tokens of every sequence, as
+ * rows k_out, v_out [T][Hkv][d] in cfg->dtype (exact); zeros where a token has
+ * no page. */
+glide_status glide_nibble_read(const glide_paged_config* cfg, const glide_nibble_cache* cache,
+                               const int32_t* cu_seqlens_host, int64_t total_tokens, void* k_out, void* v_out,
+                               void* stream);
+
 /* Static description of a status code. */
 const char* glide_status_string(glide_status s);
 

@@ -1,0 +1,169 @@
+// C ABI of the calls that fill a paged cache: argument validation (on the host,
+// before the first HIP call) and launch planning.
+#include "append.h"
+#include "paged_host.h"
+
+using namespace glide;
+
+namespace {
+
+// The sequences of one launch, from b0 on; *units: workgroups per KV head.
+// per(T): those of a sequence of T new tokens.
+template <typename F>
+int next_launch(const glide_paged_config* c, const int32_t* cu, int b0, PagedSeqs* t, F per) {
+  memset(t, 0, sizeof(*t));
+  t->seq0 = b0;
+  int b1 = b0;
+  while (b1 < c->batch && b1 - b0 < kMaxSeqPerLaunch &&
+         (b1 == b0 || int64_t(cu[b1 + 1] - cu[b0]) * c->n_q_heads <= kMaxLaunchRows)) {
+    const int i = b1 - b0;
+    t->start[i] = cu[b1];
+    t->len[i] = cu[b1 + 1] - cu[b1];
+    t->tile0[i + 1] = t->tile0[i] + (t->len[i] ? int32_t(per(int64_t(t->len[i]))) : 0);
+    ++b1;
+  }
+  t->nseq = b1 - b0;
+  return b1;
+}
+
+glide_status check_rotation(const glide_paged_config* c, const glide_rotation* r, bool four) {
+  if (!r) return GLIDE_OK;
+  if (r->rot_dim < 0 || r->rot_dim > c->head_dim || r->rot_dim % 16) return GLIDE_ERR_INVALID;
+  if (r->interleaved != 0 && r->interleaved != 1) return GLIDE_ERR_INVALID;
+  if (four && !r->interleaved && r->rot_dim % 64) return GLIDE_ERR_UNSUPPORTED;
+  if (r->rot_dim && !r->freqs) return GLIDE_ERR_NULL;
+  if (!aligned(r->freqs, 16) || !aligned(r->positions, 4)) return GLIDE_ERR_ALIGN;
+  return GLIDE_OK;
+}
+
+void fill_append(const glide_paged_config* c, const int32_t* table, const int32_t* lens, AppendArgs* a) {
+  memset(a, 0, sizeof(*a));
+  a->table = table;
+  a->lens = lens;
+  a->B = c->batch;
+  a->Hq = c->n_q_heads;
+  a->Hkv = c->n_kv_heads;
+  a->G = c->n_q_heads / c->n_kv_heads;
+  a->n_pages = c->n_pages;
+  a->max_pages = c->max_pages;
+  a->shift = __builtin_ctz(uint32_t(c->page_size));
+  a->cap = capacity(c);
+}
+void fill_pools(const glide_paged_config* c, const glide_paged_cache* k, AppendArgs* a) {
+  a->kp = static_cast<char*>(k->k);
+  a->vp = static_cast<char*>(k->v);
+  a->wp = k->weights;
+  for (int i = 0; i < 3; ++i) {
+    a->ks[i] = k->k_strides[i] * esize(c);
+    a->vs[i] = k->v_strides[i] * esize(c);
+  }
+}
+
+// An append, its cache checked and filled in.
+glide_status append(const glide_paged_config* c, const glide_rotation* rot, const void* q, const void* k,
+                    const void* v, const int32_t* cu, int64_t total, void* q_out, AppendArgs a, bool four,
+                    void* stream) {
+  glide_status s = check_rotation(c, rot, four);
+  if (s != GLIDE_OK) return s;
+  s = check_cu(c, cu, total);
+  if (s != GLIDE_OK) return s;
+  if (total == 0) return GLIDE_OK;
+  if (!k || !v || !q != !q_out) return GLIDE_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16)) return GLIDE_ERR_ALIGN;
+  a.q = static_cast<const char*>(q);
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.qo = static_cast<char*>(q_out);
+  if (rot) {
+    a.rot = rot->rot_dim;
+    a.freqs = rot->freqs;
+    a.pos = rot->positions;
+  }
+  a.unit = a.bounds ? a.shift : __builtin_ctz(uint32_t(kAppendTokens));
+  for (int b0 = 0; b0 < c->batch;) {
+    PagedSeqs t;
+    // positions p0 .. p0 + T - 1 lie in so many units, wherever p0 is
+    b0 = next_launch(c, cu, b0, &t, [&](int64_t T) { return ((T + (int64_t(1) << a.unit) - 2) >> a.unit) + 1; });
+    s = hip_status(launch_append(a, t, c->head_dim, c->dtype, four, rot && rot->interleaved, hipStream_t(stream)));
+    if (s != GLIDE_OK) return s;
+  }
+  return GLIDE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+glide_status glide_paged_append(const glide_paged_config* cfg, const glide_paged_cache* cache,
+                                const glide_rotation* rotation, const void* q, const void* k, const void* v,
+                                const int32_t* cu_seqlens_host, int64_t total_tokens, void* q_out, void* bounds,
+                                void* stream) {
+  glide_status s = check_cfg(cfg);
+  if (s != GLIDE_OK) return s;
+  s = check_cache(cfg, cache);
+  if (s != GLIDE_OK) return s;
+  if (!aligned(bounds, 16)) return GLIDE_ERR_ALIGN;
+  AppendArgs a;
+  fill_append(cfg, cache->block_table, cache->lens, &a);
+  fill_pools(cfg, cache, &a);
+  a.bounds = static_cast<char*>(bounds);
+  return append(cfg, rotation, q, k, v, cu_seqlens_host, total_tokens, q_out, a, false, stream);
+}
+
+glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged_cache* cache, int64_t max_len,
+                                void* bounds, void* stream) {
+  glide_status s = check_cfg(cfg);
+  if (s != GLIDE_OK) return s;
+  s = check_cache(cfg, cache);
+  if (s != GLIDE_OK) return s;
+  if (!bounds) return GLIDE_ERR_NULL;
+  if (max_len < 0) return GLIDE_ERR_INVALID;
+  if (!aligned(bounds, 16)) return GLIDE_ERR_ALIGN;
+  AppendArgs a;
+  fill_append(cfg, cache->block_table, cache->lens, &a);
+  fill_pools(cfg, cache, &a);
+  a.bounds = static_cast<char*>(bounds);
+  const int64_t keys = max_len ? std::min<int64_t>(max_len, capacity(cfg)) : capacity(cfg);
+  return hip_status(launch_page_bounds(a, keys, cfg->head_dim, cfg->dtype, hipStream_t(stream)));
+}
+
+glide_status glide_nibble_append(const glide_paged_config* cfg, const glide_nibble_cache* cache,
+                                 const glide_rotation* rotation, const void* q, const void* k, const void* v,
+                                 const int32_t* cu_seqlens_host, int64_t total_tokens, void* q_out, void* stream) {
+  glide_status s = check_cfg(cfg);
+  if (s != GLIDE_OK) return s;
+  s = check_cache4(cache);
+  if (s != GLIDE_OK) return s;
+  AppendArgs a;
+  fill_append(cfg, cache->block_table, cache->lens, &a);
+  a.p4 = {cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales};
+  return append(cfg, rotation, q, k, v, cu_seqlens_host, total_tokens, q_out, a, true, stream);
+}
+
+glide_status glide_nibble_read(const glide_paged_config* cfg, const glide_nibble_cache* cache,
+                               const int32_t* cu_seqlens_host, int64_t total_tokens, void* k_out, void* v_out,
+                               void* stream) {
+  glide_status s = check_cfg(cfg);
+  if (s != GLIDE_OK) return s;
+  s = check_cache4(cache);
+  if (s != GLIDE_OK) return s;
+  s = check_cu(cfg, cu_seqlens_host, total_tokens);
+  if (s != GLIDE_OK) return s;
+  if (total_tokens == 0) return GLIDE_OK;
+  if (!k_out || !v_out) return GLIDE_ERR_NULL;
+  if (!aligned(k_out, 16) || !aligned(v_out, 16)) return GLIDE_ERR_ALIGN;
+  AppendArgs a;
+  fill_append(cfg, cache->block_table, cache->lens, &a);
+  a.p4 = {cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales};
+  a.unit = __builtin_ctz(uint32_t(kAppendTokens));
+  for (int b0 = 0; b0 < cfg->batch;) {
+    PagedSeqs t;
+    b0 = next_launch(cfg, cu_seqlens_host, b0, &t, [&](int64_t T) { return (T + kAppendTokens - 1) / kAppendTokens; });
+    s = hip_status(launch_read4(a, t, static_cast<char*>(k_out), static_cast<char*>(v_out), cfg->head_dim, cfg->dtype,
+                                hipStream_t(stream)));
+    if (s != GLIDE_OK) return s;
+  }
+  return GLIDE_OK;
+}
+
+}  // extern "C"

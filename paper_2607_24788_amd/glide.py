@@ -31,7 +31,7 @@ DECODE_SCRATCH_BYTES = 16 << 20
 EXPORTS = ["glide_state_bytes", "glide_state_layout", "glide_workspace_bytes", "glide_state_init",
            "glide_prefill", "glide_decode_step", "glide_decode_step_noalloc", "glide_state_flush", "glide_feature_map",
            "glide_status_string", "glide_paged_workspace_bytes", "glide_paged_prefill", "glide_paged_decode",
-           "glide_paged_evict"]
+           "glide_paged_evict", "glide_paged_append", "glide_paged_bounds", "glide_nibble_append", "glide_nibble_read"]
 
 
 class GlideError(RuntimeError):
@@ -71,6 +71,15 @@ class PagedCacheArg(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weights", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class Paged4CacheArg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales", "block_table", "lens")]
 
 
 _lib = None
@@ -121,6 +130,15 @@ def load_library(path=None):
     lib.glide_paged_evict.argtypes = [pcfg, pcache, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp, ctypes.c_size_t,
                                       vp]
     lib.glide_paged_evict.restype = ctypes.c_int
+    rotp, p4cache, cup = ctypes.POINTER(Rotation), ctypes.POINTER(Paged4CacheArg), ctypes.POINTER(ctypes.c_int32)
+    lib.glide_paged_append.argtypes = [pcfg, pcache, rotp, vp, vp, vp, cup, ctypes.c_int64, vp, vp, vp]
+    lib.glide_paged_append.restype = ctypes.c_int
+    lib.glide_paged_bounds.argtypes = [pcfg, pcache, ctypes.c_int64, vp, vp]
+    lib.glide_paged_bounds.restype = ctypes.c_int
+    lib.glide_nibble_append.argtypes = [pcfg, p4cache, rotp, vp, vp, vp, cup, ctypes.c_int64, vp, vp]
+    lib.glide_nibble_append.restype = ctypes.c_int
+    lib.glide_nibble_read.argtypes = [pcfg, p4cache, cup, ctypes.c_int64, vp, vp, vp]
+    lib.glide_nibble_read.restype = ctypes.c_int
     lib.glide_status_string.argtypes = [ctypes.c_int]
     lib.glide_status_string.restype = ctypes.c_char_p
     if path is None:

@@ -41,6 +41,36 @@ def _tensor(name, t, device, dtype, numel):
     raise ValueError(f"{name} holds {t.numel()} elements, at least {numel} needed")
 
 
+def _cu_arg(g, cu_seqlens):
+    """cu_seqlens as the library's array, and its last entry."""
+    cu = list(map(int, cu_seqlens))
+    if len(cu) != g.batch + 1:
+        raise ValueError("cu_seqlens needs batch + 1 entries")
+    arg = g._cu(*cu)
+    if arg[:] != cu:
+        for x in cu:
+            _fits("cu_seqlens entry", x)
+    return arg, cu[-1]
+
+
+def _rotation(freqs, interleaved, positions, device, T):
+    """The library's struct of a rotation, or None where there is none."""
+    at = None if positions is None else _tensor("positions", positions, device, torch.int32, T)
+    if freqs is None:
+        return None
+    return ctypes.byref(glide.Rotation(_tensor("freqs", freqs, device, torch.float32, 0), at,
+                                       _fits("2 * freqs", 2 * freqs.numel()), int(bool(interleaved))))
+
+
+def _append_rows(g, dev, q, k, v, q_out, T):
+    """Pointers of an append of T tokens, checked."""
+    dt, nq, nkv = g.torch_dtype, T * g.n_q_heads * g.head_dim, T * g.n_kv_heads * g.head_dim
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    return (None if q is None else _tensor("q", q, dev, dt, nq), _tensor("k", k, dev, dt, nkv),
+            _tensor("v", v, dev, dt, nkv), None if q is None else _tensor("q_out", q_out, dev, dt, nq))
+
+
 class PagedCache:
     """The cache of one layer: its tensors, the struct that names them to the
     library, and the geometry that they were checked for.  Made by
@@ -205,6 +235,42 @@ class Paged:
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_prefill", cache, stream, qp, kp, vp, cu_arg, cu[-1],
                    n_observe, max_len, op, lp, ws, n)
+
+    def append(self, cache, k, v, cu_seqlens, q=None, q_out=None, freqs=None, interleaved=False, positions=None,
+               bounds=None, stream=None):
+        """Write k, v [T][Hkv][d] to their pages, k rotated, and q [T][Hq][d]
+        rotated to q_out (which may be q).  freqs: fp32 [rot_dim / 2], radians
+        per position (None: no rotation); positions: int32 [T] (None: those in
+        the cache).  bounds (``new_bounds``): the pages' least and largest keys,
+        brought up to date.  prefill, decode and sparse then take the tokens
+        without k, v."""
+        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
+        dev = cache._dev
+        cu_arg, T = _cu_arg(self, cu_seqlens)
+        rot = _rotation(freqs, interleaved, positions, dev, T)
+        qp, kp, vp, op = _append_rows(self, dev, q, k, v, q_out, max(T, 0))
+        bp = None if bounds is None else self._bounds(cache, bounds)
+        self._call("glide_paged_append", cache, stream, rot, qp, kp, vp, cu_arg, T, op, bp)
+
+    def new_bounds(self, device="cuda"):
+        """Room for the least and the largest key elements of every page: not
+        cleared (``append`` sets a page's with its first token, ``page_bounds``
+        all)."""
+        return torch.empty((self.n_pages, self.n_kv_heads, 2, self.head_dim), dtype=self.torch_dtype, device=device)
+
+    def _bounds(self, cache, bounds):
+        return _tensor("bounds", bounds, cache._dev, self.torch_dtype,
+                       2 * self.n_pages * self.n_kv_heads * self.head_dim)
+
+    def page_bounds(self, cache, bounds, max_len=0, stream=None):
+        """The bounds of every page of the sequences from the keys in the
+        cache: where they were written without ``append``, and after an
+        eviction."""
+        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
+        max_len = _fits("max_len", int(max_len), 64)
+        self._call("glide_paged_bounds", cache, stream, max_len, self._bounds(cache, bounds))
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
