@@ -473,7 +473,7 @@ glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged
  * them).  K and V are held alike, each pool contiguous:
  *   codes  [n_pages][Hkv][page_size][d/2],  scales  [n_pages][Hkv][page_size][d/32]
  * block_table and lens as in glide_paged_cache.  cfg->dtype is the type of q,
- * k, v and out. */
+ * k, v and out.  n_pages * Hkv * page_size <= 2^32, else GLIDE_ERR_UNSUPPORTED. */
 typedef struct {
   uint8_t *k_codes, *k_scales, *v_codes, *v_scales; /* device, 16-byte aligned */
   const int32_t* block_table;
@@ -493,6 +493,26 @@ glide_status glide_nibble_append(const glide_paged_config* cfg, const glide_nibb
 glide_status glide_nibble_read(const glide_paged_config* cfg, const glide_nibble_cache* cache,
                                const int32_t* cu_seqlens_host, int64_t total_tokens, void* k_out, void* v_out,
                                void* stream);
+
+/* Workspace bytes that serve glide_nibble_decode, and glide_nibble_prefill up to
+ * max_total_tokens packed tokens; as glide_paged_workspace_bytes. */
+size_t glide_nibble_workspace_bytes(const glide_paged_config* cfg, int64_t max_total_tokens);
+
+/* Reads out one row per query and head, over the values that the cache holds:
+ * T_b = cu[b+1] - cu[b] queries of every sequence b, the i-th at position
+ * lens[b] - T_b + i.  Their tokens are in the cache (glide_nibble_append).
+ * What a query sees, the order of q, out and lse, max_len and errors as for
+ * glide_paged_prefill.  Rows in GLIDE_F32 are exact to fp32 (queries and
+ * weights are split, not rounded). */
+glide_status glide_nibble_prefill(const glide_paged_config* cfg, const glide_nibble_cache* cache, const void* q,
+                                  const int32_t* cu_seqlens_host, int64_t total_tokens, int64_t max_len, void* out,
+                                  float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One query per sequence, at position lens[b] - 1, whose token is in the cache.
+ * q, out device [B][Hq][d]; otherwise as glide_nibble_prefill. */
+glide_status glide_nibble_decode(const glide_paged_config* cfg, const glide_nibble_cache* cache, const void* q,
+                                 int64_t max_len, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream);
 
 /* Static description of a status code. */
 const char* glide_status_string(glide_status s);

@@ -7,25 +7,6 @@ using namespace glide;
 
 namespace {
 
-// The sequences of one launch, from b0 on; *units: workgroups per KV head.
-// per(T): those of a sequence of T new tokens.
-template <typename F>
-int next_launch(const glide_paged_config* c, const int32_t* cu, int b0, PagedSeqs* t, F per) {
-  memset(t, 0, sizeof(*t));
-  t->seq0 = b0;
-  int b1 = b0;
-  while (b1 < c->batch && b1 - b0 < kMaxSeqPerLaunch &&
-         (b1 == b0 || int64_t(cu[b1 + 1] - cu[b0]) * c->n_q_heads <= kMaxLaunchRows)) {
-    const int i = b1 - b0;
-    t->start[i] = cu[b1];
-    t->len[i] = cu[b1 + 1] - cu[b1];
-    t->tile0[i + 1] = t->tile0[i] + (t->len[i] ? int32_t(per(int64_t(t->len[i]))) : 0);
-    ++b1;
-  }
-  t->nseq = b1 - b0;
-  return b1;
-}
-
 glide_status check_rotation(const glide_paged_config* c, const glide_rotation* r, bool four) {
   if (!r) return GLIDE_OK;
   if (r->rot_dim < 0 || r->rot_dim > c->head_dim || r->rot_dim % 16) return GLIDE_ERR_INVALID;
@@ -132,7 +113,7 @@ glide_status glide_nibble_append(const glide_paged_config* cfg, const glide_nibb
                                  const int32_t* cu_seqlens_host, int64_t total_tokens, void* q_out, void* stream) {
   glide_status s = check_cfg(cfg);
   if (s != GLIDE_OK) return s;
-  s = check_cache4(cache);
+  s = check_cache4(cfg, cache);
   if (s != GLIDE_OK) return s;
   AppendArgs a;
   fill_append(cfg, cache->block_table, cache->lens, &a);
@@ -145,7 +126,7 @@ glide_status glide_nibble_read(const glide_paged_config* cfg, const glide_nibble
                                void* stream) {
   glide_status s = check_cfg(cfg);
   if (s != GLIDE_OK) return s;
-  s = check_cache4(cache);
+  s = check_cache4(cfg, cache);
   if (s != GLIDE_OK) return s;
   s = check_cu(cfg, cu_seqlens_host, total_tokens);
   if (s != GLIDE_OK) return s;

@@ -110,6 +110,8 @@ hipError_t launch_paged_prefill(const PagedArgs& a, const PagedSeqs& s, int d, i
                                 hipStream_t stream);
 hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs& s, int n_observe, int64_t keys, int d, int dtype,
                                 hipStream_t stream);
+// Rows row0 .. row0 + rows - 1 of a call in a.npiece > 1 pieces: their records joined.
+hipError_t launch_paged_join(const PagedArgs& a, int64_t row0, int64_t rows, int d, int dtype, hipStream_t stream);
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t stream);
 
 // A row of zeros (device memory): what is read in place of a row that has no

@@ -1534,6 +1534,12 @@ hipError_t launch_paged_prefill(const PagedArgs& a, const PagedSeqs& s, int d, i
   return d == 128 ? prefill_t<float, 128>(a, s, tile_rows, stream) : prefill_t<float, 64>(a, s, tile_rows, stream);
 }
 
+hipError_t launch_paged_join(const PagedArgs& a, int64_t row0, int64_t rows, int d, int dtype, hipStream_t stream) {
+  if (dtype == GLIDE_BF16)
+    return d == 128 ? join_t<bf16_t, 128>(a, row0, rows, stream) : join_t<bf16_t, 64>(a, row0, rows, stream);
+  return d == 128 ? join_t<float, 128>(a, row0, rows, stream) : join_t<float, 64>(a, row0, rows, stream);
+}
+
 hipError_t launch_paged_weights(const PagedArgs& a, const PagedSeqs& s, int n_observe, int64_t keys, int d, int dtype,
                                 hipStream_t stream) {
   const dim3 grid(s.nseq * a.Hkv, uint32_t(std::min<int64_t>((keys + 127) / 128, 4096)));

@@ -55,12 +55,14 @@ glide_status check_cache(const glide_paged_config* c, const glide_paged_cache* k
   return GLIDE_OK;
 }
 
-glide_status check_cache4(const glide_nibble_cache* k) {
+glide_status check_cache4(const glide_paged_config* c, const glide_nibble_cache* k) {
   if (!k || !k->k_codes || !k->k_scales || !k->v_codes || !k->v_scales || !k->block_table || !k->lens)
     return GLIDE_ERR_NULL;
   if (!aligned(k->k_codes, 16) || !aligned(k->v_codes, 16) || !aligned(k->k_scales, 16) || !aligned(k->v_scales, 16) ||
       !aligned(k->block_table, 4) || !aligned(k->lens, 4))
     return GLIDE_ERR_ALIGN;
+  // the kernels number the pools' rows in 32 bits
+  if (int64_t(c->n_pages) * c->n_kv_heads > (int64_t(1) << 32) / c->page_size) return GLIDE_ERR_UNSUPPORTED;
   return GLIDE_OK;
 }
 
@@ -204,6 +206,25 @@ void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a)
   // (a scale of 0 stays a number that no -inf becomes NaN by)
   a->scale = c->sm_scale * kLog2e;
   if (fabsf(a->scale) < 1e-30f) a->scale = 1e-30f;
+}
+
+// The sequences of one launch, from b0 on; *units: workgroups per KV head.
+// per(T): those of a sequence of T new tokens.
+template <typename F>
+int next_launch(const glide_paged_config* c, const int32_t* cu, int b0, PagedSeqs* t, F per) {
+  memset(t, 0, sizeof(*t));
+  t->seq0 = b0;
+  int b1 = b0;
+  while (b1 < c->batch && b1 - b0 < kMaxSeqPerLaunch &&
+         (b1 == b0 || int64_t(cu[b1 + 1] - cu[b0]) * c->n_q_heads <= kMaxLaunchRows)) {
+    const int i = b1 - b0;
+    t->start[i] = cu[b1];
+    t->len[i] = cu[b1 + 1] - cu[b1];
+    t->tile0[i + 1] = t->tile0[i] + (t->len[i] ? int32_t(per(int64_t(t->len[i]))) : 0);
+    ++b1;
+  }
+  t->nseq = b1 - b0;
+  return b1;
 }
 
 glide_status hip_status(hipError_t e) { return e == hipSuccess ? GLIDE_OK : GLIDE_ERR_HIP; }

@@ -80,6 +80,16 @@ class Paged4:
                              f"{(self.batch, self.max_pages)}")
         return Paged4Cache(k_pool, v_pool, block_table, lens, arg, self.geometry)
 
+    def workspace_bytes(self, max_total_tokens=0):
+        return self.lib.glide_nibble_workspace_bytes(self._ref, _fits("max_total_tokens", int(max_total_tokens), 64))
+
+    def new_workspace(self, max_total_tokens=0, device="cuda"):
+        """Workspace for every call of up to max_total_tokens packed tokens."""
+        n = self.workspace_bytes(max_total_tokens)
+        if n == 0:
+            raise glide.GlideError(-2, "glide_nibble_workspace_bytes", self.lib)
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
     # -- calls ---------------------------------------------------------------
     def _check_cache(self, cache):
         """Refuse a cache whose tensors another geometry was checked for."""
@@ -115,3 +125,30 @@ class Paged4:
         kp = _tensor("k_out", k_out, cache._dev, self.torch_dtype, n)
         vp = _tensor("v_out", v_out, cache._dev, self.torch_dtype, n)
         self._call("glide_nibble_read", cache, stream, cu_arg, T, kp, vp)
+
+    def _rows(self, cache, q, out, lse, T):
+        """Pointers of a call over T rows of queries, checked."""
+        if type(cache) is not Paged4Cache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
+        dev, dt, nq = cache._dev, self.torch_dtype, T * self.n_q_heads * self.head_dim
+        return (_tensor("q", q, dev, dt, nq), _tensor("out", out, dev, dt, nq),
+                None if lse is None else _tensor("lse", lse, dev, torch.float32, T * self.n_q_heads))
+
+    def prefill(self, cache, q, cu_seqlens, out, workspace, lse=None, max_len=0, stream=None):
+        """Read out one row per query and head: q, out [T][Hq][d], lse [T][Hq]
+        fp32, for the last cu[b + 1] - cu[b] cached tokens of every sequence b.
+        max_len: a bound of lens on the host (0: none), which the work is split
+        by."""
+        cu_arg, T = _cu_arg(self, cu_seqlens)
+        max_len = _fits("max_len", int(max_len), 64)
+        qp, op, lp = self._rows(cache, q, out, lse, max(T, 0))
+        ws = _tensor("workspace", workspace, cache._dev, torch.uint8, 0)
+        self._call("glide_nibble_prefill", cache, stream, qp, cu_arg, T, max_len, op, lp, ws, workspace.numel())
+
+    def decode(self, cache, q, out, workspace, lse=None, max_len=0, stream=None):
+        """One query per sequence, of its last cached token: q, out [B][Hq][d],
+        lse [B][Hq] fp32."""
+        max_len = _fits("max_len", int(max_len), 64)
+        qp, op, lp = self._rows(cache, q, out, lse, self.batch)
+        ws = _tensor("workspace", workspace, cache._dev, torch.uint8, 0)
+        self._call("glide_nibble_decode", cache, stream, qp, max_len, op, lp, ws, workspace.numel())

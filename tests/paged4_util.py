@@ -115,4 +115,26 @@ class Case4:
 
     def ref(self):
         k, v = (values(*(t.cpu() for t in pool)) for pool in (self.k, self.v))
-        return Ref(self.g, k, v, self.dev_table, self.lens)
+        return Ref4(self.g, k, v, self.dev_table, self.lens)
+
+
+class Ref4(Ref):
+    """Ref with the error bounds of the 4-bit cache's rows.  In fp32 queries
+    and weights go in as three parts: three times the additions."""
+
+    def row(self, b, t, q, score=False):
+        g = self.g
+        G, d = g.n_q_heads // g.n_kv_heads, g.head_dim
+        out, lse, tol, ztol = super().row(b, t, q, False)
+        if g.torch_dtype == torch.bfloat16 or not lse.isfinite().any():
+            return out, lse, tol, ztol
+        seen = [j for j in range(min(t + 1, self.lens[b])) if j > t - g.window or j < g.n_sinks]
+        pg, sl = torch.tensor([x for x in (self.slot(b, j) for j in seen) if x is not None]).T
+        k, v = self.k[pg, :, sl], self.v[pg, :, sl]
+        q = q.double().view(g.n_kv_heads, G, d)
+        s = torch.einsum("hgd,nhd->hgn", q, k) * g.sm_scale
+        size = torch.einsum("hgd,nhd->hgn", q.abs(), k.abs()) * abs(g.sm_scale)
+        p = torch.exp(s - lse.view(g.n_kv_heads, G, 1))
+        dl = ((3 * d + 4) * EPS32 * size.amax(-1)).view(-1) + (3 * len(pg) + 16) * EPS32
+        part = torch.einsum("hgn,nhd->hgd", p, v.abs()).reshape(g.n_q_heads, d)
+        return out, lse, part * (2 * dl)[:, None] + EPS32 * out.abs(), dl + 4 * EPS32 * (1 + lse.abs())
