@@ -458,6 +458,41 @@ glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged
                                 void* bounds, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Attention over the pages that a cheap score selects for each query.
+ *
+ * For the query row at position t of a sequence and KV head g, of the pages
+ * 0 .. t / page_size of the sequence that are allocated: the first n_first (of
+ * numbers below n_first), the last n_recent (of numbers above t / page_size -
+ * n_recent), and of the others those of the largest
+ *   b = sum_c [ (sum_h max(q_hc, 0)) kmax_c + (sum_h min(q_hc, 0)) kmin_c ]
+ * (h over the heads of g; with a scale below 0, of -q), n_select in all.  b is
+ * an upper bound of sum_h q_h.k_j over the page; it is summed in fp64.  Of equal
+ * ones the first; NaN is the smallest.  The row then is softmax attention over
+ *   { j <= t : j's page selected }
+ * in place of cfg's window and sinks; empty rows as for the other calls. */
+
+/* Workspace bytes of a call of up to max_total_tokens rows: for a launch's
+ * rows (of which a call makes several where this would pass 256 MiB, one row's
+ * at least) 8 Hkv max_pages bytes each, the pages selected, and partial
+ * records.  0 if an argument is out of range. */
+size_t glide_paged_sparse_workspace_bytes(const glide_paged_config* cfg, int64_t max_total_tokens, int32_t n_select);
+
+/* One row per query and head; the tokens of the queries are in the cache
+ * (T_b = cu[b+1] - cu[b], the i-th at position lens[b] - T_b + i).
+ *   bounds    device [n_pages][Hkv][2][d], as glide_paged_append keeps them and
+ *             glide_paged_bounds makes them: every page of the sequences
+ *   q, out    device [T][Hq][d];  lse  device fp32 [T][Hq], or NULL
+ *   n_select  >= n_first + n_recent, n_select * page_size <= 2^30; n_first >= 0,
+ *             n_recent >= 1
+ *   selected  device int32 [T][Hkv][n_select]: the numbers of the pages in their
+ *             sequence, in order, -1 behind the last
+ * cu_seqlens_host, max_len, alignment and errors as for glide_paged_prefill. */
+glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged_cache* cache, const void* bounds,
+                                const void* q, const int32_t* cu_seqlens_host, int64_t total_tokens, int32_t n_select,
+                                int32_t n_first, int32_t n_recent, int64_t max_len, int32_t* selected, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * A paged cache held in 4 bits: 17/64 of a bf16 cache's bytes.
  *
  * 32 consecutive elements of a row share a factor 2^e, e the least integer in

@@ -79,6 +79,7 @@ struct PagedArgs {
   float* scores;            // decode with weights: [B][Hq][nv] raw scores (log2 domain)
   float* lse2;              // log2-domain lse by row, where weights need it
   int64_t nv;               // row length of scores
+  int32_t per_head;         // decode: table and lens have a row for every (sequence, KV head)
 };
 
 // The sequences of one prefill launch (at most kMaxSeqPerLaunch), in the

@@ -160,7 +160,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
     tok0 = s.start[i];
   }
   nrow = ntok * a.G;
-  const int32_t len = seq_len(a, b);
+  const int unit = DECODE && a.per_head ? int(blockIdx.x) : b;
+  const int32_t len = seq_len(a, unit);
   p0 = len - ntok;
   const int rl = nrow - 1 - r0 < kPagedRows - 1 ? nrow - 1 - r0 : kPagedRows - 1;  // last row of the tile
   const int32_t t0 = p0 + r0 / a.G > 0 ? p0 + r0 / a.G : 0, t1 = p0 + (r0 + rl) / a.G;
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows(PagedArgs a, Seqs s) {
   // (v0 in 64 bits: blockIdx.y * pl may pass 2^31 where pieces are longer than they need be)
   const int32_t v0 = int32_t(int64_t(blockIdx.y) * pl < sn.n ? int64_t(blockIdx.y) * pl : sn.n);
   const int32_t v1 = sn.n - v0 > pl ? v0 + pl : sn.n;
-  const int32_t* trow = a.table + int64_t(b) * a.max_pages;
+  const int32_t* trow = a.table + int64_t(unit) * a.max_pages;
   const gptr_t zr = (gptr_t)zero_row;
 
   Frag<T> qf[KK];

@@ -1,0 +1,34 @@
+// Launch descriptors of the attention over selected pages (kernels in
+// select.hip, host side in select_api.hip).
+#pragma once
+
+#include "paged.h"
+
+namespace glide {
+
+// Rows of one workgroup of page_scores, and the pages of one of its steps.
+constexpr int kScoreRows = 8;
+constexpr int kScorePages = 64;
+// A launch's scores take at most so many bytes (one row's at least).
+constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
+
+struct SelectArgs {
+  const char* q;         // [T][Hq][d]
+  const char* bounds;    // [n_pages][Hkv][2][d]
+  const int32_t *table, *lens;
+  int32_t Hq, Hkv, G;
+  int32_t n_pages, max_pages, shift, cap;
+  int32_t n_select, n_first, n_recent;
+  int32_t negative;      // the score's scale is below 0
+  int32_t row0, row1;    // packed rows of this launch
+  uint64_t* keys;        // [row1 - row0][Hkv][max_pages]
+  int32_t* selected;     // [T][Hkv][n_select]
+  int32_t *pages, *held; // of this launch's rows: [..][Hkv][n_select] pages, [..][Hkv] tokens
+};
+
+// seqs: start and len of whole sequences; tile0 counts workgroups of kScoreRows
+// rows among row0 .. row1 - 1.  pages: of a sequence, at most (it sizes a grid
+// only)
+hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages, int d, int dtype, hipStream_t stream);
+
+}  // namespace glide

@@ -1,0 +1,136 @@
+// C ABI of the attention over selected pages: argument validation (on the host,
+// before the first HIP call), workspace and launch planning.
+#include "paged_host.h"
+#include "select.h"
+
+using namespace glide;
+
+namespace {
+
+// Rows of one launch at most: what their scores take in the workspace.
+int64_t launch_rows(const glide_paged_config* c, int64_t rows) {
+  const int64_t one = int64_t(c->n_kv_heads) * c->max_pages * 8;
+  return std::min(rows, std::max<int64_t>(1, std::min(kMaxScoreBytes / one, (int64_t(1) << 24) / c->n_kv_heads)));
+}
+
+struct SparseSections {
+  int64_t keys, pages, held, acc, ml, bytes;
+};
+SparseSections sparse_sections(const glide_paged_config* c, int64_t total, int32_t n_select) {
+  const int64_t R = launch_rows(c, total), units = R * c->n_kv_heads;
+  const int64_t records = std::min(R * c->n_q_heads * kPagedMaxPieces, kMaxRecords);
+  SparseSections s;
+  s.keys = 0;
+  s.pages = align256(units * c->max_pages * 8);
+  s.held = s.pages + align256(units * n_select * 4);
+  s.acc = s.held + align256(units * 4);
+  s.ml = s.acc + align256(records * c->head_dim * 4);
+  s.bytes = s.ml + align256(records * 8);
+  return s;
+}
+
+bool select_fits(const glide_paged_config* c, int32_t n_select) {
+  return n_select >= 1 && int64_t(n_select) * c->page_size <= kMaxPagedWindow;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t glide_paged_sparse_workspace_bytes(const glide_paged_config* cfg, int64_t max_total_tokens, int32_t n_select) {
+  if (check_cfg(cfg) != GLIDE_OK || !select_fits(cfg, n_select)) return 0;
+  if (max_total_tokens < 0 || max_total_tokens > (int64_t(1) << 31)) return 0;
+  return size_t(std::max<int64_t>(256, sparse_sections(cfg, max_total_tokens, n_select).bytes));
+}
+
+glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged_cache* cache, const void* bounds,
+                                const void* q, const int32_t* cu_seqlens_host, int64_t total_tokens, int32_t n_select,
+                                int32_t n_first, int32_t n_recent, int64_t max_len, int32_t* selected, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  glide_status s = check_cfg(cfg);
+  if (s != GLIDE_OK) return s;
+  s = check_cache(cfg, cache);
+  if (s != GLIDE_OK) return s;
+  const int32_t* cu = cu_seqlens_host;
+  s = check_cu(cfg, cu, total_tokens);
+  if (s != GLIDE_OK) return s;
+  if (!select_fits(cfg, n_select) || n_first < 0 || n_recent < 1 || max_len < 0) return GLIDE_ERR_INVALID;
+  if (int64_t(n_first) + n_recent > n_select) return GLIDE_ERR_INVALID;
+  if (total_tokens == 0) return GLIDE_OK;
+  if (!bounds || !q || !selected || !out || !workspace) return GLIDE_ERR_NULL;
+  if (!aligned(bounds, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(selected, 4) || !aligned(lse, 4) ||
+      !aligned(workspace, 256))
+    return GLIDE_ERR_ALIGN;
+  if (workspace_bytes < glide_paged_sparse_workspace_bytes(cfg, total_tokens, n_select)) return GLIDE_ERR_SIZE;
+
+  PagedArgs a;
+  fill(cfg, cache, &a);
+  a.wp = nullptr;
+  SelectArgs e;
+  memset(&e, 0, sizeof(e));
+  e.q = static_cast<const char*>(q);
+  e.bounds = static_cast<const char*>(bounds);
+  e.table = a.table;
+  e.lens = a.lens;
+  e.Hq = a.Hq;
+  e.Hkv = a.Hkv;
+  e.G = a.G;
+  e.n_pages = a.n_pages;
+  e.max_pages = a.max_pages;
+  e.shift = a.shift;
+  e.cap = a.cap;
+  e.n_select = n_select;
+  e.n_first = n_first;
+  e.n_recent = n_recent;
+  e.negative = cfg->sm_scale < 0;
+  const SparseSections w = sparse_sections(cfg, total_tokens, n_select);
+  char* ws = static_cast<char*>(workspace);
+  e.keys = reinterpret_cast<uint64_t*>(ws + w.keys);
+  e.selected = selected;
+  e.pages = reinterpret_cast<int32_t*>(ws + w.pages);
+  e.held = reinterpret_cast<int32_t*>(ws + w.held);
+  // the attention: each (row, KV head) over a table of its own, the pages that were selected, all of them
+  a.per_head = 1;
+  a.table = e.pages;
+  a.lens = e.held;
+  a.max_pages = n_select;
+  a.cap = n_select << a.shift;
+  a.W = kMaxPagedWindow;
+  a.ns = 0;
+  const int64_t longest = max_len ? std::min<int64_t>(max_len, e.cap) : e.cap;
+  const int64_t keys = std::min<int64_t>(a.cap, longest), R = launch_rows(cfg, total_tokens);
+  for (int64_t row0 = 0, b0 = 0; row0 < total_tokens;) {
+    PagedSeqs t;
+    memset(&t, 0, sizeof(t));
+    while (cu[b0 + 1] <= row0) ++b0;  // the sequence of the first row
+    t.seq0 = int32_t(b0);
+    int64_t row1 = row0;
+    int i = 0;
+    for (int64_t b = b0; b < cfg->batch && i < kMaxSeqPerLaunch && row1 < row0 + R; ++b, ++i) {
+      row1 = std::min<int64_t>(cu[b + 1], row0 + R);
+      t.start[i] = cu[b];
+      t.len[i] = cu[b + 1] - cu[b];
+      t.tile0[i + 1] = t.tile0[i] + int32_t((row1 - std::max<int64_t>(cu[b], row0) + kScoreRows - 1) / kScoreRows);
+    }
+    t.nseq = i;
+    e.row0 = int32_t(row0);
+    e.row1 = int32_t(row1);
+    s = hip_status(launch_select(e, t, (longest + cfg->page_size - 1) / cfg->page_size, cfg->head_dim, cfg->dtype,
+                                 hipStream_t(stream)));
+    if (s != GLIDE_OK) return s;
+    const int64_t rows = row1 - row0, units = rows * cfg->n_kv_heads, row = int64_t(cfg->n_q_heads) * cfg->head_dim;
+    a.B = int32_t(rows);
+    a.q = static_cast<const char*>(q) + row0 * row * esize(cfg);
+    a.out = static_cast<char*>(out) + row0 * row * esize(cfg);
+    a.lse = lse ? lse + row0 * cfg->n_q_heads : nullptr;
+    a.acc = reinterpret_cast<float*>(ws + w.acc);
+    a.ml = reinterpret_cast<float*>(ws + w.ml);
+    plan_rows(units, keys, &a);
+    s = hip_status(launch_paged_decode(a, keys, cfg->head_dim, cfg->dtype, hipStream_t(stream)));
+    if (s != GLIDE_OK) return s;
+    row0 = row1;
+  }
+  return GLIDE_OK;
+}
+
+}  // extern "C"

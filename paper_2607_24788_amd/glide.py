@@ -32,7 +32,8 @@ EXPORTS = ["glide_state_bytes", "glide_state_layout", "glide_workspace_bytes", "
            "glide_prefill", "glide_decode_step", "glide_decode_step_noalloc", "glide_state_flush", "glide_feature_map",
            "glide_status_string", "glide_paged_workspace_bytes", "glide_paged_prefill", "glide_paged_decode",
            "glide_paged_evict", "glide_paged_append", "glide_paged_bounds", "glide_nibble_append", "glide_nibble_read",
-           "glide_nibble_workspace_bytes", "glide_nibble_prefill", "glide_nibble_decode"]
+           "glide_nibble_workspace_bytes", "glide_nibble_prefill", "glide_nibble_decode", "glide_paged_sparse",
+           "glide_paged_sparse_workspace_bytes"]
 
 
 class GlideError(RuntimeError):
@@ -147,6 +148,11 @@ def load_library(path=None):
     lib.glide_nibble_prefill.restype = ctypes.c_int
     lib.glide_nibble_decode.argtypes = [pcfg, p4cache, vp, ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
     lib.glide_nibble_decode.restype = ctypes.c_int
+    lib.glide_paged_sparse_workspace_bytes.argtypes = [pcfg, ctypes.c_int64, ctypes.c_int32]
+    lib.glide_paged_sparse_workspace_bytes.restype = ctypes.c_size_t
+    lib.glide_paged_sparse.argtypes = [pcfg, pcache, vp, vp, cup, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_int32, ctypes.c_int64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.glide_paged_sparse.restype = ctypes.c_int
     lib.glide_status_string.argtypes = [ctypes.c_int]
     lib.glide_status_string.restype = ctypes.c_char_p
     if path is None:

@@ -250,7 +250,7 @@ class Paged:
         cu_arg, T = _cu_arg(self, cu_seqlens)
         rot = _rotation(freqs, interleaved, positions, dev, T)
         qp, kp, vp, op = _append_rows(self, dev, q, k, v, q_out, max(T, 0))
-        bp = None if bounds is None else self._bounds(cache, bounds)
+        bp = None if bounds is None else self._bounds_of(cache, bounds)
         self._call("glide_paged_append", cache, stream, rot, qp, kp, vp, cu_arg, T, op, bp)
 
     def new_bounds(self, device="cuda"):
@@ -259,7 +259,9 @@ class Paged:
         all)."""
         return torch.empty((self.n_pages, self.n_kv_heads, 2, self.head_dim), dtype=self.torch_dtype, device=device)
 
-    def _bounds(self, cache, bounds):
+    def _bounds_of(self, cache, bounds):
+        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
+            self._check_cache(cache)
         return _tensor("bounds", bounds, cache._dev, self.torch_dtype,
                        2 * self.n_pages * self.n_kv_heads * self.head_dim)
 
@@ -267,10 +269,8 @@ class Paged:
         """The bounds of every page of the sequences from the keys in the
         cache: where they were written without ``append``, and after an
         eviction."""
-        if type(cache) is not PagedCache or cache.geometry is not self.geometry:
-            self._check_cache(cache)
-        max_len = _fits("max_len", int(max_len), 64)
-        self._call("glide_paged_bounds", cache, stream, max_len, self._bounds(cache, bounds))
+        bp = self._bounds_of(cache, bounds)
+        self._call("glide_paged_bounds", cache, stream, _fits("max_len", int(max_len), 64), bp)
 
     def decode(self, cache, q, out, workspace, k=None, v=None, lse=None, max_len=0, stream=None):
         """One token per sequence: q, out [B][Hq][d], k, v [B][Hkv][d],
@@ -282,6 +282,34 @@ class Paged:
         qp, kp, vp, op, lp = self._rows(cache, q, k, v, out, lse, self.batch)
         ws, n = self._workspace(cache, workspace)
         self._call("glide_paged_decode", cache, stream, qp, kp, vp, max_len, op, lp, ws, n)
+
+    def new_sparse_workspace(self, max_total_tokens, n_select, device="cuda"):
+        """Workspace for every ``sparse`` call of up to max_total_tokens rows
+        and this n_select."""
+        n = self.lib.glide_paged_sparse_workspace_bytes(self._ref, _fits("max_total_tokens", int(max_total_tokens), 64),
+                                                        _fits("n_select", int(n_select)))
+        if n == 0:
+            raise glide.GlideError(-2, "glide_paged_sparse_workspace_bytes", self.lib)
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+    def sparse(self, cache, bounds, q, cu_seqlens, n_select, selected, out, workspace, n_first=1, n_recent=1, lse=None,
+               max_len=0, stream=None):
+        """Read out one row per query and head over the n_select pages that
+        each (query, KV head) selects by the pages' bounds (kept by ``append``,
+        made by ``page_bounds``): the first n_first, the last n_recent, and the
+        largest scores of the others.  q, out [T][Hq][d], lse [T][Hq] fp32;
+        selected [T][Hkv][n_select] int32: the pages' numbers in their
+        sequence, -1 behind the last.  The queries' tokens are in the cache."""
+        bp = self._bounds_of(cache, bounds)
+        cu_arg, T = _cu_arg(self, cu_seqlens)
+        n_select, n_first, n_recent = (_fits(name, int(x)) for name, x in (
+            ("n_select", n_select), ("n_first", n_first), ("n_recent", n_recent)))
+        max_len = _fits("max_len", int(max_len), 64)
+        qp, _, _, op, lp = self._rows(cache, q, None, None, out, lse, max(T, 0))
+        sp = _tensor("selected", selected, cache._dev, torch.int32, max(T, 0) * self.n_kv_heads * max(n_select, 0))
+        ws, n = self._workspace(cache, workspace)
+        self._call("glide_paged_sparse", cache, stream, bp, qp, cu_arg, T, n_select, n_first, n_recent, max_len, sp,
+                   op, lp, ws, n)
 
     def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):
         """Keep min(len, budget) tokens per sequence and KV head, in place or
