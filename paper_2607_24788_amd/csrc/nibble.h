@@ -14,9 +14,15 @@ struct Pools4 {
   uint8_t *kc, *ks, *vc, *vs;
 };
 
+// Rows of a workgroup of nibble_tiles (four waves of 32, or eight).
+constexpr int kRows4 = 128, kRows4Big = 256;
+
 // a.kp, a.vp, a.kn, a.vn, a.wp and the strides are not used; as launch_paged_decode
 // and launch_paged_prefill otherwise.
-hipError_t launch_nibble_decode(const PagedArgs& a, const Pools4& p, int d, int dtype, hipStream_t stream);
+// tile_keys: keys of a wave's tile, 64 or (bf16) 32; tile_rows: kPagedRows
+// (nibble_rows), kRows4 or kRows4Big.
+hipError_t launch_nibble_decode(const PagedArgs& a, const Pools4& p, int d, int dtype, int tile_keys,
+                                hipStream_t stream);
 hipError_t launch_nibble_prefill(const PagedArgs& a, const Pools4& p, const PagedSeqs& s, int d, int dtype,
                                  int tile_rows, hipStream_t stream);
 

@@ -48,17 +48,19 @@ constexpr int64_t kMaxRecords = 131072;
 struct StepCost {
   int keys;
   double us1, us2;
+  int round = kPagedRound;  // workgroups of a round
+  double wg = 0;            // and the start and end of a workgroup, in each
 };
 inline double prefill_us(double tiles, int64_t keys, double avg, const StepCost& c, int64_t n, int64_t rows,
                          double kv_bytes, int d) {
   const int64_t steps = (keys + c.keys - 1) / c.keys;
   const double per = double((steps + n - 1) / n), wgs = tiles * (double(n) * avg + (1 - avg));
-  const double rounds = double(int64_t((wgs + kPagedRound - 1) / kPagedRound));
+  const double rounds = double(int64_t((wgs + c.round - 1) / c.round));
   double t = rounds * per;
-  const double even = tiles * double(steps) * avg / kPagedRound + per / 2;
+  const double even = tiles * double(steps) * avg / c.round + per / 2;
   t = t < even ? t : even > per ? even : per;
-  t *= wgs <= kPagedRound / 2 ? c.us1 : c.us2;
-  const double mem = kv_bytes / 5e6 * rounds * kPagedRound / wgs;
+  t = t * (wgs <= c.round / 2 ? c.us1 : c.us2) + c.wg * rounds;
+  const double mem = kv_bytes / 5e6 * rounds * c.round / wgs;
   return (t > mem ? t : mem) + (n > 1 ? 4 + double(rows) * double(n) * (d + 2) * 8 / 4e6 : 0);
 }
 

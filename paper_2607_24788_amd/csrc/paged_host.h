@@ -115,11 +115,12 @@ StepCost step_cost(const glide_paged_config* c, int tile_rows) {
                                   : StepCost{4 * kPagedTile, 0.5 + 4 * d, 0.7 + 7.4 * d};
 }
 // The best number of pieces of a prefill of `rows` rows in `tiles` row tiles
-// (nseq sequences), and the time that the model gives it.
-double plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
-                    int64_t keys, int64_t* pieces) {
-  const StepCost cost = step_cost(c, tile_rows);
-  const double kv = 2.0 * nseq * c->n_kv_heads * double(keys) * c->head_dim * esize(c);
+// (nseq sequences), whose longest tile sees `keys` keys (`key_bytes` of K and V
+// each), and the time that the model gives it.  coarse: of about every fifth
+// number only, for less of the host's time.
+double plan_pieces(const glide_paged_config* c, const StepCost& cost, int64_t tiles, int tile_rows, int64_t rows,
+                   int64_t nseq, int64_t keys, double key_bytes, bool coarse, int64_t* pieces) {
+  const double kv = nseq * c->n_kv_heads * double(keys) * key_bytes;
   // new tokens of a sequence, against the keys that the last of them sees
   const double T = double(rows) / (double(nseq) * c->n_q_heads), K = double(keys);
   const double avg = T <= K ? 1 - T / (2 * K) : 1 - K / (2 * T);
@@ -127,7 +128,7 @@ double plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, i
   int64_t n = 1;
   double best = us(1);
   const int64_t most = std::min((keys + cost.keys - 1) / cost.keys, max_pieces(tiles, tile_rows));
-  for (int64_t m = 2; m <= most; ++m) {
+  for (int64_t m = 2; m <= most; m += coarse ? 1 + m / 4 : 1) {
     const double x = us(m);
     if (x < best) {
       n = m;
@@ -136,6 +137,11 @@ double plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, i
   }
   *pieces = n;
   return best;
+}
+double plan_prefill(const glide_paged_config* c, int64_t tiles, int tile_rows, int64_t rows, int64_t nseq,
+                    int64_t keys, int64_t* pieces) {
+  return plan_pieces(c, step_cost(c, tile_rows), tiles, tile_rows, rows, nseq, keys, 2.0 * c->head_dim * esize(c),
+                     false, pieces);
 }
 
 // Sections of the workspace of one call, in bytes from its start.
