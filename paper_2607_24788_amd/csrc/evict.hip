@@ -24,20 +24,6 @@ __device__ __forceinline__ int64_t weight_at(const EvictArgs& a, int32_t page, i
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kBins = 2048, kCopies = 2;
 
-// Inclusive sum over the lanes of a wave: within rows of 16, then the rows'
-// last lanes (15 into rows 1 and 3, 31 into rows 2 and 3) to the rows behind.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t dpp_add(uint32_t x) {
-  return x + uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 0xf, false));
-}
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  x = dpp_add<0x111, 0xf>(x);  // row_shr:1
-  x = dpp_add<0x112, 0xf>(x);
-  x = dpp_add<0x114, 0xf>(x);
-  x = dpp_add<0x118, 0xf>(x);
-  x = dpp_add<0x142, 0xa>(x);     // row_bcast:15
-  return dpp_add<0x143, 0xc>(x);  // row_bcast:31
-}
 // Exclusive sum over the workgroup's threads; wsum: one entry per wave.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wsum, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

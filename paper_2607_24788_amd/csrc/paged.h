@@ -177,4 +177,19 @@ __device__ __forceinline__ Seen seen_by(int32_t t0, int32_t t1, int32_t W, int32
   return s;
 }
 
+// Inclusive sum over the lanes of a wave: within rows of 16, then the rows'
+// last lanes (15 into rows 1 and 3, 31 into rows 2 and 3) to the rows behind.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_add(uint32_t x) {
+  return x + uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x = dpp_add<0x111, 0xf>(x);  // row_shr:1
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);     // row_bcast:15
+  return dpp_add<0x143, 0xc>(x);  // row_bcast:31
+}
+
 }  // namespace glide

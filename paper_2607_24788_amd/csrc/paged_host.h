@@ -98,12 +98,10 @@ void set_pieces(int64_t n, int64_t keys, PagedArgs* a) {
   a->npiece = int32_t(n);
   a->piece = int32_t(((keys + n - 1) / n + 127) / 128 * 128);
 }
-void plan_rows(int64_t units, int64_t keys, PagedArgs* a) {
+void plan_decode(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
+  const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), units = int64_t(c->batch) * c->n_kv_heads;
   const int64_t piece = std::min<int64_t>(kPieceLong, std::max<int64_t>(kPieceMin, units * keys / kPagedRound));
   set_pieces(std::min((keys + piece - 1) / piece, max_pieces(units, kPagedRows)), keys, a);
-}
-void plan_decode(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
-  plan_rows(int64_t(c->batch) * c->n_kv_heads, std::max<int64_t>(1, most_seen(c, max_len)), a);
 }
 // Steps of the prefill kernels, timed with one and with two workgroups per CU.
 StepCost step_cost(const glide_paged_config* c, int tile_rows) {

@@ -6,9 +6,10 @@
 
 namespace glide {
 
-// Rows of one workgroup of page_scores, and the pages of one of its steps.
+// Rows of one workgroup of page_scores.
 constexpr int kScoreRows = 8;
-constexpr int kScorePages = 64;
+// Its workgroups take more pages each where there would be more than these.
+constexpr int64_t kScoreWorkgroups = 4096;
 // A launch's scores take at most so many bytes (one row's at least).
 constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
 
@@ -20,6 +21,8 @@ struct SelectArgs {
   int32_t n_pages, max_pages, shift, cap;
   int32_t n_select, n_first, n_recent;
   int32_t negative;      // the score's scale is below 0
+  int32_t single;        // every sequence of the launch has one row
+  int32_t chunk;         // pages of one workgroup of page_scores, at a time: a multiple of 32
   int32_t row0, row1;    // packed rows of this launch
   uint64_t* keys;        // [row1 - row0][Hkv][max_pages]
   int32_t* selected;     // [T][Hkv][n_select]

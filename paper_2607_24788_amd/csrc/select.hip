@@ -21,14 +21,34 @@ __device__ __forceinline__ uint64_t key_of(double x) {
 }
 constexpr uint64_t kAlways = ~uint64_t(0);
 
-template <typename T>
-__device__ __forceinline__ void load8d(double* x, const char* p) {
-  Frag<T> f;
-  gload_frag<false>(f, (gptr_t)p);
-  float y[8];
-  f.to_floats(y);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = double(y[i]);
+__device__ __forceinline__ void load4(float* x, const float* p) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+__device__ __forceinline__ void load4(float* x, const bf16_t* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  x[0] = __uint_as_float(v.x << 16);
+  x[1] = __uint_as_float(v.x & 0xffff0000u);
+  x[2] = __uint_as_float(v.y << 16);
+  x[3] = __uint_as_float(v.y & 0xffff0000u);
+}
+
+// Sum over SL lanes (8, or a row of 16), in each of them, in one order.
+template <int CTRL>
+__device__ __forceinline__ double dpp_mv64(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(u)), CTRL, 0xf, 0xf, false));
+  const uint32_t hi = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, 0xf, 0xf, false));
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+template <int SL>
+__device__ __forceinline__ double sum_lanes(double x) {
+  static_assert(SL == 8 || SL == 16, "half a row, or a row");
+  x += dpp_mv64<0xb1>(x);   // quad_perm [1,0,3,2]
+  x += dpp_mv64<0x4e>(x);   // quad_perm [2,3,0,1]
+  x += dpp_mv64<0x141>(x);  // row_half_mirror
+  if constexpr (SL == 16) x += dpp_mv64<0x140>(x);  // row_mirror
+  return x;
 }
 
 // ---------------------------------------------------------------------------
@@ -37,14 +57,14 @@ __device__ __forceinline__ void load8d(double* x, const char* p) {
 // sum_h q_h . k of any key of the page, for two products of a row instead of G
 // per key.  In fp64, where products of bf16 numbers are exact: neighbouring
 // pages' scores are told apart alike however the sum is ordered.
-// D / 8 lanes to a page, eight elements of both bounds each, for up to eight
-// queries of a sequence; bound by the reading of the bounds.
+// D / 8 lanes to a page, eight elements of both bounds each (asked for a page
+// ahead), for up to eight queries of a sequence.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void page_scores(SelectArgs a, PagedSeqs s) {
   constexpr int SL = D / 8, ES = int(sizeof(T)), PPI = 256 / SL;  // lanes of a page, pages at once
   __shared__ __align__(16) double uw[kScoreRows][2][D];
   const int tile = int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
-  int lo = 0, hi = s.nseq - 1;
+  int lo = a.single ? tile : 0, hi = a.single ? tile : s.nseq - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (s.tile0[mid] <= tile) lo = mid;
@@ -57,43 +77,86 @@ __global__ __launch_bounds__(256) void page_scores(SelectArgs a, PagedSeqs s) {
   const int rows = end - r0 < kScoreRows ? end - r0 : kScoreRows;
   const int32_t len = seq_len(a, b), t0 = len - ntok + (r0 - s.start[lo]);  // position of the first row
   const int32_t last = t0 + rows - 1 < 0 ? -1 : (t0 + rows - 1) >> a.shift;
-  if (int(blockIdx.y) * kScorePages > last) return;
-  for (int e = threadIdx.x; e < rows * D; e += 256) {
-    const T* q = reinterpret_cast<const T*>(a.q) + (int64_t(r0 + e / D) * a.Hq + g * a.G) * D + e % D;
-    double u = 0, w = 0;
-    for (int h = 0; h < a.G; ++h) {
-      const float x = a.negative ? -to_f32(q[h * D]) : to_f32(q[h * D]);
-      u += x < 0.f ? 0.f : x;   // (NaN counts in u: the score is NaN)
-      w += x < 0.f ? x : 0.f;
-    }
-    uw[e / D][0][e % D] = w;
-    uw[e / D][1][e % D] = u;
-  }
-  __syncthreads();
+  if (int(blockIdx.y) * a.chunk > last) return;
   const int sub = threadIdx.x % SL;
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
-  for (int32_t i0 = blockIdx.y * kScorePages; i0 <= last; i0 += gridDim.y * kScorePages) {
-#pragma unroll 1
-    for (int32_t i = i0 + int32_t(threadIdx.x) / SL; i < i0 + kScorePages; i += PPI) {
-      if (i > last) break;
-      const int32_t page = trow[i];
-      const bool ok = uint32_t(page) < uint32_t(a.n_pages);
-      double kmin[8], kmax[8];
-      const char* p = a.bounds + (int64_t(ok ? page : 0) * a.Hkv + g) * (2 * D * ES) + sub * 8 * ES;
-      load8d<T>(kmin, p);
-      load8d<T>(kmax, p + D * ES);
-      for (int r = 0; r < rows; ++r) {
-        double x = 0;
+  struct Page {
+    Frag<T> lo, hi;
+    bool ok;
+  };
+  auto fetch = [&](int32_t i) {
+    Page p;
+    const int32_t page = trow[i < last ? i : last];
+    p.ok = uint32_t(page) < uint32_t(a.n_pages);
+    const gptr_t at = (gptr_t)a.bounds + (int64_t(p.ok ? page : 0) * a.Hkv + g) * (2 * D * ES) + sub * 8 * ES;
+    gload_frag<false>(p.lo, at);
+    gload_frag<false>(p.hi, at + D * ES);
+    return p;
+  };
+  // pages of this workgroup: a.chunk in turn with the others
+  const int32_t mine = int32_t(threadIdx.x) / SL, jump = (int32_t(gridDim.y) - 1) * a.chunk;
+  int32_t i0 = int32_t(blockIdx.y) * a.chunk, in = 0;
+  Page next = fetch(i0 + mine);
+  // four elements of a row to a thread, four heads' at once
+  static_assert(kScoreRows * D / 4 <= 256, "a thread for each");
+  if (int(threadIdx.x) < rows * (D / 4)) {
+    const int r = threadIdx.x / (D / 4), c0 = (threadIdx.x % (D / 4)) * 4;
+    const T* q = reinterpret_cast<const T*>(a.q) + (int64_t(r0 + r) * a.Hq + g * a.G) * D + c0;
+    double u[4] = {}, w[4] = {};
+    for (int h0 = 0; h0 < a.G; h0 += 4) {
+      float x[4][4];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) x = fma(uw[r][1][8 * sub + c], kmax[c], fma(uw[r][0][8 * sub + c], kmin[c], x));
+      for (int k = 0; k < 4; ++k) load4(x[k], q + (h0 + k < a.G ? h0 + k : h0) * D);
 #pragma unroll
-        for (int m = 1; m < SL; m *= 2) x += __shfl_xor(x, m);
-        const int32_t mine = (t0 + r) >> a.shift;  // (t0 + r < 0: behind no page)
-        if (sub == 0 && i <= mine) {
-          uint64_t k = key_of(x);
-          if (i < a.n_first || i > mine - a.n_recent) k = kAlways;
-          a.keys[(int64_t(r0 - a.row0 + r) * a.Hkv + g) * a.max_pages + i] = ok ? k : 0;
+      for (int k = 0; k < 4; ++k) {
+        if (h0 + k >= a.G) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float y = a.negative ? -x[k][c] : x[k][c];
+          u[c] += y < 0.f ? 0.f : y;  // (NaN counts in u: the score is NaN)
+          w[c] += y < 0.f ? y : 0.f;
         }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uw[r][0][c0 + c] = w[c];
+      uw[r][1][c0 + c] = u[c];
+    }
+  }
+  __syncthreads();
+  while (i0 <= last) {
+    const Page now = next;
+    const int32_t i = i0 + mine;
+    in += PPI;
+    i0 += PPI;
+    if (in >= a.chunk) {
+      in = 0;
+      i0 += jump;
+    }
+    if (i0 <= last) next = fetch(i0 + mine);
+    double kmin[8], kmax[8];
+    float y[8];
+    now.lo.to_floats(y);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) kmin[c] = double(y[c]);
+    now.hi.to_floats(y);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) kmax[c] = double(y[c]);
+#pragma unroll 2
+    for (int r = 0; r < rows; ++r) {
+      double x = 0, z = 0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        x = fma(uw[r][1][8 * sub + c], kmax[c], x);
+        z = fma(uw[r][0][8 * sub + c], kmin[c], z);
+      }
+      x = sum_lanes<SL>(x + z);
+      const int32_t own = (t0 + r) >> a.shift;  // (t0 + r < 0: behind no page)
+      if (sub == 0 && i <= own) {
+        uint64_t k = key_of(x);
+        if (i < a.n_first || i > own - a.n_recent) k = kAlways;
+        a.keys[(int64_t(r0 - a.row0 + r) * a.Hkv + g) * a.max_pages + i] = now.ok ? k : 0;
       }
     }
   }
@@ -102,19 +165,20 @@ __global__ __launch_bounds__(256) void page_scores(SelectArgs a, PagedSeqs s) {
 // ---------------------------------------------------------------------------
 // The n_select largest keys of a row, in the order of their pages; of equal
 // ones the first.  The least key that is in is found from the highest bit in
-// which keys differ down, 11 bits at a time: a histogram of the keys that agree
-// so far, and its bins from the top.  KEYS: keys of a thread in registers; 0:
-// read again in each pass.
-template <int KEYS>
-__global__ __launch_bounds__(256) void select_pages(SelectArgs a, PagedSeqs s) {
-  constexpr int BITS = 11, BINS = 1 << BITS, PER = BINS / 256;
-  __shared__ uint32_t hist[BINS];
-  __shared__ uint64_t red[2][4];
-  __shared__ uint32_t cnt[3][4], found[3], ranks[(KEYS ? KEYS : 1) * 4];
+// which keys differ down, 11 bits at a time: a histogram in LDS of the keys that
+// agree so far (integer counts: no order of atomics shows), and its bins from
+// the top; two or three of these, as the bin of the last key in has few others.
+// Then ranks by one scan.  Four neighbouring pages to a thread; ONE: all of them
+// at once, in registers, else in turns, read again in each pass.
+// Bound by the latency of its reads and barriers.
+template <int NT, bool ONE>
+__global__ __launch_bounds__(NT) void select_pages(SelectArgs a, PagedSeqs s) {
+  constexpr int BITS = 11, BINS = 1 << BITS, PER = BINS / NT, NW = NT / 64;
+  __shared__ uint32_t hist[BINS], wsum[NW], total[4], found[3];  // total: always in, others, and their extremes
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t row = a.row0 + int32_t(blockIdx.x) / a.Hkv;
   const int g = int(blockIdx.x) % a.Hkv;
-  int lo = 0, hi = s.nseq - 1;
+  int lo = a.single ? row - a.row0 : 0, hi = a.single ? lo : s.nseq - 1;
   while (lo < hi) {  // the last sequence that starts at or before the row
     const int mid = (lo + hi + 1) >> 1;
     if (s.start[mid] <= row) lo = mid;
@@ -129,94 +193,91 @@ __global__ __launch_bounds__(256) void select_pages(SelectArgs a, PagedSeqs s) {
   int32_t* out = a.selected + (int64_t(row) * a.Hkv + g) * a.n_select;
   int32_t* pages = a.pages + unit * a.n_select;
 
-  uint64_t mine[KEYS ? KEYS : 1];
-  if constexpr (KEYS > 0) {
+  uint64_t mine[4];
+  auto load = [&](int32_t i0) {
 #pragma unroll
-    for (int e = 0; e < KEYS; ++e) {
-      const int32_t i = e * 256 + int32_t(threadIdx.x);
+    for (int e = 0; e < 4; ++e) {
+      const int32_t i = i0 + 4 * int32_t(threadIdx.x) + e;
       mine[e] = i < n ? keys[i] : 0;
     }
-  }
+  };
   auto each = [&](auto f) {
-    if constexpr (KEYS > 0) {
+    if constexpr (ONE) {
 #pragma unroll
-      for (int e = 0; e < KEYS; ++e) f(mine[e]);
+      for (int e = 0; e < 4; ++e) f(mine[e]);
     } else {
-      for (int32_t i = threadIdx.x; i < n; i += 256) f(keys[i]);
+      for (int32_t i0 = 0; i0 < n; i0 += 4 * NT) {
+        load(i0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(mine[e]);
+      }
     }
   };
-  // sums and extremes over the workgroup
-  uint32_t always = 0, free_ = 0;
-  uint64_t top = 0, bottom = ~uint64_t(0);
+  // exclusive sum over the workgroup's threads, and the sum of all
+  auto block_scan = [&](uint32_t x, uint32_t* all) {
+    const uint32_t inc = wave_scan(x);
+    __syncthreads();
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    const uint32_t w = wave_scan(lane < NW ? wsum[lane] : 0);
+    *all = __builtin_amdgcn_readlane(w, 63);
+    return (wave ? __builtin_amdgcn_readlane(w, wave - 1) : 0) + inc - x;
+  };
+  if constexpr (ONE) load(0);
+  if (threadIdx.x < 4) total[threadIdx.x] = threadIdx.x == 3 ? ~0u : 0u;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) hist[i * NT + threadIdx.x] = 0;
+  __syncthreads();
+  uint32_t always = 0, others = 0, top = 0, bottom = ~0u;  // extremes: upper halves
   each([&](uint64_t k) {
-    if (k == kAlways) ++always;
-    else if (k) {
-      ++free_;
-      top = k > top ? k : top;
-      bottom = k < bottom ? k : bottom;
-    }
+    const bool other = k != 0 && k != kAlways;
+    always += __popcll(__ballot(k == kAlways));
+    others += __popcll(__ballot(other));
+    const uint32_t h = uint32_t(k >> 32);
+    top = other && h > top ? h : top;
+    bottom = other && h < bottom ? h : bottom;
   });
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) {
-    always += __shfl_xor(always, m);
-    free_ += __shfl_xor(free_, m);
-    const uint64_t x = __shfl_xor((unsigned long long)top, m), y = __shfl_xor((unsigned long long)bottom, m);
+    const uint32_t x = uint32_t(__shfl_xor(int(top), m)), y = uint32_t(__shfl_xor(int(bottom), m));
     top = x > top ? x : top;
     bottom = y < bottom ? y : bottom;
   }
   if (lane == 0) {
-    cnt[0][wave] = always;
-    cnt[1][wave] = free_;
-    red[0][wave] = top;
-    red[1][wave] = bottom;
+    atomicAdd(&total[0], always);
+    atomicAdd(&total[1], others);
+    atomicMax(&total[2], top);
+    atomicMin(&total[3], bottom);
   }
   __syncthreads();
-  always = free_ = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    always += cnt[0][w];
-    free_ += cnt[1][w];
-    top = red[0][w] > top ? red[0][w] : top;
-    bottom = red[1][w] < bottom ? red[1][w] : bottom;
-  }
+  always = total[0];
+  others = total[1];
+  top = total[2];
+  bottom = total[3];
   uint32_t want = always < uint32_t(a.n_select) ? uint32_t(a.n_select) - always : 0;
-  const uint32_t count = want < free_ ? always + want : always + free_;
-  // in: keys at or above `least` (among equals of it the first `ties`, where that is not all of them)
-  uint64_t least = 1;
-  uint32_t ties = ~0u;
-  if (want == 0) {
-    least = kAlways;
-  } else if (want < free_) {
-    int shift = 64 - __builtin_clzll((top ^ bottom) | 1);  // bits below it differ
-    uint64_t prefix = shift < 64 ? top >> shift : 0;         // of the keys that agree so far
+  const uint32_t count = want < others ? always + want : always + others;
+  // in: keys above `least`, and the first `ties` of those equal to it
+  uint64_t least = want == 0 ? kAlways - 1 : 0;
+  uint32_t ties = 0;
+  if (want != 0 && want < others) {
+    int shift = top == bottom ? 32 : 64 - __builtin_clz(top ^ bottom);  // bits below it differ
+    uint64_t prefix = shift < 64 ? uint64_t(top) << 32 >> shift : 0;    // of the keys that agree so far
     for (;;) {
       const int step = shift < BITS ? shift : BITS, next = shift - step;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) hist[i * 256 + threadIdx.x] = 0;
-      __syncthreads();
       each([&](uint64_t k) {
         if (k && k != kAlways && (shift < 64 ? k >> shift : 0) == prefix)
           atomicAdd(&hist[(k >> next) & ((uint64_t(1) << step) - 1)], 1u);
       });
       __syncthreads();
       // bins from the top: thread x has bins BINS - 1 - PER x downwards
-      uint32_t h[PER], sum = 0;
+      uint32_t h[PER], sum = 0, all;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         h[i] = hist[BINS - 1 - int(threadIdx.x) * PER - i];
         sum += h[i];
       }
-      uint32_t upto = sum;
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) {
-        const uint32_t y = __shfl_up(upto, m);
-        upto += lane >= m ? y : 0;
-      }
-      if (lane == 63) cnt[2][wave] = upto;
-      __syncthreads();
-      for (int w = 0; w < wave; ++w) upto += cnt[2][w];
-      uint32_t above = upto - sum;
-      if (above < want && upto >= want) {  // one thread: the bin that the last one in is in
+      uint32_t above = block_scan(sum, &all);
+      if (above < want && above + sum >= want) {  // one thread: the bin that the last one in is in
         bool done = false;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -229,94 +290,48 @@ __global__ __launch_bounds__(256) void select_pages(SelectArgs a, PagedSeqs s) {
           if (!done) above += h[i];
         }
       }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) hist[BINS - 1 - int(threadIdx.x) * PER - i] = 0;
       __syncthreads();
-      const uint32_t bin = found[0];
       want -= found[1];
-      prefix = (prefix << step) | bin;
+      prefix = (prefix << step) | found[0];
       shift = next;
-      if (found[2] == want || shift == 0) {
-        if (found[2] != want) ties = want;
-        least = prefix << shift;
+      if (found[2] == want) {
+        least = (prefix << shift) - 1;  // (no key but one that cannot be selected is 0)
+        break;
+      }
+      if (shift == 0) {
+        least = prefix;
+        ties = want;
         break;
       }
     }
   }
-  // ranks of the pages that are in
-  auto emit = [&](int32_t i, uint32_t at) {
-    out[at] = i;
-    pages[at] = trow[i];
-  };
-  auto place = [&](auto in, auto put) {  // in(k, i): counted; put(i, rank)
-    if constexpr (KEYS > 0) {
-      uint64_t mask[KEYS];
+  // ranks, in the order of pages: counts of both kinds in one scan (4096 at most)
+  uint32_t above = 0, equal = 0;
+  for (int32_t i0 = 0; i0 < n; i0 += 4 * NT) {
+    if constexpr (!ONE) load(i0);
+    uint32_t x = 0, all;
 #pragma unroll
-      for (int e = 0; e < KEYS; ++e) {
-        mask[e] = __ballot(in(mine[e]));
-        if (lane == 0) ranks[e * 4 + wave] = __popcll(mask[e]);
-      }
-      __syncthreads();
-      uint32_t before = 0;
-      for (int x = 0; x < wave; ++x) before += ranks[x];
+    for (int e = 0; e < 4; ++e) x += (mine[e] > least ? 1u : 0u) + (ties && mine[e] == least ? 1u << 16 : 0u);
+    const uint32_t before = block_scan(x, &all);
+    uint32_t up = above + (before & 0xffffu), eq = equal + (before >> 16);
 #pragma unroll
-      for (int e = 0; e < KEYS; ++e) {
-        if ((mask[e] >> lane) & 1)
-          put(e, e * 256 + int32_t(threadIdx.x), before + __popcll(mask[e] & ((uint64_t(1) << lane) - 1)));
-        if (e + 1 < KEYS)
-          for (int x = 0; x < 4; ++x) before += ranks[e * 4 + wave + x];
+    for (int e = 0; e < 4; ++e) {
+      const int32_t i = i0 + 4 * int32_t(threadIdx.x) + e;
+      const bool is = ties && mine[e] == least, in = mine[e] > least || (is && eq < ties);
+      if (in) {
+        const uint32_t at = up + (eq < ties ? eq : ties);
+        out[at] = i;
+        pages[at] = trow[i];
       }
-      __syncthreads();
-    } else {
-      uint32_t before = 0;
-      for (int32_t i0 = 0; i0 < n; i0 += 256) {
-        const int32_t i = i0 + int32_t(threadIdx.x);
-        const uint64_t m = __ballot(i < n && in(i < n ? keys[i] : 0));
-        if (lane == 0) ranks[wave] = __popcll(m);
-        __syncthreads();
-        uint32_t at = before;
-        for (int x = 0; x < wave; ++x) at += ranks[x];
-        if ((m >> lane) & 1) put(0, i, at + __popcll(m & ((uint64_t(1) << lane) - 1)));
-        for (int x = 0; x < 4; ++x) before += ranks[x];
-        __syncthreads();
-      }
+      up += mine[e] > least;
+      eq += is;
     }
-  };
-  if (ties == ~0u) {
-    place([&](uint64_t k) { return k >= least && k; }, [&](int, int32_t i, uint32_t at) { emit(i, at); });
-  } else {
-    // equal keys: the first `ties` of them
-    if constexpr (KEYS > 0) {
-      place([&](uint64_t k) { return k == least; }, [&](int e, int32_t, uint32_t at) {
-#pragma unroll
-        for (int x = 0; x < KEYS; ++x)
-          if (x == e && at >= ties) mine[x] = 0;
-      });
-      place([&](uint64_t k) { return k >= least; }, [&](int, int32_t i, uint32_t at) { emit(i, at); });
-    } else {
-      uint32_t before = 0, equal = 0;
-      for (int32_t i0 = 0; i0 < n; i0 += 256) {
-        const int32_t i = i0 + int32_t(threadIdx.x);
-        const uint64_t k = i < n ? keys[i] : 0;
-        const uint64_t e = __ballot(k == least);
-        if (lane == 0) ranks[wave] = __popcll(e);
-        __syncthreads();
-        uint32_t at = equal;
-        for (int x = 0; x < wave; ++x) at += ranks[x];
-        at += __popcll(e & ((uint64_t(1) << lane) - 1));
-        for (int x = 0; x < 4; ++x) equal += ranks[x];
-        const bool in = k > least || (k == least && at < ties);
-        __syncthreads();
-        const uint64_t m = __ballot(in);
-        if (lane == 0) ranks[wave] = __popcll(m);
-        __syncthreads();
-        at = before;
-        for (int x = 0; x < wave; ++x) at += ranks[x];
-        if (in) emit(i, at + __popcll(m & ((uint64_t(1) << lane) - 1)));
-        for (int x = 0; x < 4; ++x) before += ranks[x];
-        __syncthreads();
-      }
-    }
+    above += all & 0xffffu;
+    equal += all >> 16;
   }
-  for (uint32_t i = count + threadIdx.x; i < uint32_t(a.n_select); i += 256) {
+  for (uint32_t i = count + threadIdx.x; i < uint32_t(a.n_select); i += NT) {
     out[i] = -1;
     pages[i] = -1;
   }
@@ -330,7 +345,7 @@ __global__ __launch_bounds__(256) void select_pages(SelectArgs a, PagedSeqs s) {
 template <typename T, int D>
 hipError_t scores_t(const SelectArgs& a, const PagedSeqs& s, int64_t pages, hipStream_t stream) {
   const dim3 grid(uint32_t(s.tile0[s.nseq]) * uint32_t(a.Hkv),
-                  uint32_t(std::max<int64_t>(1, std::min<int64_t>((pages + kScorePages - 1) / kScorePages, 4096))));
+                  uint32_t(std::max<int64_t>(1, std::min<int64_t>((pages + a.chunk - 1) / a.chunk, 32768))));
   page_scores<T, D><<<grid, 256, 0, stream>>>(a, s);
   return hipGetLastError();
 }
@@ -346,9 +361,9 @@ hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages,
   if (e != hipSuccess) return e;
   const uint32_t units = uint32_t(a.row1 - a.row0) * uint32_t(a.Hkv);
   // (by the table's width, which no sequence has more pages than)
-  if (a.max_pages <= 1024) select_pages<4><<<units, 256, 0, stream>>>(a, s);
-  else if (a.max_pages <= 4096) select_pages<16><<<units, 256, 0, stream>>>(a, s);
-  else select_pages<0><<<units, 256, 0, stream>>>(a, s);
+  if (a.max_pages <= 1024) select_pages<256, true><<<units, 256, 0, stream>>>(a, s);
+  else if (a.max_pages <= 4096) select_pages<1024, true><<<units, 1024, 0, stream>>>(a, s);
+  else select_pages<1024, false><<<units, 1024, 0, stream>>>(a, s);
   return hipGetLastError();
 }
 
