@@ -57,11 +57,44 @@ struct Bounds16 {
     hi[i] = fmaxf(hi[i], x);
   }
 };
-// The threads' bounds joined: C threads (elements 8 c1 .. and 8 c2 ..), the
-// others of a workgroup hold other tokens of the same elements.  Thread x < C
-// leaves them in the page's row, together with what is there if `more`.
-template <typename T, int D, int C>
-__device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32], char* row, int c1, int c2, bool more) {
+// What a page's bounds are already, of a thread's elements.
+template <typename T>
+struct OldBounds {
+  Frag<T> lo[2], hi[2];
+  __device__ __forceinline__ void load(const char* row, int D, int c1, int c2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const gptr_t p = (gptr_t)row + (h ? c2 : c1) * 8 * int(sizeof(T));
+      gload_frag<false>(lo[h], p);
+      gload_frag<false>(hi[h], p + D * int(sizeof(T)));
+    }
+  }
+};
+// A thread's bounds to the page's row, together with those there if `more`.
+template <typename T, int D>
+__device__ __forceinline__ void store_bounds(Bounds16& b, const OldBounds<T>& old, char* row, int c1, int c2,
+                                             bool more) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (more) {
+      float lo[8], hi[8];
+      old.lo[h].to_floats(lo);
+      old.hi[h].to_floats(hi);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        b.lo[8 * h + i] = fminf(b.lo[8 * h + i], lo[i]);
+        b.hi[8 * h + i] = fmaxf(b.hi[8 * h + i], hi[i]);
+      }
+    }
+    char* p = row + (h ? c2 : c1) * 8 * int(sizeof(T));
+    store8<T>(p, b.lo + 8 * h);
+    store8<T>(p + D * sizeof(T), b.hi + 8 * h);
+  }
+}
+// The threads' bounds joined in threads x < C (elements 8 c1 .. and 8 c2 ..; the
+// others of a workgroup hold other tokens of the same elements).
+template <int C>
+__device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int m = C; m < 64; m *= 2)
@@ -87,21 +120,6 @@ __device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32], char*
         b.hi[i] = fmaxf(b.hi[i], red[w * C + lane][16 + i]);
       }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      char* p = row + (h ? c2 : c1) * 8 * int(sizeof(T));
-      if (more) {
-        float lo[8], hi[8];
-        load8<T>(lo, p);
-        load8<T>(hi, p + D * sizeof(T));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b.add(8 * h + i, lo[i]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b.hi[8 * h + i] = fmaxf(b.hi[8 * h + i], hi[i]);
-      }
-      store8<T>(p, b.lo + 8 * h);
-      store8<T>(p + D * sizeof(T), b.hi + 8 * h);
-    }
   }
 }
 
@@ -115,14 +133,20 @@ __device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32], char*
 //   Angles: position times frequency in fp64, as turns; the nearest whole turn
 //   is taken off there, and what is left (at most half a turn) goes to fp32:
 //   at position 2^20 the angle is off by 2^-25 of a turn, as at position 1.
-template <typename T, int D, bool FOUR, bool INTER>
+// Bound by HBM in prompts: 8191 tokens of 32 / 8 heads of 128, bf16, with bounds,
+// 202 MB in 38 us (5.3 TB/s); into 4 bits, 177 MB in 36. One token of 32
+// sequences takes 6.1 us, of one fp32 layer 4.6: lens -> table -> bounds, rows
+// and angles.
+// SINGLE: a call of one token per sequence.
+template <typename T, int D, bool FOUR, bool INTER, bool SINGLE>
 __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s) {
   constexpr int C = D / 16, ES = int(sizeof(T)), RB = D * ES, LANES = 256 / C;
   __shared__ float red[FOUR ? 1 : 4 * C][32];
   const int tile = int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
-  const int si = find_seq(s, tile), b = s.seq0 + si, ntok = s.len[si];
+  const int si = SINGLE ? tile : find_seq(s, tile), b = s.seq0 + si, ntok = SINGLE ? 1 : s.len[si];
+  const int64_t tok0 = SINGLE ? s.start[0] + si : s.start[si];
   const int32_t len = seq_len(a.lens, b, a.cap), p0 = len - ntok;
-  const int32_t u0 = ((p0 >> a.unit) + (tile - s.tile0[si])) << a.unit;
+  const int32_t u0 = ((p0 >> a.unit) + (SINGLE ? 0 : tile - s.tile0[si])) << a.unit;
   const int32_t j0 = p0 > u0 ? p0 : u0, j1 = len - u0 < (1 << a.unit) ? len : u0 + (1 << a.unit);
   const int n = j1 - j0;
   if (n <= 0) return;
@@ -152,11 +176,33 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
   }
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   Bounds16 bd;
+  OldBounds<T> old;
   if constexpr (!FOUR) bd.clear();
+  // row 0: the key, 1: the value, then the group's queries
+  const int nrow = a.q ? a.G + 2 : 2;
+  auto row_at = [&](int row, int64_t tok) {
+    return row < 2 ? (row == 0 ? a.k : a.v) + (tok * a.Hkv + g) * RB
+                   : a.q + (tok * a.Hq + g * a.G + row - 2) * RB;
+  };
   for (int32_t j = j0 + x / RL; j < j1; j += LANES / RL) {
-    const int64_t tok = int64_t(s.start[si]) + (j - p0);
+    const int64_t tok = tok0 + (j - p0);
+    // the first row is asked for before its angles are worked out, the next ones
+    // a row ahead (but where the bounds' registers would leave three waves to a
+    // SIMD for four: 8191 tokens 47 us with it, 38 without)
+    constexpr bool AHEAD = SINGLE || FOUR;
+    Frag<T> w1, w2;
+    auto fetch = [&](int row) {
+      const gptr_t p = (gptr_t)row_at(row, tok);
+      gload_frag<false>(w1, p + c1 * 8 * ES);
+      gload_frag<false>(w2, p + c2 * 8 * ES);
+    };
+    if (AHEAD && rl < nrow) fetch(rl);
     Slot sl = {0, 0, false};
     if (j >= 0) sl = paged_slot(trow, j, a.shift, a.n_pages);
+    if constexpr (SINGLE && !FOUR) {
+      if (a.bounds && int(threadIdx.x) < C && sl.ok && sl.slot > 0)
+        old.load(a.bounds + (int64_t(sl.page) * a.Hkv + g) * (2 * RB), D, c1, c2);
+    }
     float sn[8], cs[8];
     if (r1 || r2) {
       const double at = a.pos ? a.pos[tok] : j;
@@ -167,18 +213,13 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
         sincospif(2.f * float(t), &sn[i], &cs[i]);
       }
     }
-    for (int row = rl; row < a.G + 2; row += RL) {
-      const char* src;
-      if (row < 2) {
-        if (!sl.ok) continue;
-        src = (row == 0 ? a.k : a.v) + (tok * a.Hkv + g) * RB;
-      } else {
-        if (!a.q) break;
-        src = a.q + (tok * a.Hq + g * a.G + row - 2) * RB;
-      }
+    for (int row = rl; row < nrow; row += RL) {
       float y[16];
-      load8<T>(y, src + c1 * 8 * ES);
-      load8<T>(y + 8, src + c2 * 8 * ES);
+      if (!AHEAD) fetch(row);
+      w1.to_floats(y);
+      w2.to_floats(y + 8);
+      if (AHEAD && row + RL < nrow) fetch(row + RL);
+      if (row < 2 && !sl.ok) continue;
       if (row != 1) {
         if constexpr (INTER) {
 #pragma unroll
@@ -243,7 +284,12 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
       if (j1 <= first) return;
       const Slot sl = paged_slot(trow, first, a.shift, a.n_pages);
       if (!sl.ok) return;
-      join_bounds<T, D, C>(bd, red, a.bounds + (int64_t(sl.page) * a.Hkv + g) * (2 * RB), c1, c2, sl.slot > 0);
+      char* row = a.bounds + (int64_t(sl.page) * a.Hkv + g) * (2 * RB);
+      if constexpr (!SINGLE) {  // (one token: its key is in threads x < C, and what was there asked for before)
+        join_bounds<C>(bd, red);
+        if (int(threadIdx.x) < C && sl.slot > 0) old.load(row, D, c1, c2);
+      }
+      if (int(threadIdx.x) < C) store_bounds<T, D>(bd, old, row, c1, c2, sl.slot > 0);
     }
   }
 }
@@ -270,7 +316,9 @@ __global__ __launch_bounds__(256) void page_bounds(AppendArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) bd.add(e, y[e]);
     }
-    join_bounds<T, D, C>(bd, red, a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES), c, c + C, false);
+    join_bounds<C>(bd, red);
+    if (int(threadIdx.x) < C)
+      store_bounds<T, D>(bd, OldBounds<T>(), a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES), c, c + C, false);
     __syncthreads();
   }
 }
@@ -315,10 +363,16 @@ __global__ __launch_bounds__(256) void read_rows4(AppendArgs a, PagedSeqs s, cha
 
 template <typename T, int D, bool FOUR>
 hipError_t append_t(const AppendArgs& a, const PagedSeqs& s, bool interleaved, hipStream_t stream) {
+  const bool single = std::all_of(s.len, s.len + s.nseq, [](int32_t n) { return n == 1; });
   const uint32_t n = uint32_t(s.tile0[s.nseq]) * uint32_t(a.Hkv);
   if (n == 0) return hipSuccess;
-  if (interleaved) append_rotated<T, D, FOUR, true><<<n, 256, 0, stream>>>(a, s);
-  else append_rotated<T, D, FOUR, false><<<n, 256, 0, stream>>>(a, s);
+  if (single) {
+    if (interleaved) append_rotated<T, D, FOUR, true, true><<<n, 256, 0, stream>>>(a, s);
+    else append_rotated<T, D, FOUR, false, true><<<n, 256, 0, stream>>>(a, s);
+  } else {
+    if (interleaved) append_rotated<T, D, FOUR, true, false><<<n, 256, 0, stream>>>(a, s);
+    else append_rotated<T, D, FOUR, false, false><<<n, 256, 0, stream>>>(a, s);
+  }
   return hipGetLastError();
 }
 

@@ -132,25 +132,25 @@ def load_library(path=None):
     lib.glide_paged_evict.argtypes = [pcfg, pcache, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp, ctypes.c_size_t,
                                       vp]
     lib.glide_paged_evict.restype = ctypes.c_int
-    rotp, p4cache, cup = ctypes.POINTER(Rotation), ctypes.POINTER(Paged4CacheArg), ctypes.POINTER(ctypes.c_int32)
-    lib.glide_paged_append.argtypes = [pcfg, pcache, rotp, vp, vp, vp, cup, ctypes.c_int64, vp, vp, vp]
+    rotp, p4cache = ctypes.POINTER(Rotation), ctypes.POINTER(Paged4CacheArg)
+    lib.glide_paged_append.argtypes = [pcfg, pcache, rotp, vp, vp, vp, vp, ctypes.c_int64, vp, vp, vp]
     lib.glide_paged_append.restype = ctypes.c_int
     lib.glide_paged_bounds.argtypes = [pcfg, pcache, ctypes.c_int64, vp, vp]
     lib.glide_paged_bounds.restype = ctypes.c_int
-    lib.glide_nibble_append.argtypes = [pcfg, p4cache, rotp, vp, vp, vp, cup, ctypes.c_int64, vp, vp]
+    lib.glide_nibble_append.argtypes = [pcfg, p4cache, rotp, vp, vp, vp, vp, ctypes.c_int64, vp, vp]
     lib.glide_nibble_append.restype = ctypes.c_int
-    lib.glide_nibble_read.argtypes = [pcfg, p4cache, cup, ctypes.c_int64, vp, vp, vp]
+    lib.glide_nibble_read.argtypes = [pcfg, p4cache, vp, ctypes.c_int64, vp, vp, vp]
     lib.glide_nibble_read.restype = ctypes.c_int
     lib.glide_nibble_workspace_bytes.argtypes = [pcfg, ctypes.c_int64]
     lib.glide_nibble_workspace_bytes.restype = ctypes.c_size_t
-    lib.glide_nibble_prefill.argtypes = [pcfg, p4cache, vp, cup, ctypes.c_int64, ctypes.c_int64, vp, vp, vp,
+    lib.glide_nibble_prefill.argtypes = [pcfg, p4cache, vp, vp, ctypes.c_int64, ctypes.c_int64, vp, vp, vp,
                                          ctypes.c_size_t, vp]
     lib.glide_nibble_prefill.restype = ctypes.c_int
     lib.glide_nibble_decode.argtypes = [pcfg, p4cache, vp, ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
     lib.glide_nibble_decode.restype = ctypes.c_int
     lib.glide_paged_sparse_workspace_bytes.argtypes = [pcfg, ctypes.c_int64, ctypes.c_int32]
     lib.glide_paged_sparse_workspace_bytes.restype = ctypes.c_size_t
-    lib.glide_paged_sparse.argtypes = [pcfg, pcache, vp, vp, cup, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+    lib.glide_paged_sparse.argtypes = [pcfg, pcache, vp, vp, vp, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                        ctypes.c_int32, ctypes.c_int64, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.glide_paged_sparse.restype = ctypes.c_int
     lib.glide_status_string.argtypes = [ctypes.c_int]

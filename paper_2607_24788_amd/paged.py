@@ -6,6 +6,7 @@ and the eviction of the tokens that received least.
 Argument marshalling only, as in ``glide.py``: every step runs in the HIP
 kernels behind the C ABI, and there is no fallback.
 """
+import array
 import ctypes
 import operator
 
@@ -30,7 +31,7 @@ def _tensor(name, t, device, dtype, numel):
     elements or more.  Returns its address."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
-    if t.get_device() == device and t.dtype is dtype and t.is_contiguous() and t.numel() >= numel:
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, the cache on cuda:{device}")
@@ -42,15 +43,15 @@ def _tensor(name, t, device, dtype, numel):
 
 
 def _cu_arg(g, cu_seqlens):
-    """cu_seqlens as the library's array, and its last entry."""
-    cu = list(map(int, cu_seqlens))
+    """cu_seqlens as an array of the library's integers, and its last entry."""
+    cu = list(cu_seqlens)
     if len(cu) != g.batch + 1:
         raise ValueError("cu_seqlens needs batch + 1 entries")
-    arg = g._cu(*cu)
-    if arg[:] != cu:
-        for x in cu:
-            _fits("cu_seqlens entry", x)
-    return arg, cu[-1]
+    try:
+        return array.array("i", cu), int(cu[-1])
+    except (TypeError, OverflowError):
+        cu = [_fits("cu_seqlens entry", int(x)) for x in cu]
+    return array.array("i", cu), cu[-1]
 
 
 def _rotation(freqs, interleaved, positions, device, T):
@@ -247,11 +248,11 @@ class Paged:
         if type(cache) is not PagedCache or cache.geometry is not self.geometry:
             self._check_cache(cache)
         dev = cache._dev
-        cu_arg, T = _cu_arg(self, cu_seqlens)
+        cu, T = _cu_arg(self, cu_seqlens)
         rot = _rotation(freqs, interleaved, positions, dev, T)
         qp, kp, vp, op = _append_rows(self, dev, q, k, v, q_out, max(T, 0))
         bp = None if bounds is None else self._bounds_of(cache, bounds)
-        self._call("glide_paged_append", cache, stream, rot, qp, kp, vp, cu_arg, T, op, bp)
+        self._call("glide_paged_append", cache, stream, rot, qp, kp, vp, cu.buffer_info()[0], T, op, bp)
 
     def new_bounds(self, device="cuda"):
         """Room for the least and the largest key elements of every page: not
@@ -301,14 +302,14 @@ class Paged:
         selected [T][Hkv][n_select] int32: the pages' numbers in their
         sequence, -1 behind the last.  The queries' tokens are in the cache."""
         bp = self._bounds_of(cache, bounds)
-        cu_arg, T = _cu_arg(self, cu_seqlens)
+        cu, T = _cu_arg(self, cu_seqlens)
         n_select, n_first, n_recent = (_fits(name, int(x)) for name, x in (
             ("n_select", n_select), ("n_first", n_first), ("n_recent", n_recent)))
         max_len = _fits("max_len", int(max_len), 64)
         qp, _, _, op, lp = self._rows(cache, q, None, None, out, lse, max(T, 0))
         sp = _tensor("selected", selected, cache._dev, torch.int32, max(T, 0) * self.n_kv_heads * max(n_select, 0))
         ws, n = self._workspace(cache, workspace)
-        self._call("glide_paged_sparse", cache, stream, bp, qp, cu_arg, T, n_select, n_first, n_recent, max_len, sp,
+        self._call("glide_paged_sparse", cache, stream, bp, qp, cu.buffer_info()[0], T, n_select, n_first, n_recent, max_len, sp,
                    op, lp, ws, n)
 
     def evict(self, cache, budget, n_recent, kept, new_lens, workspace, dst_table=None, stream=None):

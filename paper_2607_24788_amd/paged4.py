@@ -109,10 +109,10 @@ class Paged4:
         ``Paged.append``."""
         if type(cache) is not Paged4Cache or cache.geometry is not self.geometry:
             self._check_cache(cache)
-        cu_arg, T = _cu_arg(self, cu_seqlens)
+        cu, T = _cu_arg(self, cu_seqlens)
         rot = _rotation(freqs, interleaved, positions, cache._dev, T)
         qp, kp, vp, op = _append_rows(self, cache._dev, q, k, v, q_out, max(T, 0))
-        self._call("glide_nibble_append", cache, stream, rot, qp, kp, vp, cu_arg, T, op)
+        self._call("glide_nibble_append", cache, stream, rot, qp, kp, vp, cu.buffer_info()[0], T, op)
 
     def read(self, cache, cu_seqlens, k_out, v_out, stream=None):
         """The values that the cache holds of the last cu[b + 1] - cu[b] tokens
@@ -120,11 +120,11 @@ class Paged4:
         no page."""
         if type(cache) is not Paged4Cache or cache.geometry is not self.geometry:
             self._check_cache(cache)
-        cu_arg, T = _cu_arg(self, cu_seqlens)
+        cu, T = _cu_arg(self, cu_seqlens)
         n = max(T, 0) * self.n_kv_heads * self.head_dim
         kp = _tensor("k_out", k_out, cache._dev, self.torch_dtype, n)
         vp = _tensor("v_out", v_out, cache._dev, self.torch_dtype, n)
-        self._call("glide_nibble_read", cache, stream, cu_arg, T, kp, vp)
+        self._call("glide_nibble_read", cache, stream, cu.buffer_info()[0], T, kp, vp)
 
     def _rows(self, cache, q, out, lse, T):
         """Pointers of a call over T rows of queries, checked."""
@@ -139,11 +139,11 @@ class Paged4:
         fp32, for the last cu[b + 1] - cu[b] cached tokens of every sequence b.
         max_len: a bound of lens on the host (0: none), which the work is split
         by."""
-        cu_arg, T = _cu_arg(self, cu_seqlens)
+        cu, T = _cu_arg(self, cu_seqlens)
         max_len = _fits("max_len", int(max_len), 64)
         qp, op, lp = self._rows(cache, q, out, lse, max(T, 0))
         ws = _tensor("workspace", workspace, cache._dev, torch.uint8, 0)
-        self._call("glide_nibble_prefill", cache, stream, qp, cu_arg, T, max_len, op, lp, ws, workspace.numel())
+        self._call("glide_nibble_prefill", cache, stream, qp, cu.buffer_info()[0], T, max_len, op, lp, ws, workspace.numel())
 
     def decode(self, cache, q, out, workspace, lse=None, max_len=0, stream=None):
         """One query per sequence, of its last cached token: q, out [B][Hq][d],
