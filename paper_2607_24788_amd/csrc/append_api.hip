@@ -40,6 +40,14 @@ void fill_pools(const glide_paged_config* c, const glide_paged_cache* k, AppendA
   }
 }
 
+// log2 of the tokens of a workgroup where a page need not be one workgroup's:
+// fewer where there would be few workgroups.
+int32_t append_unit(const glide_paged_config* c, int64_t total) {
+  int32_t unit = __builtin_ctz(uint32_t(kAppendTokens));
+  while (unit > 4 && (total * c->n_kv_heads >> unit) < 4 * kPagedRound) --unit;
+  return unit;
+}
+
 // An append, its cache checked and filled in.
 glide_status append(const glide_paged_config* c, const glide_rotation* rot, const void* q, const void* k,
                     const void* v, const int32_t* cu, int64_t total, void* q_out, AppendArgs a, bool four,
@@ -60,7 +68,7 @@ glide_status append(const glide_paged_config* c, const glide_rotation* rot, cons
     a.freqs = rot->freqs;
     a.pos = rot->positions;
   }
-  a.unit = a.bounds ? a.shift : __builtin_ctz(uint32_t(kAppendTokens));
+  a.unit = a.bounds ? a.shift : append_unit(c, total);
   for (int b0 = 0; b0 < c->batch;) {
     PagedSeqs t;
     // positions p0 .. p0 + T - 1 lie in so many units, wherever p0 is
@@ -136,10 +144,10 @@ glide_status glide_nibble_read(const glide_paged_config* cfg, const glide_nibble
   AppendArgs a;
   fill_append(cfg, cache->block_table, cache->lens, &a);
   a.p4 = {cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales};
-  a.unit = __builtin_ctz(uint32_t(kAppendTokens));
+  a.unit = append_unit(cfg, total_tokens);
   for (int b0 = 0; b0 < cfg->batch;) {
     PagedSeqs t;
-    b0 = next_launch(cfg, cu_seqlens_host, b0, &t, [&](int64_t T) { return (T + kAppendTokens - 1) / kAppendTokens; });
+    b0 = next_launch(cfg, cu_seqlens_host, b0, &t, [&](int64_t T) { return (T + (int64_t(1) << a.unit) - 1) >> a.unit; });
     s = hip_status(launch_read4(a, t, static_cast<char*>(k_out), static_cast<char*>(v_out), cfg->head_dim, cfg->dtype,
                                 hipStream_t(stream)));
     if (s != GLIDE_OK) return s;
