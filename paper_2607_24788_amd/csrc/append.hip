@@ -134,9 +134,10 @@ __device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32]) {
 //   is taken off there, and what is left (at most half a turn) goes to fp32:
 //   at position 2^20 the angle is off by 2^-25 of a turn, as at position 1.
 // Bound by HBM in prompts: 8191 tokens of 32 / 8 heads of 128, bf16, with bounds,
-// 202 MB in 38 us (5.3 TB/s); into 4 bits, 177 MB in 36. One token of 32
-// sequences takes 6.1 us, of one fp32 layer 4.6: lens -> table -> bounds, rows
-// and angles.
+// 202 MB in 46 us (4.4 TB/s; from memory.  Rows are read past the caches: 49 us
+// through them), 36 out of the caches; into 4 bits 177 MB in 45 and 31.  One
+// token of 32 sequences takes 6.1 us, of one fp32 layer 4.6: lens -> table ->
+// bounds, rows and angles.
 // SINGLE: a call of one token per sequence.
 template <typename T, int D, bool FOUR, bool INTER, bool SINGLE>
 __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s) {
@@ -193,8 +194,8 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
     Frag<T> w1, w2;
     auto fetch = [&](int row) {
       const gptr_t p = (gptr_t)row_at(row, tok);
-      gload_frag<false>(w1, p + c1 * 8 * ES);
-      gload_frag<false>(w2, p + c2 * 8 * ES);
+      gload_frag<true>(w1, p + c1 * 8 * ES);
+      gload_frag<true>(w2, p + c2 * 8 * ES);
     };
     if (AHEAD && rl < nrow) fetch(rl);
     Slot sl = {0, 0, false};

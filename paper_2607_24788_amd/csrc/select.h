@@ -10,6 +10,10 @@ namespace glide {
 constexpr int kScoreRows = 8;
 // Its workgroups take more pages each where there would be more than these.
 constexpr int64_t kScoreWorkgroups = 4096;
+// As many units (row, KV head) have a wave each (picked_rows), eight to a CU;
+// fewer share workgroups (attend_rows).  bf16, d = 128: 2048 units of 2048 keys
+// 168 us by waves, 207 by workgroups; 1024 of them 131, 111.
+constexpr int64_t kPickedUnits = 2048;
 // A launch's scores take at most so many bytes (one row's at least).
 constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
 
@@ -33,5 +37,9 @@ struct SelectArgs {
 // rows among row0 .. row1 - 1.  pages: of a sequence, at most (it sizes a grid
 // only)
 hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages, int d, int dtype, hipStream_t stream);
+
+// The attention of a launch's units (row, KV head), a wave each; a as for
+// launch_paged_decode with per_head, in one piece.
+hipError_t launch_picked(const PagedArgs& a, int32_t units, int d, int dtype, hipStream_t stream);
 
 }  // namespace glide

@@ -342,6 +342,169 @@ __global__ __launch_bounds__(NT) void select_pages(SelectArgs a, PagedSeqs s) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Attention of many (row, KV head) units over their selected pages, a wave to a
+// unit: the products and the way through LDS of a tile of 32 keys are those of
+// attend_rows, whose four waves share a unit; without their join, and with eight
+// units to a CU instead of two, it goes further where units are many.  Bound by
+// the caches: neighbouring rows' pages are the same or other ones.
+// a.table and a.lens have a row for every unit; every page in it is allocated.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void picked_rows(PagedArgs a, int32_t units) {
+  constexpr int KK = D / 32, CT = D / 16, ES = int(sizeof(T)), TK = 32;
+  constexpr bool KLDS = ES == 2;
+  constexpr int RS = D + (KLDS ? 16 : 4), LPR = D * ES / 16, RPI = 64 / LPR, NL = TK / RPI;
+  __shared__ __align__(16) T klds[KLDS ? 4 : 1][KLDS ? TK * RS : 1];
+  __shared__ __align__(16) T vlds[4][TK * RS];
+  const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t unit = int32_t(blockIdx.x) * 4 + wave;
+  if (unit >= units) return;
+  const int g = unit % a.Hkv;
+  const int32_t held = __builtin_amdgcn_readfirstlane(a.lens[unit]);
+  const int32_t* trow = a.table + int64_t(unit) * a.max_pages;
+  const bool rok = n < a.G;
+  const int64_t orow = int64_t(unit / a.Hkv) * a.Hq + g * a.G + (rok ? n : 0);
+  Frag<T> qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    qf[kk].load(reinterpret_cast<const T*>(a.q) + orow * D + 32 * kk + 8 * lg);
+    if (!rok) qf[kk].zero();
+    if (a.scale < 0) qf[kk].negate();  // scores of -q: the frame is a maximum of raw scores
+  }
+  const float c = fabsf(a.scale);
+  float m = kNoMax, l = 0.f;
+  f32x4_t acc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) acc[ct] = zero4();
+  T *kt = klds[KLDS ? wave : 0], *vt = vlds[wave];
+
+  // rows of a tile: lane x looks up key x % 32 a tile ahead; rows behind the last are zeros
+  auto look = [&](int32_t x) {
+    const int32_t v = x + (lane & 31);
+    return v < held ? trow[v >> a.shift] : -1;
+  };
+  Frag<T> kf[2][KK], vf[2][KK];  // bf16: NL pieces each
+  auto fetch = [&](int32_t x, int32_t page) {
+#pragma unroll
+    for (int e = 0; e < (KLDS ? NL : 2); ++e) {
+      const int row = KLDS ? e * RPI + lane / LPR : 16 * e + n;
+      const int32_t p = __shfl(page, row);
+      const Slot sl = {p, (x + row) & ((1 << a.shift) - 1), true};
+      const gptr_t kr = p >= 0 ? (gptr_t)a.kp + slot_offset(a.ks, sl, g) : (gptr_t)zero_row;
+      const gptr_t vr = p >= 0 ? (gptr_t)a.vp + slot_offset(a.vs, sl, g) : (gptr_t)zero_row;
+      if constexpr (KLDS) {
+        gload_frag<false>(kf[e / KK][e % KK], kr + (lane % LPR) * 16);
+        gload_frag<false>(vf[e / KK][e % KK], vr + (lane % LPR) * 16);
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) gload_frag<false>(kf[e][kk], kr + (32 * kk + 8 * lg) * ES);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) gload_frag<false>(vf[e][kk], vr + (32 * kk + 8 * lg) * ES);
+      }
+    }
+  };
+  int32_t page = 0;
+  if (held > 0) {
+    const int32_t first = look(0);
+    page = look(TK);
+    fetch(0, first);
+  }
+  for (int32_t x = 0; x < held; x += TK) {
+    f32x4_t sc[2] = {zero4(), zero4()};
+    if constexpr (KLDS) {
+#pragma unroll
+      for (int e = 0; e < NL; ++e) {
+        const int at = (e * RPI + lane / LPR) * RS + (lane % LPR) * 8;
+        *reinterpret_cast<uint4*>(kt + at) = kf[e / KK][e % KK].v;
+        *reinterpret_cast<uint4*>(vt + at) = vf[e / KK][e % KK].v;
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          sc[t] = mma(kf[t][kk], qf[kk], sc[t]);
+          float w[8];
+          vf[t][kk].to_floats(w);
+          float4* at = reinterpret_cast<float4*>(vt + (16 * t + n) * RS + 32 * kk + 8 * lg);
+          at[0] = make_float4(w[0], w[1], w[2], w[3]);
+          at[1] = make_float4(w[4], w[5], w[6], w[7]);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (x + TK < held) {
+      const int32_t now = page;
+      page = look(x + 2 * TK);
+      fetch(x + TK, now);
+    }
+    if constexpr (KLDS) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          Frag<T> k;
+          k.load(kt + (16 * t + n) * RS + 32 * kk + 8 * lg);
+          sc[t] = mma(k, qf[kk], sc[t]);
+        }
+    }
+    if (held - x < TK) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (x + 16 * t + 4 * lg + i >= held) sc[t][i] = -INFINITY;
+    }
+    // the frame moves only when a score passes it by 2^8: weights up to that
+    // round alike, and fp32 sums hold them
+    float mx = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[t][i]);
+    mx = lg_max(mx) * c;
+    if (__any(mx > m + 8.f)) {
+      const float m2 = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= f;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[ct][i] *= f;
+    }
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], c, -m));
+      l += p[i];
+    }
+    Frag<T> pf;
+    pf.set8(p);  // bf16: weights rounded to half a step, 2^-8 of each at most
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      Frag<T> vc;
+      load_colfrag2(vc, vt, RS, 4 * lg, 16 + 4 * lg, 16 * ct);
+      acc[ct] = mma(vc, pf, acc[ct]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  l = lg_sum(l);
+  if (!rok) return;
+  if (lg == 0 && a.lse) a.lse[orow] = (l > 0.f ? m + __builtin_amdgcn_logf(l) : l == 0.f ? -INFINITY : l) * kLn2;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* w = reinterpret_cast<T*>(a.out) + orow * D + 4 * lg;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float y[4] = {acc[ct][0] * inv, acc[ct][1] * inv, acc[ct][2] * inv, acc[ct][3] * inv};
+    if constexpr (ES == 2)
+      *reinterpret_cast<uint2*>(w + 16 * ct) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+    else
+      *reinterpret_cast<float4*>(w + 16 * ct) = make_float4(y[0], y[1], y[2], y[3]);
+  }
+}
+
 template <typename T, int D>
 hipError_t scores_t(const SelectArgs& a, const PagedSeqs& s, int64_t pages, hipStream_t stream) {
   const dim3 grid(uint32_t(s.tile0[s.nseq]) * uint32_t(a.Hkv),
@@ -364,6 +527,18 @@ hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages,
   if (a.max_pages <= 1024) select_pages<256, true><<<units, 256, 0, stream>>>(a, s);
   else if (a.max_pages <= 4096) select_pages<1024, true><<<units, 1024, 0, stream>>>(a, s);
   else select_pages<1024, false><<<units, 1024, 0, stream>>>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_picked(const PagedArgs& a, int32_t units, int d, int dtype, hipStream_t stream) {
+  const uint32_t n = (uint32_t(units) + 3) / 4;
+  if (dtype == GLIDE_BF16) {
+    if (d == 128) picked_rows<bf16_t, 128><<<n, 256, 0, stream>>>(a, units);
+    else picked_rows<bf16_t, 64><<<n, 256, 0, stream>>>(a, units);
+  } else {
+    if (d == 128) picked_rows<float, 128><<<n, 256, 0, stream>>>(a, units);
+    else picked_rows<float, 64><<<n, 256, 0, stream>>>(a, units);
+  }
   return hipGetLastError();
 }
 

@@ -129,13 +129,17 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
     a.lse = lse ? lse + row0 * cfg->n_q_heads : nullptr;
     a.acc = reinterpret_cast<float*>(ws + w.acc);
     a.ml = reinterpret_cast<float*>(ws + w.ml);
-    // Pieces for a round of workgroups, none where every CU has one without: 8
-    // units of 4096 keys, 128 / 256 keys a piece 20.8 / 22.4 us; 192 of 2112, two
-    // pieces 49.5, three 56, one 54; 256 of 2048, one 76.5, two 77.7; 2048 of
-    // 2048, one 207, two 226.
-    const int64_t split = units >= kPagedRound / 2 ? 1 : kPagedRound / units;
-    set_pieces(std::min(split, std::min((keys + kPieceMin - 1) / kPieceMin, max_pieces(units, kPagedRows))), keys, &a);
-    s = hip_status(launch_paged_decode(a, keys, cfg->head_dim, cfg->dtype, hipStream_t(stream)));
+    if (units >= kPickedUnits) {
+      s = hip_status(launch_picked(a, int32_t(units), cfg->head_dim, cfg->dtype, hipStream_t(stream)));
+    } else {
+      // Pieces for a round of workgroups, none where every CU has one without: 8
+      // units of 4096 keys, 128 / 256 keys a piece 20.8 / 22.4 us; 192 of 2112, two
+      // pieces 49.5, three 56, one 54; 256 of 2048, one 76.5, two 77.7.
+      const int64_t split = units >= kPagedRound / 2 ? 1 : kPagedRound / units;
+      set_pieces(std::min(split, std::min((keys + kPieceMin - 1) / kPieceMin, max_pieces(units, kPagedRows))), keys,
+                 &a);
+      s = hip_status(launch_paged_decode(a, keys, cfg->head_dim, cfg->dtype, hipStream_t(stream)));
+    }
     if (s != GLIDE_OK) return s;
     row0 = row1;
   }

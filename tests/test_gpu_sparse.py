@@ -184,6 +184,20 @@ def test_rows_in_several_launches():
     run_sparse(case, [170, 9], 6, 1, 1, max_len=500)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d,Hkv,G,page,sm_scale", [(128, 16, 3, 16, None), (64, 8, 16, 32, -0.3), (128, 32, 1, 1, None)])
+def test_many_units(dtype, d, Hkv, G, page, sm_scale):
+    """As many (row, KV head) units as have a wave each: ragged lengths, empty
+    rows, missing pages, more pages than are selected and fewer."""
+    new = [2100 // Hkv, 3, 0, 9]
+    lens = [new[0] + 90, 3, 40, 5]
+    case = Case(4, Hkv * G, Hkv, d, page, lens, dtype=dtype, seed=470, sm_scale=sm_scale, order="joined")
+    case.table[0, 2] = -1
+    case.dev_table.copy_(case.table)
+    assert sum(new) * Hkv >= 2048
+    run_sparse(case, new, 5, 1, 1)
+
+
 def test_strided_pools_and_another_stream():
     case = Case(2, 8, 2, 128, 32, [500, 260], order="nhd", seed=426)
     s = torch.cuda.Stream()
