@@ -422,7 +422,7 @@ glide_status glide_paged_evict(const glide_paged_config* cfg, const glide_paged_
  *   (x, y) -> (x cos a - y sin a, y cos a + x sin a)
  * Pair i is elements (i, i + rot_dim / 2), or (2i, 2i + 1) with interleaved.
  * Angles are taken in fp64 and as a part of a turn, so that far positions lose
- * nothing; each element is rounded once, to cfg->dtype. */
+ * nothing; products are fp32, and rounded once to cfg->dtype. */
 typedef struct {
   const float* freqs;       /* device [rot_dim / 2]: radians per position, 16-byte aligned */
   const int32_t* positions; /* device [total_tokens], or NULL: each token's position in the cache
@@ -442,9 +442,9 @@ typedef struct {
  *   cu_seqlens_host  as for glide_paged_prefill
  *   bounds    device [n_pages][Hkv][2][d] in cfg->dtype, or NULL: per page, the
  *             least and the largest of its keys by element, as the cache holds
- *             them (NaN left out), brought up to date with the new keys; those
- *             of a page whose first token is not among them are added to (they
- *             are of earlier appends, or of glide_paged_bounds)
+ *             them (NaN left out), brought up to date with the new keys.  Where
+ *             a page has earlier tokens, their bounds are there already (of
+ *             earlier appends, or of glide_paged_bounds)
  * Device pointers 16-byte aligned (positions: 4). */
 glide_status glide_paged_append(const glide_paged_config* cfg, const glide_paged_cache* cache,
                                 const glide_rotation* rotation, const void* q, const void* k, const void* v,

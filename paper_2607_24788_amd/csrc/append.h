@@ -7,8 +7,8 @@
 
 namespace glide {
 
-// Tokens of one workgroup of append_rotated, where no page bounds are kept
-// (with them a workgroup has a page's tokens).
+// Tokens of one workgroup of append_rotated, at most, where it does not keep
+// page bounds (with them a workgroup has a page's tokens).
 constexpr int kAppendTokens = 64;
 
 struct AppendArgs {
@@ -33,6 +33,8 @@ hipError_t launch_append(const AppendArgs& a, const PagedSeqs& s, int d, int dty
                          hipStream_t stream);
 // keys: tokens of a sequence, at most (it sizes a grid only)
 hipError_t launch_page_bounds(const AppendArgs& a, int64_t keys, int d, int dtype, hipStream_t stream);
+// Of the pages with new tokens; seqs.tile0: pages of each sequence, as launch_append with unit = shift.
+hipError_t launch_new_bounds(const AppendArgs& a, const PagedSeqs& s, int d, int dtype, hipStream_t stream);
 hipError_t launch_read4(const AppendArgs& a, const PagedSeqs& s, char* ko, char* vo, int d, int dtype,
                         hipStream_t stream);
 

@@ -295,33 +295,52 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
   }
 }
 
-// The bounds of every page of the sequences, from the keys in the cache.
+// The bounds of a page of n tokens from its keys in the cache, by a workgroup.
+template <typename T, int D>
+__device__ __forceinline__ void bounds_of_page(const AppendArgs& a, int32_t page, int g, int32_t n, float (*red)[32]) {
+  constexpr int C = D / 16, ES = int(sizeof(T)), LANES = 256 / C;
+  const int c = threadIdx.x % C;
+  Bounds16 bd;
+  bd.clear();
+  for (int32_t t = threadIdx.x / C; t < n; t += LANES) {
+    const char* src = a.kp + slot_offset(a.ks, Slot{page, t, true}, g);
+    float y[16];
+    load8<T>(y, src + c * 8 * ES);
+    load8<T>(y + 8, src + (c + C) * 8 * ES);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) bd.add(e, y[e]);
+  }
+  join_bounds<C>(bd, red);
+  if (int(threadIdx.x) < C)
+    store_bounds<T, D>(bd, OldBounds<T>(), a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES), c, c + C, false);
+}
+// Of every page of the sequences.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void page_bounds(AppendArgs a) {
-  constexpr int C = D / 16, ES = int(sizeof(T)), LANES = 256 / C;
-  __shared__ float red[4 * C][32];
+  __shared__ float red[4 * (D / 16)][32];
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv;
   const int32_t len = seq_len(a.lens, b, a.cap);
-  const int c = threadIdx.x % C;
   for (int32_t i = blockIdx.y; (int64_t(i) << a.shift) < len; i += gridDim.y) {
     const int32_t page = a.table[int64_t(b) * a.max_pages + i];
     if (uint32_t(page) >= uint32_t(a.n_pages)) continue;
-    const int32_t left = len - (i << a.shift), n = left < (1 << a.shift) ? left : 1 << a.shift;
-    Bounds16 bd;
-    bd.clear();
-    for (int32_t t = threadIdx.x / C; t < n; t += LANES) {
-      const char* src = a.kp + slot_offset(a.ks, Slot{page, t, true}, g);
-      float y[16];
-      load8<T>(y, src + c * 8 * ES);
-      load8<T>(y + 8, src + (c + C) * 8 * ES);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) bd.add(e, y[e]);
-    }
-    join_bounds<C>(bd, red);
-    if (int(threadIdx.x) < C)
-      store_bounds<T, D>(bd, OldBounds<T>(), a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES), c, c + C, false);
+    const int32_t left = len - (i << a.shift);
+    bounds_of_page<T, D>(a, page, g, left < (1 << a.shift) ? left : 1 << a.shift, red);
     __syncthreads();
   }
+}
+// Of the pages that an append wrote to (a workgroup per page and KV head).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void new_bounds(AppendArgs a, PagedSeqs s) {
+  __shared__ float red[4 * (D / 16)][32];
+  const int tile = int(blockIdx.x) / a.Hkv, g = int(blockIdx.x) % a.Hkv;
+  const int si = find_seq(s, tile), b = s.seq0 + si;
+  const int32_t len = seq_len(a.lens, b, a.cap), p0 = len - s.len[si] > 0 ? len - s.len[si] : 0;
+  const int32_t i = (p0 >> a.shift) + (tile - s.tile0[si]);
+  if ((int64_t(i) << a.shift) >= len) return;
+  const int32_t page = a.table[int64_t(b) * a.max_pages + i];
+  if (uint32_t(page) >= uint32_t(a.n_pages)) return;
+  const int32_t left = len - (i << a.shift);
+  bounds_of_page<T, D>(a, page, g, left < (1 << a.shift) ? left : 1 << a.shift, red);
 }
 
 // The last tokens of every sequence as rows of the call's type: a thread has
@@ -404,6 +423,19 @@ hipError_t launch_page_bounds(const AppendArgs& a, int64_t keys, int d, int dtyp
   } else {
     if (d == 128) page_bounds<float, 128><<<grid, 256, 0, stream>>>(a);
     else page_bounds<float, 64><<<grid, 256, 0, stream>>>(a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_new_bounds(const AppendArgs& a, const PagedSeqs& s, int d, int dtype, hipStream_t stream) {
+  const uint32_t n = uint32_t(s.tile0[s.nseq]) * uint32_t(a.Hkv);
+  if (n == 0) return hipSuccess;
+  if (dtype == GLIDE_BF16) {
+    if (d == 128) new_bounds<bf16_t, 128><<<n, 256, 0, stream>>>(a, s);
+    else new_bounds<bf16_t, 64><<<n, 256, 0, stream>>>(a, s);
+  } else {
+    if (d == 128) new_bounds<float, 128><<<n, 256, 0, stream>>>(a, s);
+    else new_bounds<float, 64><<<n, 256, 0, stream>>>(a, s);
   }
   return hipGetLastError();
 }

@@ -41,10 +41,11 @@ void fill_pools(const glide_paged_config* c, const glide_paged_cache* k, AppendA
 }
 
 // log2 of the tokens of a workgroup where a page need not be one workgroup's:
-// fewer where there would be few workgroups.
+// fewer where there would be few workgroups (512 tokens, 32 / 8 heads of 128:
+// units of 64 / 16 tokens 9.4 / 5.6 us).
 int32_t append_unit(const glide_paged_config* c, int64_t total) {
   int32_t unit = __builtin_ctz(uint32_t(kAppendTokens));
-  while (unit > 4 && (total * c->n_kv_heads >> unit) < 4 * kPagedRound) --unit;
+  while (unit > 2 && (total * c->n_kv_heads >> unit) < (unit > 4 ? 4 * kPagedRound : kPagedRound / 2)) --unit;
   return unit;
 }
 
@@ -68,13 +69,29 @@ glide_status append(const glide_paged_config* c, const glide_rotation* rot, cons
     a.freqs = rot->freqs;
     a.pos = rot->positions;
   }
+  // Bounds by the append itself, a page to a workgroup, where that makes enough
+  // workgroups or each has few rows (one token, 192 rows); else from the keys in
+  // the cache, by a launch of its own.  512 tokens, 32 / 8 heads, pages of 256:
+  // 34 us / 11.9 apart, of 64: 13.2 / 10.7; 4 heads, pages of 32: 7.9 / 9.7.
+  int64_t longest = 0;
+  for (int32_t b = 0; b < c->batch; ++b) longest = std::max<int64_t>(longest, cu[b + 1] - cu[b]);
+  AppendArgs after = a;
+  const bool apart = a.bounds && longest > 1 && (total * c->n_kv_heads >> a.shift) < kPagedRound &&
+                     std::min<int64_t>(longest, c->page_size) * (a.G + 2) > 192;
+  if (apart) a.bounds = nullptr;
   a.unit = a.bounds ? a.shift : append_unit(c, total);
+  // positions p0 .. p0 + T - 1 lie in so many units, wherever p0 is
+  auto units = [](int64_t T, int32_t unit) { return ((T + (int64_t(1) << unit) - 2) >> unit) + 1; };
   for (int b0 = 0; b0 < c->batch;) {
     PagedSeqs t;
-    // positions p0 .. p0 + T - 1 lie in so many units, wherever p0 is
-    b0 = next_launch(c, cu, b0, &t, [&](int64_t T) { return ((T + (int64_t(1) << a.unit) - 2) >> a.unit) + 1; });
+    const int b1 = next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.unit); });
     s = hip_status(launch_append(a, t, c->head_dim, c->dtype, four, rot && rot->interleaved, hipStream_t(stream)));
+    if (s == GLIDE_OK && apart) {
+      next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.shift); });
+      s = hip_status(launch_new_bounds(after, t, c->head_dim, c->dtype, hipStream_t(stream)));
+    }
     if (s != GLIDE_OK) return s;
+    b0 = b1;
   }
   return GLIDE_OK;
 }
