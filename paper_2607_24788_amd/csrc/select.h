@@ -14,6 +14,11 @@ constexpr int64_t kScoreWorkgroups = 4096;
 // fewer share workgroups (attend_rows).  bf16, d = 128: 2048 units of 2048 keys
 // 168 us by waves, 207 by workgroups; 1024 of them 131, 111.
 constexpr int64_t kPickedUnits = 2048;
+// Rows of a sequence share a wave (picked_tiles; bf16, pages of 32 tokens or more)
+// where that leaves so many waves of two rows or more on average.  d = 128, 32 /
+// 8 heads: 1880 rows of 16 of 23 pages of 128 tokens 409 us, 928 by picked_rows;
+// 2048 of 32 of 250 pages of 64 837, 1221; 256 of them (512 waves) 277, 168.
+constexpr int64_t kSharedUnits = 1024;
 // A launch's scores take at most so many bytes (one row's at least).
 constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
 
@@ -41,5 +46,11 @@ hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages,
 // The attention of a launch's units (row, KV head), a wave each; a as for
 // launch_paged_decode with per_head, in one piece.
 hipError_t launch_picked(const PagedArgs& a, int32_t units, int d, int dtype, hipStream_t stream);
+
+// The same (bf16) with `rows` neighbouring rows of a sequence (16 / G, 2 or more) to
+// a wave, over pages of 32 tokens or more; a: the sequences' own table and lens;
+// seqs.tile0 counts waves per KV head.
+hipError_t launch_picked_tiles(const PagedArgs& a, const PagedSeqs& s, const SelectArgs& e, int rows, int d,
+                               hipStream_t stream);
 
 }  // namespace glide

@@ -510,6 +510,244 @@ __global__ __launch_bounds__(256, 2) void picked_rows(PagedArgs a, int32_t units
   }
 }
 
+// ---------------------------------------------------------------------------
+// The same (bf16) for neighbouring rows of a sequence together: a wave takes R = 16 / G
+// rows of one KV head, whose heads fill the MFMA's columns, over the pages that
+// any of them selects, in order; a page that several rows select is read once.
+// The rows' lists are merged on the way: 64 / R lanes hold the next entries of
+// each, a step takes the least head of all.  Pages of 32 tokens or more, so that
+// a tile of 32 keys lies in one.
+//   A value that is not finite would reach every column (0 times infinity): in a
+//   tile that some row does not see in full such values are looked for, and where
+//   there are any the rows take the tile one by one, each with the rows of V that
+//   it sees and the others 0.
+struct Picked {
+  const int32_t* selected;
+  int32_t n_select, row0, row1;  // the launch's rows
+  int32_t R, lanes;              // rows of a wave, log2 of the lanes of each row's list
+  int32_t units;
+};
+template <int D>
+__global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s, Picked w) {
+  typedef bf16_t T;
+  constexpr int KK = D / 32, CT = D / 16, TK = 32, RS = D + 16, LPR = D / 8, RPI = 64 / LPR, NL = TK / RPI;
+  __shared__ __align__(16) T klds[4][TK * RS], vlds[4][TK * RS];
+  const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t unit = int32_t(blockIdx.x) * 4 + wave;
+  if (unit >= w.units) return;
+  const int tile = unit / a.Hkv, g = unit % a.Hkv;
+  int si = 0, hi = s.nseq - 1;
+  while (si < hi) {
+    const int mid = (si + hi + 1) >> 1;
+    if (s.tile0[mid] <= tile) si = mid;
+    else hi = mid - 1;
+  }
+  const int b = s.seq0 + si, ntok = s.len[si];
+  const int32_t begin = s.start[si] > w.row0 ? s.start[si] : w.row0;
+  const int32_t end = s.start[si] + ntok < w.row1 ? s.start[si] + ntok : w.row1;
+  const int32_t r0 = begin + (tile - s.tile0[si]) * w.R;
+  const int rows = end - r0 < w.R ? end - r0 : w.R;
+  int32_t len = a.lens[b];
+  len = __builtin_amdgcn_readfirstlane(len < 0 ? 0 : len > a.cap ? a.cap : len);
+  const int32_t t0 = len - ntok + (r0 - s.start[si]), tmax = t0 + rows - 1;  // positions of the first row and the last
+  const int32_t* trow = a.table + int64_t(b) * a.max_pages;
+  const bool rok = n < rows * a.G;
+  const int rr = rok ? n / a.G : rows - 1;  // this lane's row
+  const int32_t tr = t0 + rr;
+  const int64_t orow = int64_t(r0 - w.row0 + rr) * a.Hq + g * a.G + (rok ? n - rr * a.G : 0);
+  Frag<T> qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    qf[kk].load(reinterpret_cast<const T*>(a.q) + orow * D + 32 * kk + 8 * lg);
+    if (!rok) qf[kk].zero();
+    if (a.scale < 0) qf[kk].negate();  // scores of -q: the frame is a maximum of raw scores
+  }
+  const float c = fabsf(a.scale);
+  float m = kNoMax, l = 0.f;
+  f32x4_t acc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) acc[ct] = zero4();
+  T *kt = klds[wave], *vt = vlds[wave];
+
+  // the rows' lists: lane (row, x) has entry x of the row's current run and of the next
+  const int LW = 1 << w.lanes, lrow = lane >> w.lanes, lx = lane & (LW - 1);
+  const int32_t* list = w.selected + (int64_t(r0 + (lrow < rows ? lrow : 0)) * a.Hkv + g) * w.n_select;
+  auto run = [&](int32_t at) { return lrow < rows && at + lx < w.n_select ? list[at + lx] : -1; };
+  int32_t idx = 0, cur = run(0), nxt = run(LW);
+  constexpr int32_t kNone = 0x7fffffff;
+  struct Tile {
+    int32_t j0, page;  // first position (kNone: no more), page in the pools
+    uint64_t rows;     // at lane (row, 0): whether the row selects the page
+  };
+  auto next_page = [&]() {
+    int32_t h = __shfl(cur, (lane & ~(LW - 1)) + (idx & (LW - 1)));
+    if (h < 0) h = kNone;
+    int32_t least = h;
+    for (int x = LW; x < 64; x *= 2) {
+      const int32_t y = __shfl_xor(least, x);
+      least = y < least ? y : least;
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    Tile t = {kNone, 0, __ballot(h == least)};
+    if (least == kNone) return t;
+    if (h == least) {
+      ++idx;
+      if ((idx & (LW - 1)) == 0) {
+        cur = nxt;
+        nxt = run(idx + LW);
+      }
+    }
+    t.j0 = least << a.shift;
+    t.page = trow[least];
+    return t;
+  };
+  auto next_tile = [&](Tile t) {
+    const int32_t j = t.j0 + TK;
+    if (t.j0 != kNone && (j & ((1 << a.shift) - 1)) != 0 && j <= tmax) {
+      t.j0 = j;
+      return t;
+    }
+    return next_page();
+  };
+  Frag<T> kf[NL], vf[NL];  // whole rows by neighbouring lanes
+  auto fetch = [&](const Tile& t) {
+    const int32_t page = __builtin_amdgcn_readfirstlane(t.page), slot = t.j0 & ((1 << a.shift) - 1);
+    const gptr_t kb = (gptr_t)a.kp + slot_offset(a.ks, Slot{page, slot, true}, g);
+    const gptr_t vb = (gptr_t)a.vp + slot_offset(a.vs, Slot{page, slot, true}, g);
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int row = e * RPI + lane / LPR;
+      const bool there = t.j0 + row <= tmax;  // (rows behind the last query are zeros)
+      gload_frag<false>(kf[e], (there ? kb + int64_t(row) * a.ks[2] : (gptr_t)zero_row) + (lane % LPR) * 16);
+      gload_frag<false>(vf[e], (there ? vb + int64_t(row) * a.vs[2] : (gptr_t)zero_row) + (lane % LPR) * 16);
+    }
+  };
+  // whether the fetched tile has values that are not finite: an exponent of ones carries into the bit above it
+  auto nonfinite = [&]() {
+    uint32_t x = 0;
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const uint4 v = vf[e].v;
+      x |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) |
+           ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
+    }
+    x &= 0x80008000u;
+    return __any(x != 0);
+  };
+  auto order = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  uint64_t every = 0;  // of Tile::rows: all rows
+  for (int x = 0; x < rows; ++x) every |= (LW == 64 ? ~uint64_t(0) : ((uint64_t(1) << LW) - 1) << (x * LW));
+
+  Tile now = next_page();
+  if (now.j0 != kNone) fetch(now);
+  Tile after = next_tile(now);
+  while (now.j0 != kNone) {
+    const int32_t j0 = now.j0;
+    const uint64_t mine = now.rows;
+    // (a tile that all rows see in full needs no mask)
+    const bool full = (mine & every) == every && j0 + TK - 1 <= t0;
+    const bool bad = !full && nonfinite();
+    f32x4_t sc[2] = {zero4(), zero4()};
+#pragma unroll
+    for (int e = 0; e < NL; ++e) {
+      const int at = (e * RPI + lane / LPR) * RS + (lane % LPR) * 8;
+      *reinterpret_cast<uint4*>(kt + at) = kf[e].v;
+      *reinterpret_cast<uint4*>(vt + at) = vf[e].v;
+    }
+    order();
+    now = after;
+    if (now.j0 != kNone) {
+      fetch(now);
+      after = next_tile(now);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        Frag<T> k;
+        k.load(kt + (16 * t + n) * RS + 32 * kk + 8 * lg);
+        sc[t] = mma(k, qf[kk], sc[t]);
+      }
+    if (!full) {
+      const bool sees = rok && ((mine >> (rr << w.lanes)) & 1);
+      const int32_t most = sees ? tr - j0 - 4 * lg : -1;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * t + i > most) sc[t][i] = -INFINITY;
+    }
+    // the frame moves only when a score passes it by 2^8: weights up to that
+    // round alike, and fp32 sums hold them
+    float mx = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[t][i]);
+    mx = lg_max(mx) * c;
+    if (__any(mx > m + 8.f)) {
+      const float m2 = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= f;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[ct][i] *= f;
+    }
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], c, -m));
+      l += p[i];
+    }
+    Frag<T> pf;
+    pf.set8(p);  // bf16: weights rounded to half a step, 2^-8 of each at most
+    if (!bad) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        Frag<T> vc;
+        load_colfrag2(vc, vt, RS, 4 * lg, 16 + 4 * lg, 16 * ct);
+        acc[ct] = mma(vc, pf, acc[ct]);
+      }
+    } else {
+      // from the last row back: each sees no more than the one after it
+#pragma unroll 1
+      for (int x = rows - 1; x >= 0; --x) {
+        if (!((mine >> (x << w.lanes)) & 1)) continue;
+        const int32_t keep = t0 + x - j0 + 1;  // keys of the tile that it sees
+        order();
+#pragma unroll 1
+        for (int key = keep > 0 ? keep : 0; key < TK; ++key)
+          for (int e = lane; e < D; e += 64) vt[key * RS + e] = T(0);
+        order();
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          Frag<T> vc;
+          load_colfrag2(vc, vt, RS, 4 * lg, 16 + 4 * lg, 16 * ct);
+          const f32x4_t y = mma(vc, pf, zero4());
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[ct][i] += rr == x ? y[i] : 0.f;
+        }
+      }
+    }
+    order();
+  }
+  l = lg_sum(l);
+  if (!rok) return;
+  if (lg == 0 && a.lse) a.lse[orow] = (l > 0.f ? m + __builtin_amdgcn_logf(l) : l == 0.f ? -INFINITY : l) * kLn2;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* o = reinterpret_cast<T*>(a.out) + orow * D + 4 * lg;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float y[4] = {acc[ct][0] * inv, acc[ct][1] * inv, acc[ct][2] * inv, acc[ct][3] * inv};
+    *reinterpret_cast<uint2*>(o + 16 * ct) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+  }
+}
+
 template <typename T, int D>
 hipError_t scores_t(const SelectArgs& a, const PagedSeqs& s, int64_t pages, hipStream_t stream) {
   const dim3 grid(uint32_t(s.tile0[s.nseq]) * uint32_t(a.Hkv),
@@ -532,6 +770,17 @@ hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages,
   if (a.max_pages <= 1024) select_pages<256, true><<<units, 256, 0, stream>>>(a, s);
   else if (a.max_pages <= 4096) select_pages<1024, true><<<units, 1024, 0, stream>>>(a, s);
   else select_pages<1024, false><<<units, 1024, 0, stream>>>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_picked_tiles(const PagedArgs& a, const PagedSeqs& s, const SelectArgs& e, int rows, int d,
+                               hipStream_t stream) {
+  int lanes = 6;
+  while ((64 >> lanes) < rows) --lanes;
+  const Picked w = {e.selected, e.n_select, e.row0, e.row1, rows, lanes, s.tile0[s.nseq] * a.Hkv};
+  const uint32_t n = (uint32_t(w.units) + 3) / 4;
+  if (d == 128) picked_tiles<128><<<n, 256, 0, stream>>>(a, s, w);
+  else picked_tiles<64><<<n, 256, 0, stream>>>(a, s, w);
   return hipGetLastError();
 }
 

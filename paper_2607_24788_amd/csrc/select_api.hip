@@ -129,7 +129,23 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
     a.lse = lse ? lse + row0 * cfg->n_q_heads : nullptr;
     a.acc = reinterpret_cast<float*>(ws + w.acc);
     a.ml = reinterpret_cast<float*>(ws + w.ml);
-    if (units >= kPickedUnits) {
+    // rows of a wave that share their pages (see kSharedUnits)
+    const int together = kPagedRows / a.G;
+    PagedSeqs u = t;
+    for (int x = 0; x < t.nseq; ++x) {
+      const int64_t lo = std::max<int64_t>(t.start[x], row0);
+      const int64_t hi = std::min<int64_t>(int64_t(t.start[x]) + t.len[x], row1);
+      u.tile0[x + 1] = u.tile0[x] + int32_t((std::max<int64_t>(hi - lo, 0) + together - 1) / together);
+    }
+    const int64_t waves = int64_t(u.tile0[u.nseq]) * cfg->n_kv_heads;
+    if (cfg->dtype == GLIDE_BF16 && cfg->page_size >= 32 && waves >= kSharedUnits && 2 * waves <= units) {
+      PagedArgs o = a;
+      o.table = e.table;
+      o.lens = e.lens;
+      o.max_pages = e.max_pages;
+      o.cap = e.cap;
+      s = hip_status(launch_picked_tiles(o, u, e, together, cfg->head_dim, hipStream_t(stream)));
+    } else if (units >= kPickedUnits) {
       s = hip_status(launch_picked(a, int32_t(units), cfg->head_dim, cfg->dtype, hipStream_t(stream)));
     } else {
       // Pieces for a round of workgroups, none where every CU has one without: 8

@@ -176,6 +176,61 @@ def test_not_finite(dtype):
     assert not (chosen == 4).any() and not (chosen == 5).any()
 
 
+@pytest.mark.parametrize("Hkv,G,page,select,scale", [
+    (64, 2, 32, 3, 1.0), (32, 1, 64, 2, 1.0), (32, 4, 128, 2, -1.0), (96, 8, 32, 4, 1.0), (64, 5, 32, 9, 1.0)])
+def test_rows_that_share_a_wave(Hkv, G, page, select, scale):
+    """Rows of a sequence together: ragged ends, missing pages, rows that see
+    nothing, lists of different lengths."""
+    new = [150 + 900 // Hkv, 1, 0, 23, 7]
+    lens = [new[0] + 101, 1, 9, 20, 300]
+    R = 16 // G
+    assert Hkv * sum(-(-n // R) for n in new) >= 1024 or G == 1
+    case = Case(5, Hkv * G, Hkv, 64 if Hkv > 32 else 128, page, lens, seed=480, sm_scale=scale * 0.15)
+    if page < 100:
+        case.table[0, 1] = -1
+        case.dev_table.copy_(case.table)
+    run_sparse(case, new, select, 0, 1)
+
+
+@pytest.mark.parametrize("new", [150, 530])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_not_finite_in_shared_pages(new, where):
+    """Keys or values that are not finite in pages that some rows of a wave
+    select and others do not, and at positions that some see and others do not:
+    every row has what the definition gives of what it sees."""
+    Hkv, G, d, page, hist = (64, 2, 64, 32, 100) if new == 150 else (16, 4, 128, 32, 70)
+    assert Hkv * -(-new // (16 // G)) >= 1024
+    case = Case(1, Hkv * G, Hkv, d, page, [hist + new], seed=490 + new)
+    bounds = made_bounds(case)             # of finite keys
+    pool = case.k if where == "k" else case.v
+    for j, e, x in ((5, 3, math.nan), (33, 7, math.inf), (70, 9, -math.inf), (hist + 80, 11, math.nan),
+                    (hist + 81, 12, math.inf), (hist + new - 9, 13, math.nan), (hist + new - 1, 14, math.inf)):
+        pool[int(case.table[0, j // page]), ::3, j % page, e] = x
+    g, select, T = case.g, 3, new
+    q = case.normal(T, Hkv * G, d)
+    kb, ref = bounds.cpu().double(), case.ref()
+    out, lse = nan_like(T, Hkv * G, d, dtype=BF16), nan_like(T, Hkv * G, dtype=FP32)
+    sel = torch.full((T, Hkv, select), 77, dtype=torch.int32, device="cuda")
+    g.sparse(case.cache, bounds, q.cuda(), [0, T], select, sel, out, g.new_sparse_workspace(T, select), n_first=0, lse=lse)
+    got, z = out.cpu().double(), lse.cpu().double()
+    clean = lost = 0
+    for i in list(range(0, T, 13)) + list(range(T - 12, T)) + list(range(76, 92)):
+        t = hist + i
+        pages = pages_of(case, 0, t, q[i], kb, select, 0, 1)
+        for h in (0, 1, 2, 3, Hkv - 1):
+            assert sel[i, h].tolist() == pages[h] + [-1] * (select - len(pages[h]))
+            over = [j for p in pages[h] for j in range(p * page, min(t + 1, (p + 1) * page))]
+            o, zl, tol, ztol = over_tokens(ref, 0, h, over, q[i, h * G:(h + 1) * G])
+            x, y = got[i, h * G:(h + 1) * G], z[i, h * G:(h + 1) * G]
+            fine = o.isfinite()
+            clean, lost = clean + int(fine.all()), lost + int((~fine).sum())
+            assert torch.equal(x.isfinite(), fine), (i, h)
+            assert ((x - o).abs()[fine] <= tol[fine] + 1e-30).all(), (i, h)
+            ok = zl.isfinite()
+            assert torch.equal(y.isfinite(), ok) and ((y - zl).abs()[ok] <= ztol[ok]).all(), (i, h)
+    assert clean > 0 and lost > 0
+
+
 def test_rows_in_several_launches():
     """More rows than the scores of one launch hold: a table of 2^17 pages,
     256 MiB / (8 * 2 * 2^17 * ..) rows to a launch."""

@@ -8,7 +8,8 @@ import pytest
 from .test_registers import kernels
 
 NAMES = ("append_rotated", "page_bounds", "read_rows4", "nibble_rows", "nibble_tiles", "page_scores", "select_pages",
-         "picked_rows", "new_bounds")
+         "picked_rows", "picked_tiles",
+         "new_bounds")
 KERNELS = {n: (m[1], k) for n, k in kernels().items() if (m := re.search(r"\d+(" + "|".join(NAMES) + r")I", n))}
 
 
@@ -17,7 +18,8 @@ def test_every_kernel_is_there():
     for name, _ in KERNELS.values():
         count[name] += 1
     assert count == {"append_rotated": 32, "page_bounds": 4, "read_rows4": 4, "nibble_rows": 10, "nibble_tiles": 8,
-                     "page_scores": 4, "select_pages": 3, "picked_rows": 4, "new_bounds": 4}
+                     "page_scores": 4, "select_pages": 3, "picked_rows": 4, "picked_tiles": 2,
+                     "new_bounds": 4}
 
 
 # fp32, d = 128, 256 rows: a few words outside the loop over tiles
