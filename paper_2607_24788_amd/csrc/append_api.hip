@@ -84,10 +84,10 @@ glide_status append(const glide_paged_config* c, const glide_rotation* rot, cons
   auto units = [](int64_t T, int32_t unit) { return ((T + (int64_t(1) << unit) - 2) >> unit) + 1; };
   for (int b0 = 0; b0 < c->batch;) {
     PagedSeqs t;
-    const int b1 = next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.unit); });
+    const int b1 = next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.unit); }, kMaxLaunchUnits);
     s = hip_status(launch_append(a, t, c->head_dim, c->dtype, four, rot && rot->interleaved, hipStream_t(stream)));
     if (s == GLIDE_OK && apart) {
-      next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.shift); });
+      next_launch(c, cu, b0, &t, [&](int64_t T) { return units(T, a.shift); }, kMaxLaunchUnits);
       s = hip_status(launch_new_bounds(after, t, c->head_dim, c->dtype, hipStream_t(stream)));
     }
     if (s != GLIDE_OK) return s;

@@ -16,6 +16,8 @@ constexpr int32_t kMaxPagedWindow = 1 << 30;
 constexpr int32_t kMaxSinks = 1 << 20;
 constexpr int64_t kMaxUnits = int64_t(1) << 20;       // B * Hkv, a grid dimension
 constexpr int64_t kMaxLaunchRows = int64_t(1) << 27;  // rows of one prefill launch
+// Workgroups of one launch, where a row may be one: a grid has fewer than 2^32 threads.
+constexpr int64_t kMaxLaunchUnits = int64_t(1) << 23;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -215,14 +217,15 @@ void fill(const glide_paged_config* c, const glide_paged_cache* k, PagedArgs* a)
 }
 
 // The sequences of one launch, from b0 on; *units: workgroups per KV head.
-// per(T): those of a sequence of T new tokens.
+// per(T): those of a sequence of T new tokens.  most: rows of several sequences.
 template <typename F>
-int next_launch(const glide_paged_config* c, const int32_t* cu, int b0, PagedSeqs* t, F per) {
+int next_launch(const glide_paged_config* c, const int32_t* cu, int b0, PagedSeqs* t, F per,
+                int64_t most = kMaxLaunchRows) {
   memset(t, 0, sizeof(*t));
   t->seq0 = b0;
   int b1 = b0;
   while (b1 < c->batch && b1 - b0 < kMaxSeqPerLaunch &&
-         (b1 == b0 || int64_t(cu[b1 + 1] - cu[b0]) * c->n_q_heads <= kMaxLaunchRows)) {
+         (b1 == b0 || int64_t(cu[b1 + 1] - cu[b0]) * c->n_q_heads <= most)) {
     const int i = b1 - b0;
     t->start[i] = cu[b1];
     t->len[i] = cu[b1 + 1] - cu[b1];

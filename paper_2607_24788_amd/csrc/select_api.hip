@@ -10,7 +10,7 @@ namespace {
 // Rows of one launch at most: what their scores take in the workspace.
 int64_t launch_rows(const glide_paged_config* c, int64_t rows) {
   const int64_t one = int64_t(c->n_kv_heads) * c->max_pages * 8;
-  return std::min(rows, std::max<int64_t>(1, std::min(kMaxScoreBytes / one, (int64_t(1) << 24) / c->n_kv_heads)));
+  return std::min(rows, std::max<int64_t>(1, std::min(kMaxScoreBytes / one, kMaxLaunchUnits / c->n_kv_heads)));
 }
 
 struct SparseSections {

@@ -85,3 +85,54 @@ def test_bounds_and_sparse():
         got.append([x.clone() for x in (out, lse, sel)] + [x[used].clone() for x in (kp, vp, bounds)])
     for x, y in zip(*got):
         assert torch.equal(x, y) and x.float().isfinite().all()
+
+
+def test_pages_of_one_token_by_the_million():
+    """An append that keeps bounds has a workgroup for every page and KV head:
+    2^24 of them, 2^32 threads, over several launches."""
+    Hkv, T, n_seq = 16, 1 << 18, 4
+    g = paged.Paged(n_seq, Hkv, Hkv, 64, 1, T * n_seq, T, dtype=BF16)
+    kp, vp, _ = g.new_pools()
+    bounds = g.new_bounds()
+    table = torch.arange(T * n_seq, dtype=torch.int32, device="cuda").view(n_seq, T)
+    c = g.cache(kp, vp, table, torch.full((n_seq,), T, dtype=torch.int32, device="cuda"))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k = torch.empty((T * n_seq, Hkv, 64), dtype=BF16, device="cuda").normal_(generator=gen)
+    for x in (kp, vp, bounds):
+        x.fill_(float("nan"))
+    g.append(c, k, k, [T * i for i in range(n_seq + 1)], bounds=bounds)
+    assert torch.equal(kp.view_as(k), k) and torch.equal(vp.view_as(k), k)
+    assert torch.equal(bounds[:, :, 0], k) and torch.equal(bounds[:, :, 1], k)
+
+
+def test_sparse_rows_by_the_million():
+    """2^24 rows of queries and KV heads, of which all but the last see nothing."""
+    Hkv, T, P, lens = 8, 1 << 20, 256, [256, 77]
+    g = paged.Paged(2, Hkv, Hkv, 64, P, 2, 1, dtype=BF16)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    kp, vp, _ = g.new_pools()
+    for x in (kp, vp):
+        x.normal_(generator=gen)
+    c = g.cache(kp, vp, torch.tensor([[1], [0]], dtype=torch.int32, device="cuda"),
+                torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    bounds = g.new_bounds()
+    g.page_bounds(c, bounds)
+    q = torch.empty((2 * T, Hkv, 64), dtype=BF16, device="cuda").normal_(generator=gen)
+    out, lse = torch.full_like(q, float("nan")), torch.full((2 * T, Hkv), float("nan"), device="cuda")
+    sel = torch.full((2 * T, Hkv, 1), 77, dtype=torch.int32, device="cuda")
+    g.sparse(c, bounds, q, [0, T, 2 * T], 1, sel, out, g.new_sparse_workspace(2 * T, 1), n_first=0, lse=lse)
+    for b, n in enumerate(lens):
+        blind, seen = slice(b * T, (b + 1) * T - n), slice((b + 1) * T - n, (b + 1) * T)
+        assert (sel[blind] == -1).all() and (out[blind] == 0).all() and (lse[blind] == float("-inf")).all()
+        assert (sel[seen] == 0).all()
+        # the rows that see something, by a call of their own
+        few = [0, n if b == 0 else 0, n]
+        o, l = torch.empty_like(q[seen]), torch.empty_like(lse[seen])
+        s = torch.empty((n, Hkv, 1), dtype=torch.int32, device="cuda")
+        g.sparse(c, bounds, q[seen].contiguous(), few, 1, s, o, g.new_sparse_workspace(n, 1), n_first=0, lse=l)
+        scores = (q[seen].float().unsqueeze(1) * kp[1 - b, :, :n].float().transpose(0, 1)).sum(-1) / 8
+        scores = scores.masked_fill(torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1).unsqueeze(-1), float("-inf"))
+        want = scores.double().logsumexp(1)
+        # (fp32 sums of 64 products, 80 in all: 64 * 80 * 2^-24 / 8 each; outputs: weights and result, of both calls)
+        assert (lse[seen].double() - want).abs().max() < 1e-4 and (l.double() - want).abs().max() < 1e-4
+        assert out[seen].isfinite().all() and (out[seen].float() - o.float()).abs().max() < 4 * 2 ** -8 * 6
