@@ -18,6 +18,11 @@ constexpr int64_t kPickedUnits = 2048;
 // where that leaves so many waves of two rows or more on average.  d = 128, 32 /
 // 8 heads: 1880 rows of 16 of 23 pages of 128 tokens 409 us, 928 by picked_rows;
 // 2048 of 32 of 250 pages of 64 837, 1221; 256 of them (512 waves) 277, 168.
+// Pages of 16 tokens fill half a tile: there only if a page is selected by enough
+// of a wave's rows, the root of them.  2000 rows of 250 pages, by waves / alone: four
+// rows to a wave, 60 pages each (1.4 rows to a page) 766 / 721 us, 120 (2.1) 1043 /
+// 1143, 180 1206 / 1568; 16 rows (d = 64), 30 (2.2) 475 / 387, 60 (3.9) 563 / 567,
+// 120 604 / 928.
 constexpr int64_t kSharedUnits = 1024;
 // A launch's scores take at most so many bytes (one row's at least).
 constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
@@ -48,7 +53,7 @@ hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages,
 hipError_t launch_picked(const PagedArgs& a, int32_t units, int d, int dtype, hipStream_t stream);
 
 // The same (bf16) with `rows` neighbouring rows of a sequence (16 / G, 2 or more) to
-// a wave, over pages of 32 tokens or more; a: the sequences' own table and lens;
+// a wave, over pages of 16 tokens or more; a: the sequences' own table and lens;
 // seqs.tile0 counts waves per KV head.
 hipError_t launch_picked_tiles(const PagedArgs& a, const PagedSeqs& s, const SelectArgs& e, int rows, int d,
                                hipStream_t stream);

@@ -515,8 +515,8 @@ __global__ __launch_bounds__(256, 2) void picked_rows(PagedArgs a, int32_t units
 // rows of one KV head, whose heads fill the MFMA's columns, over the pages that
 // any of them selects, in order; a page that several rows select is read once.
 // The rows' lists are merged on the way: 64 / R lanes hold the next entries of
-// each, a step takes the least head of all.  Pages of 32 tokens or more, so that
-// a tile of 32 keys lies in one.
+// each, a step takes the least head of all.  A tile of 32 keys lies in one page;
+// of a page of 16 it has the 16.
 //   A value that is not finite would reach every column (0 times infinity): in a
 //   tile that some row does not see in full such values are looked for, and where
 //   there are any the rows take the tile one by one, each with the rows of V that
@@ -611,6 +611,7 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
     return next_page();
   };
   Frag<T> kf[NL], vf[NL];  // whole rows by neighbouring lanes
+  const int32_t keys = a.shift < 5 ? 1 << a.shift : TK;  // of a tile
   auto fetch = [&](const Tile& t) {
     const int32_t page = __builtin_amdgcn_readfirstlane(t.page), slot = t.j0 & ((1 << a.shift) - 1);
     const gptr_t kb = (gptr_t)a.kp + slot_offset(a.ks, Slot{page, slot, true}, g);
@@ -618,7 +619,7 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
 #pragma unroll
     for (int e = 0; e < NL; ++e) {
       const int row = e * RPI + lane / LPR;
-      const bool there = t.j0 + row <= tmax;  // (rows behind the last query are zeros)
+      const bool there = row < keys && t.j0 + row <= tmax;  // (rows behind the last query are zeros)
       gload_frag<false>(kf[e], (there ? kb + int64_t(row) * a.ks[2] : (gptr_t)zero_row) + (lane % LPR) * 16);
       gload_frag<false>(vf[e], (there ? vb + int64_t(row) * a.vs[2] : (gptr_t)zero_row) + (lane % LPR) * 16);
     }
@@ -649,7 +650,7 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
     const int32_t j0 = now.j0;
     const uint64_t mine = now.rows;
     // (a tile that all rows see in full needs no mask)
-    const bool full = (mine & every) == every && j0 + TK - 1 <= t0;
+    const bool full = keys == TK && (mine & every) == every && j0 + TK - 1 <= t0;
     const bool bad = !full && nonfinite();
     f32x4_t sc[2] = {zero4(), zero4()};
 #pragma unroll
@@ -674,7 +675,7 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
       }
     if (!full) {
       const bool sees = rok && ((mine >> (rr << w.lanes)) & 1);
-      const int32_t most = sees ? tr - j0 - 4 * lg : -1;
+      const int32_t most = sees ? (tr - j0 < keys ? tr - j0 : keys - 1) - 4 * lg : -1;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll

@@ -138,7 +138,11 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
       u.tile0[x + 1] = u.tile0[x] + int32_t((std::max<int64_t>(hi - lo, 0) + together - 1) / together);
     }
     const int64_t waves = int64_t(u.tile0[u.nseq]) * cfg->n_kv_heads;
-    if (cfg->dtype == GLIDE_BF16 && cfg->page_size >= 32 && waves >= kSharedUnits && 2 * waves <= units) {
+    // times that a page is selected by a wave's rows, if they choose by chance
+    const double part = std::min(1.0, double(n_select) * cfg->page_size / double(longest));
+    const double share = together * part / (1 - pow(1 - part, together));
+    const bool fits = cfg->page_size >= 32 || (cfg->page_size == 16 && share * share >= together);
+    if (cfg->dtype == GLIDE_BF16 && fits && waves >= kSharedUnits && 2 * waves <= units) {
       PagedArgs o = a;
       o.table = e.table;
       o.lens = e.lens;

@@ -177,7 +177,8 @@ def test_not_finite(dtype):
 
 
 @pytest.mark.parametrize("Hkv,G,page,select,scale", [
-    (64, 2, 32, 3, 1.0), (32, 1, 64, 2, 1.0), (32, 4, 128, 2, -1.0), (96, 8, 32, 4, 1.0), (64, 5, 32, 9, 1.0)])
+    (64, 2, 32, 3, 1.0), (32, 1, 64, 2, 1.0), (32, 4, 128, 2, -1.0), (96, 8, 32, 4, 1.0), (64, 5, 32, 9, 1.0),
+    (64, 2, 16, 14, 1.0), (96, 1, 16, 9, -1.0)])
 def test_rows_that_share_a_wave(Hkv, G, page, select, scale):
     """Rows of a sequence together: ragged ends, missing pages, rows that see
     nothing, lists of different lengths."""
@@ -189,7 +190,7 @@ def test_rows_that_share_a_wave(Hkv, G, page, select, scale):
     if page < 100:
         case.table[0, 1] = -1
         case.dev_table.copy_(case.table)
-    run_sparse(case, new, select, 0, 1)
+    run_sparse(case, new, select, 0, 1, max_len=max(lens))
 
 
 @pytest.mark.parametrize("new", [150, 530])
