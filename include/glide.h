@@ -515,7 +515,9 @@ typedef struct {
   const int32_t* lens;
 } glide_nibble_cache;
 
-/* As glide_paged_append: k (after its rotation) and v are rounded to 4 bits.
+/* As glide_paged_append: k (after its rotation) and v are rounded to 4 bits, k
+ * from its rotation in fp64: a code is that of the exact number, but where that
+ * is within 2^-30 of a tie (positions to 2^20).
  * Pairs that are not interleaved: rot_dim a multiple of 64, else
  * GLIDE_ERR_UNSUPPORTED. */
 glide_status glide_nibble_append(const glide_paged_config* cfg, const glide_nibble_cache* cache,

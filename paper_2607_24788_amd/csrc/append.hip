@@ -39,6 +39,52 @@ __device__ __forceinline__ void store8(char* p, const float* x) {
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   }
 }
+// Sine and cosine of t turns, |t| <= 1/2, in fp64: the nearest quarter off, then
+// their series up to x^15 / 15! and x^16 / 16!, x at most pi / 4 (what follows is
+// 5e-17 of x at most).  The coefficients come from memory: it is called seldom,
+// and they would take registers all along.
+__constant__ const double kSeries[8][2] = {
+    {-1. / 1307674368000, 1. / 20922789888000}, {1. / 6227020800, -1. / 87178291200},
+    {-1. / 39916800, 1. / 479001600},           {1. / 362880, -1. / 3628800},
+    {-1. / 5040, 1. / 40320},                   {1. / 120, -1. / 720},
+    {-1. / 6, 1. / 24},                         {1., -0.5}};
+constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
+__device__ __forceinline__ void sincos_turn(double t, double* sn, double* cs) {
+  const double k = __builtin_rint(4 * t), x = (t - 0.25 * k) * 6.28318530717958647693, z = x * x;
+  double s = 0, c = 0;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    s = fma(s, z, kSeries[i][0]);
+    c = fma(c, z, kSeries[i][1]);
+  }
+  s *= x;
+  c = fma(c, z, 1.);
+  const int q = int(k);
+  const double u = q & 1 ? c : s, v = q & 1 ? s : c;
+  *sn = q & 2 ? -u : u;
+  *cs = (q + 1) & 2 ? -v : v;
+}
+// Element e of a key, rotated in fp64; row: the key, at: its position.
+template <typename T, bool INTER>
+__device__ __forceinline__ double rotated(const T* row, int e, const float* freqs, int rot, double at) {
+  if (e >= rot) return to_f32(row[e]);
+  const int half = rot / 2, p = INTER ? e >> 1 : e < half ? e : e - half;
+  const bool second = INTER ? e & 1 : e >= half;
+  const double u = to_f32(row[INTER ? 2 * p : p]), v = to_f32(row[INTER ? 2 * p + 1 : p + half]);
+  double t = at * (double(freqs[p]) * kTurn), s, c;
+  t -= __builtin_rint(t);
+  sincos_turn(t, &s, &c);
+  return second ? fma(v, c, u * s) : fma(u, c, -(v * s));
+}
+// The next fp32 number from x >= 0 on, for the scale that it takes: scales end at fp32 numbers.
+__device__ __forceinline__ float above(double x) {
+  const float y = float(x);
+  return double(y) < x ? __uint_as_float(__float_as_uint(y) + 1) : y;
+}
+__device__ __forceinline__ float group_max(float m) {  // over four neighbouring threads
+  m = fmaxf(m, dpp_mv<0xb1, 0xf>(m));
+  return fmaxf(m, dpp_mv<0x4e, 0xf>(m));
+}
 template <typename T>
 __device__ __forceinline__ float held(float x) { return to_f32(from_f32<T>(x)); }
 
@@ -133,9 +179,13 @@ __device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32]) {
 //   Angles: position times frequency in fp64, as turns; the nearest whole turn
 //   is taken off there, and what is left (at most half a turn) goes to fp32:
 //   at position 2^20 the angle is off by 2^-25 of a turn, as at position 1.
+//   4 bits: a code is that of the key rotated in 64 bits.  Few elements come so
+//   near to a step's middle that fp32 could miss it; those alone are worked out
+//   in fp64 (8191 tokens 56.6 us with the read back, 54.3 without; all of them in
+//   fp64 78).
 // Bound by HBM in prompts: 8191 tokens of 32 / 8 heads of 128, bf16, with bounds,
 // 202 MB in 46 us (4.4 TB/s; from memory.  Rows are read past the caches: 49 us
-// through them), 36 out of the caches; into 4 bits 177 MB in 45 and 31.  One
+// through them), 36 out of the caches; into 4 bits 177 MB in 48 and 33.  One
 // token of 32 sequences takes 6.1 us, of one fp32 layer 4.6: lens -> table ->
 // bounds, rows and angles.
 // SINGLE: a call of one token per sequence.
@@ -168,12 +218,11 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
     c2 = r1 ? c + half : c1 + (D - a.rot) / 16;
   }
   double f[8];  // turns per position
-  const double turn = 0.15915494309189533577;  // 1 / (2 pi)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int at = INTER ? (i < 4 ? 4 * c1 + i : 4 * c2 + i - 4) : 8 * c1 + i;
     const bool on = INTER ? (i < 4 ? r1 : r2) : r1;
-    f[i] = on ? double(a.freqs[at]) * turn : 0.0;
+    f[i] = on ? double(a.freqs[at]) * kTurn : 0.0;
   }
   const int32_t* trow = a.table + int64_t(b) * a.max_pages;
   Bounds16 bd;
@@ -221,7 +270,19 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
       w2.to_floats(y + 8);
       if (AHEAD && row + RL < nrow) fetch(row + RL);
       if (row < 2 && !sl.ok) continue;
+      float size[2] = {0.f, 0.f};  // 4 bits: of a half's pairs |x| + |y| at most, where they are rotated
       if (row != 1) {
+        if constexpr (FOUR) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float z = INTER ? fabsf(y[2 * i]) + fabsf(y[2 * i + 1]) : fabsf(y[i]) + fabsf(y[8 + i]);
+            const int h = INTER ? i / 4 : 0;
+            size[h] = z > size[h] ? z : size[h];
+          }
+          if (!INTER) size[1] = size[0];
+          if (row != 0 || !r1) size[0] = 0.f;
+          if (row != 0 || !r2) size[1] = 0.f;
+        }
         if constexpr (INTER) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -258,10 +319,51 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
             z = z == z ? z : 0.f;
             m = fmaxf(m, fabsf(z));
           }
-          m = fmaxf(m, dpp_mv<0xb1, 0xf>(m));
-          m = fmaxf(m, dpp_mv<0x4e, 0xf>(m));
+          m = group_max(m);
+          // What fp32 may be off by, at most: 2^-21 of |x| + |y| (angle 3.2, sine and
+          // cosine 2, products and sum 2 half steps), and as much again.  Where that
+          // leaves the scale or a code open, the elements are rotated in fp64: about
+          // one key in 400.
+          const float slack = group_max(size[h]) * 0x1p-20f;
+          auto exact = [&](int i) {
+            const double z = rotated<T, INTER>(reinterpret_cast<const T*>(row_at(0, tok)), 8 * ch + i, a.freqs, a.rot,
+                                               a.pos ? a.pos[tok] : j);
+            return z == z ? z : 0.0;
+          };
+          const bool open = scale_byte(m - slack) != scale_byte(m + slack) && slack > 0.f;
+          if (__any(open)) {
+            double most = 0;
+            if (open) {
+#pragma unroll 1
+              for (int i = 0; i < 8; ++i) most = fmax(most, fabs(exact(i)));
+            }
+            const float x = group_max(above(most));
+            m = open ? x : m;
+          }
           const uint32_t byte = scale_byte(m);
-          *reinterpret_cast<uint32_t*>(codes + ch * 4) = codes8(y + 8 * h, __uint_as_float((254u - byte) << 23));
+          const float inv = __uint_as_float((254u - byte) << 23);
+          float off;
+          uint32_t w = codes8(y + 8 * h, inv, &off);
+          const float near = 0.5f - 2.f * slack * inv;  // (steps of 1/2 at least)
+          if (__any(slack > 0.f && !(off < near))) {
+            uint32_t left = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              code_of(fabsf(y[8 * h + i]) * inv, &off);
+              left |= off < near ? 0u : 1u << i;
+            }
+            if (!(slack > 0.f)) left = 0;
+#pragma unroll 1
+            while (left) {
+              const int i = __builtin_ctz(left);
+              left &= left - 1;
+              const double z = exact(i);
+              double rest;
+              const uint32_t code = code_of(fabs(z) * double(inv), &rest) | (z < 0 ? 8u : 0u);
+              w = (w & ~(15u << (4 * i))) | code << (4 * i);
+            }
+          }
+          *reinterpret_cast<uint32_t*>(codes + ch * 4) = w;
           if ((c & 3) == 0) scales[ch / 4] = uint8_t(byte);
         }
       } else {
@@ -277,6 +379,7 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
         }
       }
     }
+    if (SINGLE) break;
   }
   if constexpr (!FOUR) {
     if (a.bounds) {

@@ -45,18 +45,28 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
   const uint32_t b = byte < uint32_t(kMinScale) ? kMinScale : byte > uint32_t(kMaxScale) ? kMaxScale : byte;
   return __uint_as_float(b << 23);
 }
-// Eight values of one group to eight codes, element i in bits 4 i .. 4 i + 3;
-// ties to the even code.  inv = 2^-e.
-__device__ __forceinline__ uint32_t codes8(const float* x, float inv) {
+// The code of a magnitude a = |x| 2^-e, ties to the even one; *off: how far a is
+// from it in its steps (1/2: a tie).  F: float or double.
+template <typename F>
+__device__ __forceinline__ uint32_t code_of(F a, F* off) {
+  a = a < F(6) ? a : F(6);
+  const uint32_t e = a < F(2) ? 0u : a < F(4) ? 1u : 2u;  // steps of 1/2, 1 and 2
+  const F t = a * (e == 0 ? F(2) : e == 1 ? F(1) : F(0.5)), r = __builtin_elementwise_roundeven(t);
+  *off = t < r ? r - t : t - r;
+  return uint32_t(int(r)) + 2 * e;
+}
+// Eight values of one group to eight codes, element i in bits 4 i .. 4 i + 3.
+// inv = 2^-e; *off: the largest.
+__device__ __forceinline__ uint32_t codes8(const float* x, float inv, float* off) {
   uint32_t w = 0;
+  float far = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float a = fminf(fabsf(x[i]) * inv, 6.f);
-    const uint32_t e = a < 2.f ? 0u : a < 4.f ? 1u : 2u;  // steps of 1/2, 1 and 2
-    const float r = __builtin_rintf(a * (e == 0 ? 2.f : e == 1 ? 1.f : 0.5f));
-    const uint32_t c = uint32_t(int(r)) + 2 * e;
-    w |= (c | (x[i] < 0.f ? 8u : 0u)) << (4 * i);
+    float o;
+    w |= (code_of(fabsf(x[i]) * inv, &o) | (x[i] < 0.f ? 8u : 0u)) << (4 * i);
+    far = fmaxf(far, o);
   }
+  *off = far;
   return w;
 }
 // Eight codes to eight bf16 values times 2^e (exact), in order.

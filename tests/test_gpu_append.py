@@ -297,6 +297,25 @@ def test_rounding_to_four_bits(dtype):
             assert values(c, e).isfinite().all()
 
 
+@pytest.mark.parametrize("dtype,interleaved,far", [(BF16, False, 0), (BF16, True, 0), (FP32, False, 900000)])
+def test_codes_of_the_rotated_key(dtype, interleaved, far):
+    """Each code is that of the key rotated in 64 bits, also where an fp32
+    product would be on the other side of a step's middle: 2^22 elements, of
+    which a rounding of 2^-24 would move several.  (Both sides' 64-bit errors,
+    2^-30 of a number at these positions, would move one in about 1000 runs.)"""
+    T, Hkv, d = 4096, 8, 128
+    case = Case4(1, Hkv, Hkv, d, 64, [T], dtype=dtype, seed=30)
+    gen = torch.Generator().manual_seed(31)
+    k = torch.randn((T, Hkv, d), generator=gen).to(dtype)
+    f = frequencies(d)
+    pos = torch.arange(T, dtype=torch.int32) + far
+    case.g.append(case.cache, k.cuda(), k.cuda(), [0, T], freqs=f.cuda(), interleaved=interleaved, positions=pos.cuda())
+    codes, scales = quantise(rotate(k, pos, f, interleaved, dtype)[0])
+    page, at = case.table[0, torch.arange(T) // 64].long(), torch.arange(T) % 64
+    assert torch.equal(case.k[1].cpu()[page, :, at], scales)
+    assert torch.equal(case.k[0].cpu()[page, :, at], codes)
+
+
 def test_scales_out_of_range_read():
     """Bytes that no call writes count as the nearest that one does."""
     case = Case4(1, 2, 1, 64, 16, [20], seed=23)
