@@ -540,7 +540,7 @@ size_t glide_nibble_workspace_bytes(const glide_paged_config* cfg, int64_t max_t
  * lens[b] - T_b + i.  Their tokens are in the cache (glide_nibble_append).
  * What a query sees, the order of q, out and lse, max_len and errors as for
  * glide_paged_prefill.  Rows in GLIDE_F32 are exact to fp32 (queries and
- * weights are split, not rounded). */
+ * weights are split, not rounded; their bits below 2^-133 do not count). */
 glide_status glide_nibble_prefill(const glide_paged_config* cfg, const glide_nibble_cache* cache, const void* q,
                                   const int32_t* cu_seqlens_host, int64_t total_tokens, int64_t max_len, void* out,
                                   float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -31,32 +31,42 @@ __device__ __forceinline__ int32_t seq_len(const PagedArgs& a, int b) {
 
 // Eight numbers as bf16 operands: one rounded (bf16 calls: half a step, 2^-8 of
 // each at most), or three parts that sum to each exactly (fp32 calls: what is
-// left after 24 bits is 0).
+// left after 24 bits is 0; bits below 2^-133 have no place).
 template <typename T>
 struct Parts {
   static constexpr int N = sizeof(T) == 2 ? 1 : 3;
   Frag<bf16_t> f[N];
   __device__ __forceinline__ void set8(const float* x) {
-    f[0].set8(x);
-    if constexpr (N == 3) {
-      float y[8], z[8];
-      f[0].to_floats(y);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = x[i] - y[i];
-      f[1].set8(y);
-      f[1].to_floats(z);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = y[i] - z[i];
-      f[2].set8(z);
-    }
+    split8(x, [](Frag<bf16_t>& part, const float* y) { part.set8(y); });
   }
+  // The largest fp32 numbers would round to infinity: a query's parts are cut off.
   __device__ __forceinline__ void load(const T* p) {
     Frag<T> x;
     x.load(p);
     if constexpr (N == 1) {
       f[0] = x;
     } else {
-      set8(x.v);
+      split8(x.v, [](Frag<bf16_t>& part, const float* y) {
+        auto upper = [](float a, float b) {  // their upper halves, a's in the lower
+          return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+        };
+        part.v = make_uint4(upper(y[0], y[1]), upper(y[2], y[3]), upper(y[4], y[5]), upper(y[6], y[7]));
+      });
+    }
+  }
+  template <typename F>  // part(f, y): y to the operand f
+  __device__ __forceinline__ void split8(const float* x, F part) {
+    part(f[0], x);
+    if constexpr (N == 3) {
+      float y[8], z[8];
+      f[0].to_floats(y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = x[i] - y[i];
+      part(f[1], y);
+      f[1].to_floats(z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = y[i] - z[i];
+      part(f[2], z);
     }
   }
   __device__ __forceinline__ void zero() {
