@@ -444,7 +444,10 @@ typedef struct {
  *             least and the largest of its keys by element, as the cache holds
  *             them (NaN left out), brought up to date with the new keys.  Where
  *             a page has earlier tokens, their bounds are there already (of
- *             earlier appends, or of glide_paged_bounds)
+ *             earlier appends, or of glide_paged_bounds), and are only ever
+ *             widened: after tokens were taken back (lens moved back into a
+ *             page, as for drafts that were rejected) a page's bounds span their
+ *             keys too until glide_paged_bounds makes them anew
  * Device pointers 16-byte aligned (positions: 4). */
 glide_status glide_paged_append(const glide_paged_config* cfg, const glide_paged_cache* cache,
                                 const glide_rotation* rotation, const void* q, const void* k, const void* v,
@@ -452,8 +455,9 @@ glide_status glide_paged_append(const glide_paged_config* cfg, const glide_paged
                                 void* stream);
 
 /* The bounds of every page of the sequences from the keys in the cache: where
- * rows were written otherwise, and after an eviction.  max_len: the caller's
- * upper bound of lens (0: the table's capacity); a wrong one costs time only. */
+ * rows were written otherwise, after an eviction, and after tokens were taken
+ * back.  max_len: the caller's upper bound of lens (0: the table's capacity); a
+ * wrong one costs time only. */
 glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged_cache* cache, int64_t max_len,
                                 void* bounds, void* stream);
 

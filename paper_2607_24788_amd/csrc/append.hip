@@ -398,14 +398,19 @@ __global__ __launch_bounds__(256) void append_rotated(AppendArgs a, PagedSeqs s)
   }
 }
 
-// The bounds of a page of n tokens from its keys in the cache, by a workgroup.
+// The bounds of a page's tokens from slot `first` to n - 1, from their keys in
+// the cache, by a workgroup; those there already count for the slots before.
 template <typename T, int D>
-__device__ __forceinline__ void bounds_of_page(const AppendArgs& a, int32_t page, int g, int32_t n, float (*red)[32]) {
+__device__ __forceinline__ void bounds_of_page(const AppendArgs& a, int32_t page, int g, int32_t first, int32_t n,
+                                               float (*red)[32]) {
   constexpr int C = D / 16, ES = int(sizeof(T)), LANES = 256 / C;
   const int c = threadIdx.x % C;
+  char* row = a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES);
+  OldBounds<T> old;
+  if (int(threadIdx.x) < C && first > 0) old.load(row, D, c, c + C);
   Bounds16 bd;
   bd.clear();
-  for (int32_t t = threadIdx.x / C; t < n; t += LANES) {
+  for (int32_t t = first + int32_t(threadIdx.x) / C; t < n; t += LANES) {
     const char* src = a.kp + slot_offset(a.ks, Slot{page, t, true}, g);
     float y[16];
     load8<T>(y, src + c * 8 * ES);
@@ -414,8 +419,7 @@ __device__ __forceinline__ void bounds_of_page(const AppendArgs& a, int32_t page
     for (int e = 0; e < 16; ++e) bd.add(e, y[e]);
   }
   join_bounds<C>(bd, red);
-  if (int(threadIdx.x) < C)
-    store_bounds<T, D>(bd, OldBounds<T>(), a.bounds + (int64_t(page) * a.Hkv + g) * (2 * D * ES), c, c + C, false);
+  if (int(threadIdx.x) < C) store_bounds<T, D>(bd, old, row, c, c + C, first > 0);
 }
 // Of every page of the sequences.
 template <typename T, int D>
@@ -427,11 +431,13 @@ __global__ __launch_bounds__(256) void page_bounds(AppendArgs a) {
     const int32_t page = a.table[int64_t(b) * a.max_pages + i];
     if (uint32_t(page) >= uint32_t(a.n_pages)) continue;
     const int32_t left = len - (i << a.shift);
-    bounds_of_page<T, D>(a, page, g, left < (1 << a.shift) ? left : 1 << a.shift, red);
+    bounds_of_page<T, D>(a, page, g, 0, left < (1 << a.shift) ? left : 1 << a.shift, red);
     __syncthreads();
   }
 }
-// Of the pages that an append wrote to (a workgroup per page and KV head).
+// Of the pages that an append wrote to (a workgroup per page and KV head): the
+// new keys joined to what is there, as append_rotated does it, so that which of
+// the two keeps the bounds shows in none of them.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void new_bounds(AppendArgs a, PagedSeqs s) {
   __shared__ float red[4 * (D / 16)][32];
@@ -442,8 +448,8 @@ __global__ __launch_bounds__(256) void new_bounds(AppendArgs a, PagedSeqs s) {
   if ((int64_t(i) << a.shift) >= len) return;
   const int32_t page = a.table[int64_t(b) * a.max_pages + i];
   if (uint32_t(page) >= uint32_t(a.n_pages)) return;
-  const int32_t left = len - (i << a.shift);
-  bounds_of_page<T, D>(a, page, g, left < (1 << a.shift) ? left : 1 << a.shift, red);
+  const int32_t u0 = i << a.shift, left = len - u0;
+  bounds_of_page<T, D>(a, page, g, p0 > u0 ? p0 - u0 : 0, left < (1 << a.shift) ? left : 1 << a.shift, red);
 }
 
 // The last tokens of every sequence as rows of the call's type: a thread has

@@ -268,8 +268,9 @@ class Paged:
 
     def page_bounds(self, cache, bounds, max_len=0, stream=None):
         """The bounds of every page of the sequences from the keys in the
-        cache: where they were written without ``append``, and after an
-        eviction."""
+        cache: where they were written without ``append``, after an eviction,
+        and after tokens were taken back (``append`` only ever widens a page's
+        bounds)."""
         bp = self._bounds_of(cache, bounds)
         self._call("glide_paged_bounds", cache, stream, _fits("max_len", int(max_len), 64), bp)
 
