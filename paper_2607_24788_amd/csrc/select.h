@@ -48,6 +48,16 @@ struct SelectArgs {
 // only)
 hipError_t launch_select(const SelectArgs& a, const PagedSeqs& s, int64_t pages, int d, int dtype, hipStream_t stream);
 
+// Tiles of picked_tiles: first positions, kNoTile behind the last.
+constexpr int32_t kTileSlots = 32, kNoTile = 0x7fffffff;
+// The tile behind the one at j0 in the same page, among positions up to tmax;
+// kNoTile where there is none.
+constexpr int32_t next_in_page(int32_t j0, int32_t shift, int32_t tmax) {
+  if (j0 == kNoTile) return kNoTile;  // (before j0 is added to)
+  const int32_t j = j0 + kTileSlots;
+  return (j & ((1 << shift) - 1)) != 0 && j <= tmax ? j : kNoTile;
+}
+
 // The attention of a launch's units (row, KV head), a wave each; a as for
 // launch_paged_decode with per_head, in one piece.
 hipError_t launch_picked(const PagedArgs& a, int32_t units, int d, int dtype, hipStream_t stream);

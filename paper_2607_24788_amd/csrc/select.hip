@@ -530,7 +530,7 @@ struct Picked {
 template <int D>
 __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s, Picked w) {
   typedef bf16_t T;
-  constexpr int KK = D / 32, CT = D / 16, TK = 32, RS = D + 16, LPR = D / 8, RPI = 64 / LPR, NL = TK / RPI;
+  constexpr int KK = D / 32, CT = D / 16, TK = kTileSlots, RS = D + 16, LPR = D / 8, RPI = 64 / LPR, NL = TK / RPI;
   __shared__ __align__(16) T klds[4][TK * RS], vlds[4][TK * RS];
   const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -575,22 +575,21 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
   const int32_t* list = w.selected + (int64_t(r0 + (lrow < rows ? lrow : 0)) * a.Hkv + g) * w.n_select;
   auto run = [&](int32_t at) { return lrow < rows && at + lx < w.n_select ? list[at + lx] : -1; };
   int32_t idx = 0, cur = run(0), nxt = run(LW);
-  constexpr int32_t kNone = 0x7fffffff;
   struct Tile {
-    int32_t j0, page;  // first position (kNone: no more), page in the pools
+    int32_t j0, page;  // first position, page in the pools
     uint64_t rows;     // at lane (row, 0): whether the row selects the page
   };
   auto next_page = [&]() {
     int32_t h = __shfl(cur, (lane & ~(LW - 1)) + (idx & (LW - 1)));
-    if (h < 0) h = kNone;
+    if (h < 0) h = kNoTile;
     int32_t least = h;
     for (int x = LW; x < 64; x *= 2) {
       const int32_t y = __shfl_xor(least, x);
       least = y < least ? y : least;
     }
     least = __builtin_amdgcn_readfirstlane(least);
-    Tile t = {kNone, 0, __ballot(h == least)};
-    if (least == kNone) return t;
+    Tile t = {kNoTile, 0, __ballot(h == least)};
+    if (least == kNoTile) return t;
     if (h == least) {
       ++idx;
       if ((idx & (LW - 1)) == 0) {
@@ -603,12 +602,8 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
     return t;
   };
   auto next_tile = [&](Tile t) {
-    const int32_t j = t.j0 + TK;
-    if (t.j0 != kNone && (j & ((1 << a.shift) - 1)) != 0 && j <= tmax) {
-      t.j0 = j;
-      return t;
-    }
-    return next_page();
+    t.j0 = next_in_page(t.j0, a.shift, tmax);
+    return t.j0 != kNoTile ? t : next_page();
   };
   Frag<T> kf[NL], vf[NL];  // whole rows by neighbouring lanes
   const int32_t keys = a.shift < 5 ? 1 << a.shift : TK;  // of a tile
@@ -644,9 +639,9 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
   for (int x = 0; x < rows; ++x) every |= (LW == 64 ? ~uint64_t(0) : ((uint64_t(1) << LW) - 1) << (x * LW));
 
   Tile now = next_page();
-  if (now.j0 != kNone) fetch(now);
+  if (now.j0 != kNoTile) fetch(now);
   Tile after = next_tile(now);
-  while (now.j0 != kNone) {
+  while (now.j0 != kNoTile) {
     const int32_t j0 = now.j0;
     const uint64_t mine = now.rows;
     // (a tile that all rows see in full needs no mask)
@@ -661,7 +656,7 @@ __global__ __launch_bounds__(256, 2) void picked_tiles(PagedArgs a, PagedSeqs s,
     }
     order();
     now = after;
-    if (now.j0 != kNone) {
+    if (now.j0 != kNoTile) {
       fetch(now);
       after = next_tile(now);
     }
