@@ -15,9 +15,12 @@ constexpr int64_t kScoreWorkgroups = 4096;
 // 168 us by waves, 207 by workgroups; 1024 of them 131, 111.
 constexpr int64_t kPickedUnits = 2048;
 // Rows of a sequence share a wave (picked_tiles; bf16, pages of 32 tokens or more)
-// where that leaves so many waves of two rows or more on average.  d = 128, 32 /
+// where that leaves so many waves, of 1.6 rows or more on average.  d = 128, 32 /
 // 8 heads: 1880 rows of 16 of 23 pages of 128 tokens 409 us, 928 by picked_rows;
 // 2048 of 32 of 250 pages of 64 837, 1221; 256 of them (512 waves) 277, 168.
+// 64 / 8 heads, two rows to a wave: 1881 rows of 12 of 39 pages of 128 493, 722,
+// of 40 of 559 of 32 945, 1043; 60 sequences of 5 rows (1.67 to a wave) 223, 289
+// and 292, 324; 200 of one or two (1.5) 318, 322 and 358, 327.
 // Pages of 16 tokens fill half a tile: there only if a page is selected by enough
 // of a wave's rows, the root of them.  2000 rows of 250 pages, by waves / alone: four
 // rows to a wave, 60 pages each (1.4 rows to a page) 766 / 721 us, 120 (2.1) 1043 /
@@ -26,6 +29,15 @@ constexpr int64_t kPickedUnits = 2048;
 constexpr int64_t kSharedUnits = 1024;
 // A launch's scores take at most so many bytes (one row's at least).
 constexpr int64_t kMaxScoreBytes = int64_t(1) << 28;
+
+// Who attends to a launch's rows: the four waves of a workgroup to a unit in
+// pieces (attend_rows), a wave to a unit (picked_rows), a wave to several rows
+// (picked_tiles).
+enum class SparseForm : int32_t { workgroups, waves, tiles };
+// Which, of the first launch of a valid call of one row or more; not a part of
+// the library's interface (for its tests).
+extern "C" int32_t glide_internal_sparse_form(const glide_paged_config* cfg, const int32_t* cu_seqlens_host,
+                                              int32_t n_select, int64_t max_len);
 
 struct SelectArgs {
   const char* q;         // [T][Hq][d]

@@ -33,6 +33,49 @@ bool select_fits(const glide_paged_config* c, int32_t n_select) {
   return n_select >= 1 && int64_t(n_select) * c->page_size <= kMaxPagedWindow;
 }
 
+int64_t longest_seq(const glide_paged_config* c, int64_t max_len) {
+  return max_len ? std::min<int64_t>(max_len, capacity(c)) : capacity(c);
+}
+
+// The sequences of the launch that starts at row0, R rows at most, whose first
+// is *b0 or a later one; returns the row behind its last.
+int64_t launch_seqs(const glide_paged_config* c, const int32_t* cu, int64_t row0, int64_t R, int64_t* b0,
+                    PagedSeqs* t) {
+  memset(t, 0, sizeof(*t));
+  while (cu[*b0 + 1] <= row0) ++*b0;  // the sequence of the first row
+  t->seq0 = int32_t(*b0);
+  int64_t row1 = row0;
+  int i = 0;
+  for (int64_t b = *b0; b < c->batch && i < kMaxSeqPerLaunch && row1 < row0 + R; ++b, ++i) {
+    row1 = std::min<int64_t>(cu[b + 1], row0 + R);
+    t->start[i] = cu[b];
+    t->len[i] = cu[b + 1] - cu[b];
+    t->tile0[i + 1] = t->tile0[i] + int32_t((row1 - std::max<int64_t>(cu[b], row0) + kScoreRows - 1) / kScoreRows);
+  }
+  t->nseq = i;
+  return row1;
+}
+
+// How the rows row0 .. row1 - 1 of a launch are attended to (see kPickedUnits,
+// kSharedUnits); u: tile0 counts picked_tiles' waves per KV head.
+SparseForm sparse_form(const glide_paged_config* c, const PagedSeqs& t, int64_t row0, int64_t row1, int32_t n_select,
+                       int64_t longest, PagedSeqs* u) {
+  const int together = kPagedRows / (c->n_q_heads / c->n_kv_heads);  // rows of a wave
+  *u = t;
+  for (int x = 0; x < t.nseq; ++x) {
+    const int64_t lo = std::max<int64_t>(t.start[x], row0);
+    const int64_t hi = std::min<int64_t>(int64_t(t.start[x]) + t.len[x], row1);
+    u->tile0[x + 1] = u->tile0[x] + int32_t((std::max<int64_t>(hi - lo, 0) + together - 1) / together);
+  }
+  const int64_t units = (row1 - row0) * c->n_kv_heads, waves = int64_t(u->tile0[u->nseq]) * c->n_kv_heads;
+  // times that a page is selected by a wave's rows, if they choose by chance
+  const double part = std::min(1.0, double(n_select) * c->page_size / double(longest));
+  const double share = together * part / (1 - pow(1 - part, together));
+  const bool fits = c->page_size >= 32 || (c->page_size == 16 && share * share >= together);
+  if (c->dtype == GLIDE_BF16 && fits && waves >= kSharedUnits && 5 * units >= 8 * waves) return SparseForm::tiles;
+  return units >= kPickedUnits ? SparseForm::waves : SparseForm::workgroups;
+}
+
 }  // namespace
 
 extern "C" {
@@ -97,22 +140,11 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
   a.cap = n_select << a.shift;
   a.W = kMaxPagedWindow;
   a.ns = 0;
-  const int64_t longest = max_len ? std::min<int64_t>(max_len, e.cap) : e.cap;
+  const int64_t longest = longest_seq(cfg, max_len);
   const int64_t keys = std::min<int64_t>(a.cap, longest), R = launch_rows(cfg, total_tokens);
   for (int64_t row0 = 0, b0 = 0; row0 < total_tokens;) {
-    PagedSeqs t;
-    memset(&t, 0, sizeof(t));
-    while (cu[b0 + 1] <= row0) ++b0;  // the sequence of the first row
-    t.seq0 = int32_t(b0);
-    int64_t row1 = row0;
-    int i = 0;
-    for (int64_t b = b0; b < cfg->batch && i < kMaxSeqPerLaunch && row1 < row0 + R; ++b, ++i) {
-      row1 = std::min<int64_t>(cu[b + 1], row0 + R);
-      t.start[i] = cu[b];
-      t.len[i] = cu[b + 1] - cu[b];
-      t.tile0[i + 1] = t.tile0[i] + int32_t((row1 - std::max<int64_t>(cu[b], row0) + kScoreRows - 1) / kScoreRows);
-    }
-    t.nseq = i;
+    PagedSeqs t, u;
+    const int64_t row1 = launch_seqs(cfg, cu, row0, R, &b0, &t);
     e.row0 = int32_t(row0);
     e.row1 = int32_t(row1);
     e.single = t.nseq == row1 - row0 && t.tile0[t.nseq] == t.nseq;
@@ -129,27 +161,15 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
     a.lse = lse ? lse + row0 * cfg->n_q_heads : nullptr;
     a.acc = reinterpret_cast<float*>(ws + w.acc);
     a.ml = reinterpret_cast<float*>(ws + w.ml);
-    // rows of a wave that share their pages (see kSharedUnits)
-    const int together = kPagedRows / a.G;
-    PagedSeqs u = t;
-    for (int x = 0; x < t.nseq; ++x) {
-      const int64_t lo = std::max<int64_t>(t.start[x], row0);
-      const int64_t hi = std::min<int64_t>(int64_t(t.start[x]) + t.len[x], row1);
-      u.tile0[x + 1] = u.tile0[x] + int32_t((std::max<int64_t>(hi - lo, 0) + together - 1) / together);
-    }
-    const int64_t waves = int64_t(u.tile0[u.nseq]) * cfg->n_kv_heads;
-    // times that a page is selected by a wave's rows, if they choose by chance
-    const double part = std::min(1.0, double(n_select) * cfg->page_size / double(longest));
-    const double share = together * part / (1 - pow(1 - part, together));
-    const bool fits = cfg->page_size >= 32 || (cfg->page_size == 16 && share * share >= together);
-    if (cfg->dtype == GLIDE_BF16 && fits && waves >= kSharedUnits && 2 * waves <= units) {
+    const SparseForm form = sparse_form(cfg, t, row0, row1, n_select, longest, &u);
+    if (form == SparseForm::tiles) {
       PagedArgs o = a;
       o.table = e.table;
       o.lens = e.lens;
       o.max_pages = e.max_pages;
       o.cap = e.cap;
-      s = hip_status(launch_picked_tiles(o, u, e, together, cfg->head_dim, hipStream_t(stream)));
-    } else if (units >= kPickedUnits) {
+      s = hip_status(launch_picked_tiles(o, u, e, kPagedRows / a.G, cfg->head_dim, hipStream_t(stream)));
+    } else if (form == SparseForm::waves) {
       s = hip_status(launch_picked(a, int32_t(units), cfg->head_dim, cfg->dtype, hipStream_t(stream)));
     } else {
       // Pieces for a round of workgroups, none where every CU has one without: 8
@@ -164,6 +184,14 @@ glide_status glide_paged_sparse(const glide_paged_config* cfg, const glide_paged
     row0 = row1;
   }
   return GLIDE_OK;
+}
+
+int32_t glide_internal_sparse_form(const glide_paged_config* cfg, const int32_t* cu, int32_t n_select,
+                                   int64_t max_len) {
+  PagedSeqs t, u;
+  int64_t b0 = 0;
+  const int64_t row1 = launch_seqs(cfg, cu, 0, launch_rows(cfg, cu[cfg->batch]), &b0, &t);
+  return int32_t(sparse_form(cfg, t, 0, row1, n_select, longest_seq(cfg, max_len), &u));
 }
 
 }  // extern "C"

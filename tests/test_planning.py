@@ -1,10 +1,14 @@
-"""Host arithmetic of the kernels' planning, evaluated by the compiler: a sum
-that overflows is no constant, and an assertion on it does not compile."""
+"""Which kernel a call is planned for, and host arithmetic of the kernels
+evaluated by the compiler (a sum that overflows is no constant, and an assertion
+on it does not compile)."""
+import ctypes
+import itertools
 import subprocess
 
 import pytest
+import torch
 
-from paper_2607_24788_amd import build
+from paper_2607_24788_amd import build, paged
 
 
 def compiles(tmp_path, text):
@@ -24,3 +28,37 @@ def test_tiles_of_a_page(tmp_path, j0, shift, tmax, want):
     a, b = (("glide::kNoTile" if x is None else str(x)) for x in (j0, want))
     ok, err = compiles(tmp_path, f'#include "select.h"\nstatic_assert(glide::next_in_page({a}, {shift}, {tmax}) == {b}, "");\n')
     assert ok, err
+
+
+BF16, FP32 = torch.bfloat16, torch.float32
+WORKGROUPS, WAVES, TILES = range(3)
+
+
+def sparse_form(g, new, n_select, max_len=0):
+    """How a call of the layer g over `new` rows per sequence attends to them."""
+    cu = (ctypes.c_int32 * (len(new) + 1))(0, *itertools.accumulate(new))
+    f = g.lib.glide_internal_sparse_form
+    f.restype, f.argtypes = ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64]
+    return f(ctypes.addressof(g.cfg), ctypes.addressof(cu), n_select, max_len)
+
+
+@pytest.mark.parametrize("G,page", [(8, 128), (7, 64), (6, 32), (4, 64), (3, 32), (1, 64)])
+def test_rows_share_waves_whatever_their_parity(G, page):
+    """One row more or less than a multiple of a wave's, of one sequence or of
+    many, does not send the call to a kernel that reads every page per row."""
+    for new in ([2048], [2047], [2049], [120] * 20, [121] * 20, [119, 120, 121] * 7, [5] * 500):
+        g = paged.Paged(len(new), 8 * G, 8, 128, page, 1000, 200, dtype=BF16)
+        assert sparse_form(g, new, 12, 9000) == TILES, new
+
+
+def test_who_attends_to_the_rows():
+    def form(new, G=4, page=64, n_select=20, dtype=BF16, Hkv=8, max_len=8000):
+        g = paged.Paged(len(new), Hkv * G, Hkv, 128, page, 1000, 500, dtype=dtype)
+        return sparse_form(g, new, n_select, max_len)
+    assert form([1]) == form([255]) == form([1] * 32) == form([300], Hkv=4) == WORKGROUPS
+    assert form([256]) == form([1] * 128, Hkv=16) == WAVES   # few waves; nothing to share
+    assert form([2048], dtype=FP32) == form([2048], page=8) == form([2048], G=16) == form([2048], G=9) == WAVES
+    assert form([1, 2, 1] * 42, Hkv=16) == WAVES             # 1.33 rows to a wave
+    assert form([5] * 60, G=8) == form([1, 3] * 64) == TILES  # 1.67, 2
+    assert form([2048], page=16, n_select=20) == WAVES       # pages that fill half a tile: by how many rows select one
+    assert form([2048], page=16, n_select=400) == TILES
