@@ -678,11 +678,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : Parts<T>::N == 1 ? 2 :
 template <typename T, int D>
 hipError_t decode_t(const PagedArgs& a, const Pools4& p, int tile_keys, hipStream_t stream) {
   const dim3 grid(a.B * a.Hkv, a.npiece);
-  if constexpr (sizeof(T) == 2) {
-    if (tile_keys == 32) nibble_rows<T, D, NoSeqs, 32><<<grid, 256, 0, stream>>>(a, p, NoSeqs());
+  if (tile_keys == 64) {
+    nibble_rows<T, D, NoSeqs, 64><<<grid, 256, 0, stream>>>(a, p, NoSeqs());
+    return hipGetLastError();
   }
-  if (tile_keys == 64) nibble_rows<T, D, NoSeqs, 64><<<grid, 256, 0, stream>>>(a, p, NoSeqs());
-  return hipGetLastError();
+  if constexpr (sizeof(T) == 2) {
+    if (tile_keys == 32) {
+      nibble_rows<T, D, NoSeqs, 32><<<grid, 256, 0, stream>>>(a, p, NoSeqs());
+      return hipGetLastError();
+    }
+  }
+  return hipErrorInvalidValue;  // no such kernel
 }
 template <typename T, int D>
 hipError_t prefill_t(const PagedArgs& a, const Pools4& p, const PagedSeqs& s, int tile_rows, hipStream_t stream) {
@@ -690,6 +696,7 @@ hipError_t prefill_t(const PagedArgs& a, const Pools4& p, const PagedSeqs& s, in
   if (tile_rows == kRows4Big) nibble_tiles<T, D, 8><<<grid, 512, 0, stream>>>(a, p, s);
   else if (tile_rows == kRows4) nibble_tiles<T, D, 4><<<grid, 256, 0, stream>>>(a, p, s);
   else if (tile_rows == kPagedRows) nibble_rows<T, D, PagedSeqs, 64><<<grid, 256, 0, stream>>>(a, p, s);
+  else return hipErrorInvalidValue;  // no such kernel
   return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@ import subprocess
 import pytest
 import torch
 
-from paper_2607_24788_amd import build, paged
+from paper_2607_24788_amd import build, glide, paged
 
 
 def compiles(tmp_path, text):
@@ -62,3 +62,20 @@ def test_who_attends_to_the_rows():
     assert form([5] * 60, G=8) == form([1, 3] * 64) == TILES  # 1.67, 2
     assert form([2048], page=16, n_select=20) == WAVES       # pages that fill half a tile: by how many rows select one
     assert form([2048], page=16, n_select=400) == TILES
+
+
+def test_launches_of_kernels_that_are_not_there():
+    """An error, not a success with nothing launched."""
+    lib = glide.load_library()
+    args, pools, seqs = ((ctypes.c_char * 4096)() for _ in range(3))
+    ctypes.cast(seqs, ctypes.POINTER(ctypes.c_int32))[0] = 1                           # one sequence,
+    ctypes.cast(seqs, ctypes.POINTER(ctypes.c_int32))[2 + 2 * 128 + 1] = 1             # one tile
+    invalid = 1                                                                        # hipErrorInvalidValue
+    decode = lib._ZN5glide20launch_nibble_decodeERKNS_9PagedArgsERKNS_6Pools4EiiiP12ihipStream_t
+    prefill = lib._ZN5glide21launch_nibble_prefillERKNS_9PagedArgsERKNS_6Pools4ERKNS_9PagedSeqsEiiiP12ihipStream_t
+    for dtype in (0, 1):
+        for d in (64, 128):
+            for keys in (0, 16, 48, 128) + ((32,) if dtype == glide.F32 else ()):
+                assert decode(args, pools, d, dtype, keys, None) == invalid
+            for rows in (0, 32, 64, 512):
+                assert prefill(args, pools, seqs, d, dtype, rows, None) == invalid
