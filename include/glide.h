@@ -473,7 +473,9 @@ glide_status glide_paged_bounds(const glide_paged_config* cfg, const glide_paged
  * an upper bound of sum_h q_h.k_j over the page; it is summed in fp64.  Of equal
  * ones the first; NaN is the smallest.  The row then is softmax attention over
  *   { j <= t : j's page selected }
- * in place of cfg's window and sinks; empty rows as for the other calls. */
+ * in place of cfg's window and sinks; empty rows as for the other calls.
+ * cache->weights are neither read nor added to: an eviction ranks tokens by the
+ * queries that went through glide_paged_prefill and _decode alone. */
 
 /* Workspace bytes of a call of up to max_total_tokens rows: for a launch's
  * rows (of which a call makes several where this would pass 256 MiB, one row's

@@ -301,7 +301,9 @@ class Paged:
         made by ``page_bounds``): the first n_first, the last n_recent, and the
         largest scores of the others.  q, out [T][Hq][d], lse [T][Hq] fp32;
         selected [T][Hkv][n_select] int32: the pages' numbers in their
-        sequence, -1 behind the last.  The queries' tokens are in the cache."""
+        sequence, -1 behind the last.  The queries' tokens are in the cache.  A
+        cache's weights are left as they are: ``evict`` does not know of these
+        queries."""
         bp = self._bounds_of(cache, bounds)
         cu, T = _cu_arg(self, cu_seqlens)
         n_select, n_first, n_recent = (_fits(name, int(x)) for name, x in (

@@ -63,3 +63,14 @@ def test_many_rows_to_a_wave(Hkv, G, page, d, select, form):
     assert sparse_form(case.g, new, select, max(lens)) == form
     rows = {0, 1, R - 1, R, 333 % 700, 699, 700, 701, 1129, 1130, *range(5, 1131, 83)}
     sampled_sparse(case, new, select, sorted(rows), (0, Hkv - 1), max_len=max(lens))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("new", [[1, 1], [3, 9], [600, 40]])
+def test_weights_are_left_as_they_are(dtype, new):
+    """On a cache with weights nothing is added to them, in any of the forms."""
+    lens = [n + 200 for n in new]
+    case = Case(2, 32, 8, 64, 32, lens, dtype=dtype, weights=True, seed=660)
+    before = case.w.clone()
+    sampled_sparse(case, new, 4, sorted({0, sum(new) - 1, sum(new) // 2}), (0, 7), max_len=max(lens))
+    assert torch.equal(case.w.isnan(), before.isnan()) and torch.equal(case.w.nan_to_num(), before.nan_to_num())
