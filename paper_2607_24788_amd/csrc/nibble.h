@@ -26,6 +26,12 @@ hipError_t launch_nibble_decode(const PagedArgs& a, const Pools4& p, int d, int 
 hipError_t launch_nibble_prefill(const PagedArgs& a, const Pools4& p, const PagedSeqs& s, int d, int dtype,
                                  int tile_rows, hipStream_t stream);
 
+// Rows of a workgroup of a prefill (its first launch; pieces: of each row tile), or
+// with cu_seqlens_host NULL the keys of a wave's tile of a decode; not a part of
+// the library's interface (for its tests).
+extern "C" int32_t glide_internal_nibble_plan(const glide_paged_config* cfg, const int32_t* cu_seqlens_host,
+                                              int64_t max_len, int32_t* pieces);
+
 // ---------------------------------------------------------------------------
 // Four bits.  A value is s 2^e: s one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their
 // negatives (three bits: two of exponent, one of mantissa; and a sign), e one

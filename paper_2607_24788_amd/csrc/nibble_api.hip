@@ -76,16 +76,21 @@ int tile_rows4(const glide_paged_config* c, const int32_t* cu, int b0, int b1, i
 //    end weigh more than what shorter pieces even out): 8 sequences of 32768,
 //    1024 / 2048 / 4096 keys 55 / 50 / 54 us; 32 of 16384 .. 32768, 512 / 4096
 //    161 / 151 us (tiles of 64 keys, two to a CU: 192 / 168).
-//  Where that would leave pieces under kSmall4 keys, and for the others (fp32;
-//    d = 64, where 16 sequences of 20000 take 40.7 / 43.3 us in tiles of 64 /
-//    32): tiles of 64 keys, two workgroups to a CU.  One sequence of 32768:
+//  d = 64 in the same way where whole rows of up to 4096 keys make four
+//    workgroups to a CU: 1024 (row, KV head) pairs of 300 / 2000 / 4000 keys 8.7 / 29.6 /
+//    54.7 us (tiles of 64: 11.4 / 36.5 / 66.7), 2048 of 2000 58.3 (61.2), 8192 of
+//    3000 330 (324); in pieces it gains nothing (16 sequences of 20000 41 / 41 us,
+//    96 of 500 .. 40000 with W = 8192 105 / 96).
+//  Where that would leave pieces under kSmall4 keys, and for the others (fp32 among
+//    them): tiles of 64 keys, two workgroups to a CU.  One sequence of 32768:
 //    512 keys 14.1 us (tiles of 32: 256 keys 16.8); of 8192: 256 keys 9.6 us,
 //    512 10.6 (tiles of 32: 10.0).
 int plan_decode4(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
   constexpr int64_t kWhole4 = 1024, kSmall4 = 384, kLeast4 = 256, kMost4 = 4096;
   const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), units = int64_t(c->batch) * c->n_kv_heads;
   const int64_t all = units * keys;
-  const bool large = c->dtype == GLIDE_BF16 && c->head_dim == 128 && all >= kSmall4 * 2 * kPagedRound;
+  const bool many = c->head_dim == 128 ? all >= kSmall4 * 2 * kPagedRound : units >= 2 * kPagedRound && keys <= kMost4;
+  const bool large = c->dtype == GLIDE_BF16 && many;
   int64_t piece = std::min(kMost4, std::max(kLeast4, all / (large ? 2 * kPagedRound : kPagedRound)));
   if (keys <= kWhole4) piece = keys;
   set_pieces(std::min((keys + piece - 1) / piece, max_pieces(units, kPagedRows)), keys, a);
@@ -168,6 +173,22 @@ glide_status glide_nibble_decode(const glide_paged_config* cfg, const glide_nibb
   a.acc = reinterpret_cast<float*>(ws + w.acc);
   a.ml = reinterpret_cast<float*>(ws + w.ml);
   return hip_status(launch_nibble_decode(a, p, cfg->head_dim, cfg->dtype, tile, hipStream_t(stream)));
+}
+
+int32_t glide_internal_nibble_plan(const glide_paged_config* cfg, const int32_t* cu, int64_t max_len,
+                                   int32_t* pieces) {
+  if (!cu) {
+    PagedArgs a;
+    const int tile = plan_decode4(cfg, max_len, &a);
+    *pieces = a.npiece;
+    return tile;
+  }
+  PagedSeqs t;
+  const int b1 = next_launch(cfg, cu, 0, &t, [](int64_t) { return 0; });
+  int64_t n, keys;
+  const int rows = tile_rows4(cfg, cu, 0, b1, max_len, &n, &keys);
+  *pieces = int32_t(n);
+  return rows;
 }
 
 }  // extern "C"

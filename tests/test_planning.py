@@ -8,7 +8,7 @@ import subprocess
 import pytest
 import torch
 
-from paper_2607_24788_amd import build, glide, paged
+from paper_2607_24788_amd import build, glide, paged, paged4
 
 
 def compiles(tmp_path, text):
@@ -62,6 +62,29 @@ def test_who_attends_to_the_rows():
     assert form([5] * 60, G=8) == form([1, 3] * 64) == TILES  # 1.67, 2
     assert form([2048], page=16, n_select=20) == WAVES       # pages that fill half a tile: by how many rows select one
     assert form([2048], page=16, n_select=400) == TILES
+
+
+def nibble_plan(g, new, max_len=0):
+    """Of a 4-bit layer's prefill of `new` rows per sequence: rows of a
+    workgroup, pieces; of its decode (None): keys of a wave's tile, pieces."""
+    cu = None if new is None else (ctypes.c_int32 * (len(new) + 1))(0, *itertools.accumulate(new))
+    n, f = ctypes.c_int32(), g.lib.glide_internal_nibble_plan
+    f.restype, f.argtypes = ctypes.c_int32, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+    return f(ctypes.addressof(g.cfg), None if cu is None else ctypes.addressof(cu), max_len, ctypes.addressof(n)), n.value
+
+
+def test_tiles_of_a_decode():
+    """Every kernel of a decode is one that some call is planned for."""
+    def plan(units, keys, d, dtype=BF16):
+        g = paged4.Paged4(units // 8, 32, 8, d, 64, 1000, 1024, dtype=dtype)
+        return nibble_plan(g, None, keys)
+    assert plan(8, 40000, 128)[0] == 64 and plan(8, 65536, 128)[0] == plan(64, 7000, 128)[0] == 32
+    assert plan(256, 24000, 128) == (32, 6)
+    assert plan(1024, 300, 64) == plan(2048, 4000, 64) == (32, 1)
+    assert plan(1016, 300, 64) == (64, 1) and plan(2048, 5000, 64)[0] == plan(128, 20000, 64)[0] == 64
+    for d in (64, 128):
+        for units, keys in ((1024, 300), (2048, 4000), (256, 24000)):
+            assert plan(units, keys, d, FP32)[0] == 64
 
 
 def test_launches_of_kernels_that_are_not_there():
