@@ -1,0 +1,122 @@
+"""Every kernel of the attention over a 4-bit cache against float64 on the CPU:
+each call asserts the kernel and the pieces that it is planned for."""
+import pytest
+import torch
+
+from paper_2607_24788_amd import paged4
+
+from .paged4_util import Ref4, values
+from .paged_util import check_rows
+from .test_gpu_nibble_more import sampled_prefill4
+from .test_gpu_paged import nan_like
+from .test_planning import nibble_plan
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+class Bytes4:
+    """A 4-bit cache of random bytes (scales near 1 in the pages that are read,
+    any elsewhere).  shared: all sequences have the same pages, in orders of
+    their own."""
+
+    def __init__(self, lens, Hq, Hkv, d, page, window, sinks, dtype, seed, shared=False):
+        self.gen = torch.Generator().manual_seed(seed)
+        B, counts = len(lens), [-(-n // page) for n in lens]
+        used = max(counts) if shared else sum(counts)
+        self.g = g = paged4.Paged4(B, Hq, Hkv, d, page, used + 5, max(counts) + 1, window=window, n_sinks=sinks, dtype=dtype)
+        self.dtype, self.lens_host = dtype, list(lens)
+        self.table = torch.full((B, max(counts) + 1), -1, dtype=torch.int32)
+        ids, at = torch.randperm(used, generator=self.gen).int(), 0
+        for b, n in enumerate(counts):
+            self.table[b, :n] = torch.randperm(used, generator=self.gen).int()[:n] if shared else ids[at:at + n]
+            at += n
+        self.pools = []
+        for _ in range(2):
+            codes = torch.randint(0, 256, (used + 5, Hkv, page, d // 2), generator=self.gen, dtype=torch.uint8)
+            scales = torch.randint(125, 128, (used + 5, Hkv, page, d // 32), generator=self.gen, dtype=torch.uint8)
+            scales[used:] = torch.randint(0, 256, scales[used:].shape, generator=self.gen, dtype=torch.uint8)
+            self.pools.append((codes.cuda(), scales.cuda()))
+        self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        self.dev_table = self.table.cuda()
+        self.cache = g.cache(*self.pools, self.dev_table, self.lens)
+
+    def drop_pages(self, *entries):
+        for b, i in entries:
+            self.table[b, i] = -1 if i % 2 else self.g.n_pages
+        self.dev_table.copy_(self.table)
+
+    def normal(self, *shape):
+        return torch.randn(shape, generator=self.gen).to(self.dtype)
+
+    def ref(self):
+        k, v = (values(*(t.cpu() for t in pool)) for pool in self.pools)
+        return Ref4(self.g, k, v, self.dev_table, self.lens)
+
+
+PREFILL = [
+    # dtype, d, rows of a workgroup, in pieces; Hkv, G, tokens, before them, window, sinks
+    (BF16, 64, 128, False, 4, 3, 700, 0, 333, 70),
+    (BF16, 64, 128, True, 4, 3, 700, 500, 1000, 4),
+    (BF16, 64, 128, True, 1, 3, 300, 3000, None, 0),
+    (BF16, 64, 256, True, 1, 3, 14566, 0, None, 0),
+    (BF16, 128, 128, False, 4, 3, 700, 0, 333, 70),
+    (BF16, 128, 128, True, 4, 3, 700, 500, 1000, 4),
+    (BF16, 128, 128, True, 1, 3, 400, 3000, None, 0),
+    (BF16, 128, 256, False, 16, 3, 700, 77, 1000, 4),
+    (BF16, 128, 256, False, 8, 5, 1000, 0, None, 0),
+    (BF16, 128, 256, True, 2, 8, 700, 3000, None, 0),
+    (FP32, 64, 128, False, 8, 4, 300, 77, 333, 70),
+    (FP32, 64, 128, True, 4, 3, 700, 500, 1000, 4),
+    (FP32, 64, 256, False, 4, 3, 3000, 0, 333, 70),
+    (FP32, 64, 256, True, 16, 3, 700, 77, 1000, 4),
+    (FP32, 64, 256, True, 2, 8, 200, 3000, None, 0),
+    (FP32, 128, 128, False, 16, 3, 300, 0, 333, 70),
+    (FP32, 128, 128, True, 2, 8, 300, 3000, None, 0),
+    (FP32, 128, 256, False, 4, 3, 3000, 77, 333, 70),
+    (FP32, 128, 256, True, 16, 3, 700, 77, 1000, 4),
+    (FP32, 128, 256, True, 1, 3, 1500, 3000, None, 0),
+]
+
+
+@pytest.mark.parametrize("i", range(len(PREFILL)))
+def test_prefill(i):
+    """Ragged sequences, one of them empty and one with more tokens than lens
+    says; a missing page; rows at the tiles' edges and in between."""
+    dtype, d, rows, pieces, Hkv, G, T, hist, W, ns = PREFILL[i]
+    new = [T - 41, 0, 41]
+    if T > 10000:
+        new = [T, 0, 0]
+    lens = [new[0] + hist, 9, 30]
+    case = Bytes4(lens, Hkv * G, Hkv, d, 16, W, ns, dtype, 700 + i)
+    case.drop_pages((0, 2), (0, max(3, lens[0] // 32)), (0, max(4, (lens[0] - 20) // 16)))
+    plan = nibble_plan(case.g, new, max(lens))
+    assert plan[0] == rows and (plan[1] > 1) == pieces, plan
+    per = rows // G
+    at = {0, 1, per - 1, per, per + 1, 2 * per, new[0] - 2, new[0] - 1, new[0] // 2, *range(7, new[0], new[0] // 16 + 1)}
+    at |= set(range(new[0], sum(new)))
+    sampled_prefill4(case, new, sorted(r for r in at if r < sum(new)), max_len=max(lens))
+
+
+@pytest.mark.parametrize("d,G,W,ns,keys", [(128, 4, None, 0, 32), (128, 3, 6500, 5, 32), (128, 16, None, 0, 32),
+                                           (64, 3, None, 0, 32), (64, 8, 100, 7, 32), (64, 1, None, 0, 64)])
+def test_large_decode(d, G, W, ns, keys):
+    """As many rows as take tiles of 32 keys: ragged lengths up to many tiles,
+    a window that begins inside one, sinks, a missing page, empty sequences."""
+    if d == 128:
+        B, Hkv, most = 8, 8, 9001
+    else:
+        B, Hkv, most = (16, 64, 421) if keys == 32 else (8, 8, 421)
+    gen = torch.Generator().manual_seed(740 + G)
+    lens = [most, 0, 1, 33] + torch.randint(most // 2, most, (B - 4,), generator=gen).tolist()
+    case = Bytes4(lens, Hkv * G, Hkv, d, 16, W, ns, BF16, 750 + G, shared=True)
+    case.drop_pages((0, 3), (0, (most - 50) // 16), (4, 8))
+    assert nibble_plan(case.g, None, most)[0] == keys
+    q, g = case.normal(B, Hkv * G, d), case.g
+    out, lse = nan_like(B + 1, Hkv * G, d, dtype=BF16), nan_like(B + 1, Hkv * G, dtype=FP32)
+    g.decode(case.cache, q.cuda(), out, g.new_workspace().fill_(0xff), lse=lse, max_len=most)
+    torch.cuda.synchronize()
+    ref = case.ref()
+    check_rows(out[:B], lse[:B], [ref.row(b, n - 1, q[b], False) for b, n in enumerate(ref.lens)])
+    assert out[B:].isnan().all() and lse[B:].isnan().all()
