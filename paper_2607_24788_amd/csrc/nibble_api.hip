@@ -76,11 +76,12 @@ int tile_rows4(const glide_paged_config* c, const int32_t* cu, int b0, int b1, i
 //    end weigh more than what shorter pieces even out): 8 sequences of 32768,
 //    1024 / 2048 / 4096 keys 55 / 50 / 54 us; 32 of 16384 .. 32768, 512 / 4096
 //    161 / 151 us (tiles of 64 keys, two to a CU: 192 / 168).
-//  d = 64 in the same way where whole rows of up to 4096 keys make four
-//    workgroups to a CU: 1024 (row, KV head) pairs of 300 / 2000 / 4000 keys 8.7 / 29.6 /
-//    54.7 us (tiles of 64: 11.4 / 36.5 / 66.7), 2048 of 2000 58.3 (61.2), 8192 of
-//    3000 330 (324); in pieces it gains nothing (16 sequences of 20000 41 / 41 us,
-//    96 of 500 .. 40000 with W = 8192 105 / 96).
+//  d = 64: tiles of 32 keys where rows of up to 512 keys are more than three
+//    workgroups to a CU, which is what tiles of 64 have at once: 784 rows of 300
+//    keys 8.2 us (64: 10.6), 1024 of 300 8.4 (10.9), 2048 of 300 16.0 (19.6), of 1
+//    .. 500 17.0 (18.8).  768 of 700 11.8 (10.9), 1056 of 700 18.8 (17.6), 1024
+//    of 100 .. 4000 45.5 (44); in pieces nothing is gained (16 sequences of 20000
+//    41 / 41, 96 of 500 .. 40000 with W = 8192 105 / 96).  (1520 of 500: 16.9, 16.2.)
 //  Where that would leave pieces under kSmall4 keys, and for the others (fp32 among
 //    them): tiles of 64 keys, two workgroups to a CU.  One sequence of 32768:
 //    512 keys 14.1 us (tiles of 32: 256 keys 16.8); of 8192: 256 keys 9.6 us,
@@ -89,7 +90,7 @@ int plan_decode4(const glide_paged_config* c, int64_t max_len, PagedArgs* a) {
   constexpr int64_t kWhole4 = 1024, kSmall4 = 384, kLeast4 = 256, kMost4 = 4096;
   const int64_t keys = std::max<int64_t>(1, most_seen(c, max_len)), units = int64_t(c->batch) * c->n_kv_heads;
   const int64_t all = units * keys;
-  const bool many = c->head_dim == 128 ? all >= kSmall4 * 2 * kPagedRound : units >= 2 * kPagedRound && keys <= kMost4;
+  const bool many = c->head_dim == 128 ? all >= kSmall4 * 2 * kPagedRound : units > kPagedRound * 3 / 2 && keys <= 512;
   const bool large = c->dtype == GLIDE_BF16 && many;
   int64_t piece = std::min(kMost4, std::max(kLeast4, all / (large ? 2 * kPagedRound : kPagedRound)));
   if (keys <= kWhole4) piece = keys;

@@ -80,8 +80,8 @@ def test_tiles_of_a_decode():
         return nibble_plan(g, None, keys)
     assert plan(8, 40000, 128)[0] == 64 and plan(8, 65536, 128)[0] == plan(64, 7000, 128)[0] == 32
     assert plan(256, 24000, 128) == (32, 6)
-    assert plan(1024, 300, 64) == plan(2048, 4000, 64) == (32, 1)
-    assert plan(1016, 300, 64) == (64, 1) and plan(2048, 5000, 64)[0] == plan(128, 20000, 64)[0] == 64
+    assert plan(776, 300, 64) == plan(1024, 300, 64) == plan(4096, 512, 64) == (32, 1)
+    assert plan(768, 300, 64) == plan(4096, 513, 64) == (64, 1) and plan(128, 20000, 64)[0] == 64
     for d in (64, 128):
         for units, keys in ((1024, 300), (2048, 4000), (256, 24000)):
             assert plan(units, keys, d, FP32)[0] == 64
