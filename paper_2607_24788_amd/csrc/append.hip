@@ -41,7 +41,7 @@ __device__ __forceinline__ void store8(char* p, const float* x) {
 }
 // Sine and cosine of t turns, |t| <= 1/2, in fp64: the nearest quarter off, then
 // their series up to x^15 / 15! and x^16 / 16!, x at most pi / 4 (what follows is
-// 5e-17 of x at most).  The coefficients come from memory: it is called seldom,
+// 6e-17 of x at most).  The coefficients come from memory: it is called seldom,
 // and they would take registers all along.
 __constant__ const double kSeries[8][2] = {
     {-1. / 1307674368000, 1. / 20922789888000}, {1. / 6227020800, -1. / 87178291200},
@@ -181,11 +181,12 @@ __device__ __forceinline__ void join_bounds(Bounds16& b, float (*red)[32]) {
 //   at position 2^20 the angle is off by 2^-25 of a turn, as at position 1.
 //   4 bits: a code is that of the key rotated in 64 bits.  Few elements come so
 //   near to a step's middle that fp32 could miss it; those alone are worked out
-//   in fp64 (8191 tokens 56.6 us with the read back, 54.3 without; all of them in
-//   fp64 78).
+//   in fp64 (8191 tokens and their read back, builds on one card: 56.6 us, in fp32
+//   alone 54.3, all of them in fp64 78).
 // Bound by HBM in prompts: 8191 tokens of 32 / 8 heads of 128, bf16, with bounds,
 // 202 MB in 46 us (4.4 TB/s; from memory.  Rows are read past the caches: 49 us
-// through them), 36 out of the caches; into 4 bits 177 MB in 48 and 33.  One
+// through them), 36 out of the caches; into 4 bits 177 MB in 48 (3.7 TB/s) and 33:
+// its 122 registers leave four waves to a SIMD, each with a row ahead.  One
 // token of 32 sequences takes 6.1 us, of one fp32 layer 4.6: lens -> table ->
 // bounds, rows and angles.
 // SINGLE: a call of one token per sequence.

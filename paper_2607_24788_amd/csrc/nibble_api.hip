@@ -79,9 +79,9 @@ int tile_rows4(const glide_paged_config* c, const int32_t* cu, int b0, int b1, i
 //  d = 64: tiles of 32 keys where rows of up to 512 keys are more than three
 //    workgroups to a CU, which is what tiles of 64 have at once: 784 rows of 300
 //    keys 8.2 us (64: 10.6), 1024 of 300 8.4 (10.9), 2048 of 300 16.0 (19.6), of 1
-//    .. 500 17.0 (18.8).  768 of 700 11.8 (10.9), 1056 of 700 18.8 (17.6), 1024
-//    of 100 .. 4000 45.5 (44); in pieces nothing is gained (16 sequences of 20000
-//    41 / 41, 96 of 500 .. 40000 with W = 8192 105 / 96).  (1520 of 500: 16.9, 16.2.)
+//    .. 500 17.0 (18.8), 1520 of 500 16.9 (16.2).  Beyond: 768 of 700 11.8 (10.9),
+//    1056 of 700 18.8 (17.6), 1024 of 100 .. 4000 45.5 (44); in pieces, 16
+//    sequences of 20000 41 (41), 96 of 500 .. 40000 with W = 8192 105 (96).
 //  Where that would leave pieces under kSmall4 keys, and for the others (fp32 among
 //    them): tiles of 64 keys, two workgroups to a CU.  One sequence of 32768:
 //    512 keys 14.1 us (tiles of 32: 256 keys 16.8); of 8192: 256 keys 9.6 us,

@@ -55,8 +55,8 @@ __device__ __forceinline__ double sum_lanes(double x) {
 // Scores of pages: with u_c = sum_h max(q_hc, 0) and w_c = sum_h min(q_hc, 0)
 // over the group's heads, sum_c (u_c kmax_c + w_c kmin_c) is no less than
 // sum_h q_h . k of any key of the page, for two products of a row instead of G
-// per key.  In fp64, where products of bf16 numbers are exact: neighbouring
-// pages' scores are told apart alike however the sum is ordered.
+// per key.  In fp64, summed in one order: pages of the same bounds have the same
+// score, and others are told apart down to that sum's rounding.
 // D / 8 lanes to a page, eight elements of both bounds each (asked for a page
 // ahead), for up to eight queries of a sequence.
 template <typename T, int D>

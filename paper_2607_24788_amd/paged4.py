@@ -41,7 +41,7 @@ class Paged4:
                  dtype=torch.bfloat16, sm_scale=None, lib=None):
         g = Paged(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, window, n_sinks, dtype,
                   sm_scale, lib)
-        self.lib, self.cfg, self._ref, self._cu = g.lib, g.cfg, g._ref, g._cu
+        self.lib, self.cfg, self._ref = g.lib, g.cfg, g._ref
         self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = g.batch, g.n_q_heads, g.n_kv_heads, g.head_dim
         self.page_size, self.n_pages, self.max_pages = g.page_size, g.n_pages, g.max_pages
         self.window, self.n_sinks, self.sm_scale, self.torch_dtype = g.window, g.n_sinks, g.sm_scale, g.torch_dtype
