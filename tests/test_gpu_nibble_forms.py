@@ -120,3 +120,28 @@ def test_large_decode(d, G, W, ns, keys):
     ref = case.ref()
     check_rows(out[:B], lse[:B], [ref.row(b, n - 1, q[b], False) for b, n in enumerate(ref.lens)])
     assert out[B:].isnan().all() and lse[B:].isnan().all()
+
+
+@pytest.mark.parametrize("i", [1, 8, 11, 13, 18])
+def test_captured(i):
+    """A prefill captured into a graph, without lse, and replayed after other
+    inputs came in, with eager work between: the bits of the eager call."""
+    dtype, d, rows, pieces, Hkv, G, T, hist, W, ns = PREFILL[i]
+    new = [T - 41, 0, 41]
+    case = Bytes4([new[0] + hist, 9, 30], Hkv * G, Hkv, d, 16, W, ns, dtype, 760 + i)
+    g, q, cu = case.g, case.normal(T, Hkv * G, d).cuda(), [0, new[0], new[0], T]
+    out, ws = torch.empty_like(q), g.new_workspace(T)
+    call = lambda: g.prefill(case.cache, q, cu, out, ws, max_len=new[0] + hist)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n in range(3):
+        q.copy_(case.normal(*q.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.zero_(), ws.fill_(0xff)
+        call()
+        assert torch.equal(got, out) and out.isfinite().all(), n

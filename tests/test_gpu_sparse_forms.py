@@ -74,3 +74,40 @@ def test_weights_are_left_as_they_are(dtype, new):
     before = case.w.clone()
     sampled_sparse(case, new, 4, sorted({0, sum(new) - 1, sum(new) // 2}), (0, 7), max_len=max(lens))
     assert torch.equal(case.w.isnan(), before.isnan()) and torch.equal(case.w.nan_to_num(), before.nan_to_num())
+
+
+@pytest.mark.parametrize("order", ["nhd", "joined"])
+@pytest.mark.parametrize("G,d,page", [(4, 128, 64), (8, 64, 32)])
+def test_shared_waves_over_strided_pools(order, G, d, page):
+    """Rows at other strides, first and last pages kept, a scale below 0."""
+    new, lens = [301, 77], [301 + 500, 77 + 9]
+    case = Case(2, 16 * G, 16, d, page, lens, seed=670 + G, order=order, sm_scale=-0.1)
+    assert sparse_form(case.g, new, 6, max(lens)) == TILES
+    sampled_sparse(case, new, 6, [0, 1, 150, 299, 300, 301, 320, 377], (0, 5, 15), first=2, recent=3, max_len=max(lens))
+
+
+@pytest.mark.parametrize("Hkv,G,new,form", [(16, 4, [300, 45], TILES), (8, 4, [400, 45], WAVES), (4, 4, [30, 1], 0)])
+def test_captured(Hkv, G, new, form):
+    """Each form captured into a graph, without lse, and replayed after other
+    inputs came in, with eager work between: the bits of the eager call."""
+    dtype = FP32 if form == WAVES else BF16
+    lens, T = [n + 400 for n in new], sum(new)
+    case = Case(2, Hkv * G, Hkv, 128, 32, lens, dtype=dtype, seed=680 + Hkv)
+    g, bounds, q = case.g, made_bounds(case), case.normal(T, Hkv * G, 128).cuda()
+    assert sparse_form(g, new, 5, max(lens)) == form
+    out, sel = torch.empty_like(q), torch.empty(T, Hkv, 5, dtype=torch.int32, device="cuda")
+    ws = g.new_sparse_workspace(T, 5)
+    call = lambda: g.sparse(case.cache, bounds, q, cu_of(new), 5, sel, out, ws, max_len=max(lens))  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n in range(3):
+        q.copy_(case.normal(*q.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), sel.clone()
+        out.zero_(), sel.zero_(), ws.fill_(0xff)
+        call()
+        assert torch.equal(got[0], out) and torch.equal(got[1], sel) and out.isfinite().all(), n
